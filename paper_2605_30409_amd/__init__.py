@@ -7,6 +7,10 @@ the frame-wise forward (``frame_forward``, ``gdn_frame_forward*``), the
 frame-wise forward with the normalizer (``frame_forward_norm``), the
 bidirectional frame-wise forward (``frame_forward_bidir``) and the fused
 operator with its prologue and epilogue (``frame_forward_fused``).
+
+Around it (``include/gdn_ops.h``, :mod:`.ops`): the recurrent step of a decoding
+batch (``step``) and the norms, gate and scaled residual between two blocks
+(``block_norm``, ``block_norm_backward``).
 """
 from .gdn import (CHUNK, FRAME_STAGE_NAMES, STAGE_NAMES, GdnError, LIB_PATH,  # noqa: F401
                   default_key_scale, forward, frame_forward, frame_forward_bidir, frame_forward_fused,
@@ -18,3 +22,4 @@ from .gdn import (CHUNK, FRAME_STAGE_NAMES, STAGE_NAMES, GdnError, LIB_PATH,  # 
                   gdn_frame_token_splits, gdn_frame_workspace_bytes, gdn_profile_stages,
                   gdn_scan_group_size, gdn_status_string, gdn_workspace_bytes,
                   gdn_workspace_bytes_ex, lib, workspace)
+from .ops import block_norm, block_norm_backward, block_norm_workspace, step  # noqa: F401

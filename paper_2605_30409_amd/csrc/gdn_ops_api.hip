@@ -1,0 +1,260 @@
+// Host side of the operators in gdn_ops.h: argument validation, the choice of
+// kernel variants, launches, and the extern "C" entry points.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+#include <initializer_list>
+
+#include "gdn_norm.h"
+#include "gdn_ops.h"
+#include "gdn_step.h"
+
+namespace {
+
+bool misaligned(const void *p, uintptr_t to = 16) { return ((uintptr_t)p & (to - 1)) != 0; }
+
+struct Range {
+    uintptr_t lo, hi;
+    Range(const void *p, size_t bytes) : lo((uintptr_t)p), hi((uintptr_t)p + (p ? bytes : 0)) {}
+    bool overlaps(const Range &o) const { return lo < o.hi && o.lo < hi; }
+    bool same(const Range &o) const { return lo == o.lo && hi == o.hi; }
+};
+
+// Launch one kernel whose only argument is a parameter struct; returns the
+// launch's own status (the thread's pending HIP error is neither read nor cleared).
+template <class P>
+int launch(void (*fn)(P), dim3 grid, dim3 block, size_t lds, hipStream_t s, const P &p) {
+    P copy = p;
+    void *args[] = {&copy};
+    return hipLaunchKernel((const void *)fn, grid, block, args, lds, s) == hipSuccess ? GDN_OK : GDN_ERR_HIP;
+}
+
+bool dims_ok(int Dk, int Dv) { return (Dk == 64 || Dk == 128) && (Dv == 64 || Dv == 128); }
+
+// ---------------------------------------------------------------------------
+// Recurrent step.
+
+template <class E, int DK, int DV> int launch_step(const gdn::StepParams<E> &p, hipStream_t s) {
+    const long long units = (long long)p.N * p.H * (DV / gdn::kStepCols);
+    return launch(gdn::gdn_step_kernel<E, DK, DV>, dim3((unsigned)((units + gdn::kStepWaves - 1) / gdn::kStepWaves)),
+                  dim3(64 * gdn::kStepWaves), 0, s, p);
+}
+
+template <class E>
+int run_step(const void *q, const void *k, const void *v, const float *alpha, const float *beta, const float *state_in,
+             const int *slots, const int *lengths, void *out, float *state_out, int N, int L, int P, int Hk, int H,
+             int Dk, int Dv, hipStream_t s) {
+    gdn::StepParams<E> p;
+    p.q = (const E *)q;
+    p.k = (const E *)k;
+    p.v = (const E *)v;
+    p.alpha = alpha;
+    p.beta = beta;
+    p.state_in = state_in;
+    p.slots = slots;
+    p.lengths = lengths;
+    p.out = (E *)out;
+    p.state_out = state_out;
+    p.N = N;
+    p.L = L;
+    p.P = P;
+    p.Hk = Hk;
+    p.H = H;
+    if (Dk == 128) return Dv == 128 ? launch_step<E, 128, 128>(p, s) : launch_step<E, 128, 64>(p, s);
+    return Dv == 128 ? launch_step<E, 64, 128>(p, s) : launch_step<E, 64, 64>(p, s);
+}
+
+// ---------------------------------------------------------------------------
+// Block norm.
+
+constexpr int kNormMaxC = 8192;
+
+// Threads that share a row: 8 channels each.
+int norm_team(int C) {
+    int t = 64;
+    while (t * 8 < C) t *= 2;
+    return t;
+}
+
+// How the gradient's rows are cut into strips (runs of consecutive rows whose
+// sums one team keeps).
+struct Strips {
+    int strips, strip_rows, per_unit, unit_rows;
+};
+
+Strips norm_strips(int R, int gate_tokens) {
+    int rows = (R + 511) / 512;
+    Strips t;
+    if (gate_tokens > rows) {             // a gate row spans strips: partial sums for dgate
+        t.per_unit = (gate_tokens + rows - 1) / rows;
+        t.strip_rows = (gate_tokens + t.per_unit - 1) / t.per_unit;
+        t.per_unit = (gate_tokens + t.strip_rows - 1) / t.strip_rows;
+        t.unit_rows = gate_tokens;
+        t.strips = R / gate_tokens * t.per_unit;
+    } else {                              // strips of whole gate rows
+        t.per_unit = 1;
+        t.strip_rows = t.unit_rows = rows / gate_tokens * gate_tokens;
+        t.strips = (R + t.strip_rows - 1) / t.strip_rows;
+    }
+    return t;
+}
+
+bool norm_shape_ok(int R, int C, int gate_tokens) {
+    return R >= 1 && C >= 1 && gate_tokens >= 1 && R % gate_tokens == 0;
+}
+
+template <class E, int TPR> int launch_norm(const gdn::NormParams<E> &p, bool grad, hipStream_t s) {
+    constexpr int threads = gdn::norm_threads<TPR>(), teams = threads / TPR;
+    const dim3 grid((unsigned)((p.strips + teams - 1) / teams));
+    if (!grad) return launch(gdn::gdn_block_norm_kernel<E, TPR>, grid, dim3(threads), 0, s, p);
+    const int st = launch(gdn::gdn_block_norm_grad_kernel<E, TPR>, grid, dim3(threads), 0, s, p);
+    if (st != GDN_OK) return st;
+    const unsigned gates = p.gate && p.per_unit > 1 ? (unsigned)(p.R / p.gate_tokens) : 0u;
+    return launch(gdn::gdn_block_norm_reduce_kernel<E>, dim3((unsigned)((2 * p.C + 63) / 64), 1 + gates),
+                  dim3(64 * gdn::kNormReduceWaves), 0, s, p);
+}
+
+template <class E> int dispatch_norm(const gdn::NormParams<E> &p, bool grad, hipStream_t s) {
+    switch (norm_team(p.C)) {
+    case 64: return launch_norm<E, 64>(p, grad, s);
+    case 128: return launch_norm<E, 128>(p, grad, s);
+    case 256: return launch_norm<E, 256>(p, grad, s);
+    case 512: return launch_norm<E, 512>(p, grad, s);
+    default: return launch_norm<E, 1024>(p, grad, s);
+    }
+}
+
+size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+
+}  // namespace
+
+extern "C" {
+
+int gdn_step_forward(const void *q, const void *k, const void *v, const float *alpha, const float *beta,
+                     const float *state_in, const int *slots, const int *lengths, void *out,
+                     float *state_out, int N, int L, int P, int Hk, int H, int Dk, int Dv, int is_bf16,
+                     void *stream) {
+    if (!q || !k || !v || !alpha || !beta || !state_in || !out || !state_out) return GDN_ERR_NULL;
+    if (N < 1 || L < 1 || P < 1 || Hk < 1 || H < 1 || H % Hk || (!slots && N > P)) return GDN_ERR_SHAPE;
+    if ((long long)N * H > (1LL << 30)) return GDN_ERR_SHAPE;
+    if (!dims_ok(Dk, Dv)) return GDN_ERR_UNSUPPORTED;
+    for (const void *p : {q, k, v, (const void *)alpha, (const void *)beta, (const void *)state_in, (const void *)out,
+                          (const void *)state_out})
+        if (misaligned(p)) return GDN_ERR_ALIGN;
+    if (misaligned(slots, 4) || misaligned(lengths, 4)) return GDN_ERR_ALIGN;
+    const size_t esz = is_bf16 ? 2 : 4, nt = (size_t)N * L;
+    const Range ro(out, nt * H * Dv * esz), rs(state_out, (size_t)P * H * Dk * Dv * 4),
+        ri(state_in, (size_t)P * H * Dk * Dv * 4);
+    for (const Range &r : {Range(q, nt * Hk * Dk * esz), Range(k, nt * Hk * Dk * esz), Range(v, nt * H * Dv * esz),
+                           Range(alpha, nt * H * 4), Range(beta, nt * H * 4), Range(slots, (size_t)N * 4),
+                           Range(lengths, (size_t)N * 4)})
+        if (ro.overlaps(r) || rs.overlaps(r)) return GDN_ERR_ALIAS;
+    if (ro.overlaps(rs) || ro.overlaps(ri) || (rs.overlaps(ri) && !rs.same(ri))) return GDN_ERR_ALIAS;
+    const auto run = is_bf16 ? run_step<uint16_t> : run_step<float>;
+    return run(q, k, v, alpha, beta, state_in, slots, lengths, out, state_out, N, L, P, Hk, H, Dk, Dv,
+               (hipStream_t)stream);
+}
+
+int gdn_block_norm_forward(const void *x, const void *y, const void *gate, const float *w_post,
+                           const float *w_pre, void *r, void *u, int R, int C, int gate_tokens,
+                           float res_scale, float eps, int is_bf16, void *stream) {
+    if (!x || !y || !w_post || !w_pre || !r || !u) return GDN_ERR_NULL;
+    if (!norm_shape_ok(R, C, gate_tokens)) return GDN_ERR_SHAPE;
+    if (C > kNormMaxC) return GDN_ERR_UNSUPPORTED;
+    for (const void *p : {x, y, gate, (const void *)w_post, (const void *)w_pre, (const void *)r, (const void *)u})
+        if (misaligned(p)) return GDN_ERR_ALIGN;
+    const size_t bytes = (size_t)R * C * (is_bf16 ? 2 : 4);
+    const Range rx(x, bytes), ry(y, bytes), rr(r, bytes), ru(u, bytes);
+    for (const Range &o : {Range(gate, bytes / gate_tokens), Range(w_post, (size_t)C * 4), Range(w_pre, (size_t)C * 4)})
+        if (rr.overlaps(o) || ru.overlaps(o)) return GDN_ERR_ALIAS;
+    if (rr.overlaps(ru) || ru.overlaps(rx) || (ru.overlaps(ry) && !ru.same(ry)) ||
+        (rr.overlaps(rx) && !rr.same(rx)) || (rr.overlaps(ry) && !rr.same(ry)))
+        return GDN_ERR_ALIAS;
+    auto run = [&](auto *e) {
+        using E = std::remove_pointer_t<decltype(e)>;
+        gdn::NormParams<E> p{};
+        p.x = (const E *)x;
+        p.y = (const E *)y;
+        p.gate = (const E *)gate;
+        p.w_post = w_post;
+        p.w_pre = w_pre;
+        p.r = (E *)r;
+        p.u = (E *)u;
+        p.R = R;
+        p.C = C;
+        p.gate_tokens = gate_tokens;
+        p.strip_rows = (R + 2047) / 2048;
+        p.strips = (R + p.strip_rows - 1) / p.strip_rows;
+        p.res_scale = res_scale;
+        p.eps = eps;
+        return dispatch_norm<E>(p, false, (hipStream_t)stream);
+    };
+    return is_bf16 ? run((uint16_t *)nullptr) : run((float *)nullptr);
+}
+
+size_t gdn_block_norm_workspace_bytes(int R, int C, int gate_tokens) {
+    if (!norm_shape_ok(R, C, gate_tokens) || C > kNormMaxC) return 0;
+    const Strips t = norm_strips(R, gate_tokens);
+    return align256((size_t)t.strips * 2 * C * 4) + align256(t.per_unit > 1 ? (size_t)t.strips * C * 4 : 0);
+}
+
+int gdn_block_norm_backward(const void *x, const void *y, const void *gate, const float *w_post,
+                            const float *w_pre, const void *du, const void *dr, void *dx, void *dy,
+                            void *dgate, float *dw_post, float *dw_pre, int R, int C, int gate_tokens,
+                            float res_scale, float eps, int is_bf16, void *ws, size_t ws_bytes,
+                            void *stream) {
+    if (!x || !y || !w_post || !w_pre || !du || !dx || !dy || !dw_post || !dw_pre || !gate != !dgate) return GDN_ERR_NULL;
+    if (!norm_shape_ok(R, C, gate_tokens)) return GDN_ERR_SHAPE;
+    if (C > kNormMaxC) return GDN_ERR_UNSUPPORTED;
+    for (const void *p : {x, y, gate, (const void *)w_post, (const void *)w_pre, du, dr, (const void *)dx,
+                          (const void *)dy, (const void *)dgate, (const void *)dw_post, (const void *)dw_pre})
+        if (misaligned(p)) return GDN_ERR_ALIGN;
+    if (!ws || misaligned(ws, 256) || ws_bytes < gdn_block_norm_workspace_bytes(R, C, gate_tokens))
+        return GDN_ERR_WORKSPACE;
+    const size_t bytes = (size_t)R * C * (is_bf16 ? 2 : 4), wb = (size_t)C * 4;
+    const Range in[] = {Range(x, bytes), Range(gate, bytes / gate_tokens), Range(w_post, wb), Range(w_pre, wb),
+                        Range(y, bytes), Range(du, bytes), Range(dr, bytes)};
+    const Range outs[] = {Range(dx, bytes), Range(dy, bytes), Range(dgate, bytes / gate_tokens), Range(dw_post, wb),
+                          Range(dw_pre, wb), Range(ws, gdn_block_norm_workspace_bytes(R, C, gate_tokens))};
+    for (int i = 0; i < 6; ++i) {
+        for (int j = 0; j < 7; ++j) {
+            // a row's y, du and dr are in registers before its dx and dy are written
+            const bool shared = (i == 0 && j >= 5) || (i == 1 && j >= 4);
+            if (outs[i].overlaps(in[j]) && !(shared && outs[i].same(in[j]))) return GDN_ERR_ALIAS;
+        }
+        for (int j = 0; j < i; ++j)
+            if (outs[i].overlaps(outs[j])) return GDN_ERR_ALIAS;
+    }
+    auto run = [&](auto *e) {
+        using E = std::remove_pointer_t<decltype(e)>;
+        const Strips t = norm_strips(R, gate_tokens);
+        gdn::NormParams<E> p{};
+        p.x = (const E *)x;
+        p.y = (const E *)y;
+        p.gate = (const E *)gate;
+        p.w_post = w_post;
+        p.w_pre = w_pre;
+        p.du = (const E *)du;
+        p.dr = (const E *)dr;
+        p.dx = (E *)dx;
+        p.dy = (E *)dy;
+        p.dgate = (E *)dgate;
+        p.dw_post = dw_post;
+        p.dw_pre = dw_pre;
+        p.part_w = (float *)ws;
+        p.part_g = (float *)((unsigned char *)ws + align256((size_t)t.strips * 2 * C * 4));
+        p.R = R;
+        p.C = C;
+        p.gate_tokens = gate_tokens;
+        p.strips = t.strips;
+        p.strip_rows = t.strip_rows;
+        p.per_unit = t.per_unit;
+        p.unit_rows = t.unit_rows;
+        p.res_scale = res_scale;
+        p.eps = eps;
+        return dispatch_norm<E>(p, true, (hipStream_t)stream);
+    };
+    return is_bf16 ? run((uint16_t *)nullptr) : run((float *)nullptr);
+}
+
+}  // extern "C"

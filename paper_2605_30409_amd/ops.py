@@ -1,0 +1,207 @@
+"""The operators around the gated delta-rule forward (include/gdn_ops.h): the
+recurrent step of a decoding batch, and the norms, gate and scaled residual
+between two blocks with their gradient.
+
+Thin binding like :mod:`.gdn`: argument checks and marshalling only.  Outputs and
+workspaces that are not given are allocated on the stream the call runs on.
+"""
+import ctypes
+
+import torch
+
+from . import gdn as _gdn
+from .gdn import GDN_OK, GdnError
+
+_fns = None
+
+
+def _lib():
+    global _fns
+    if _fns is None:
+        L = _gdn.lib()
+        vp, i, sz, fl = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_float
+        L.gdn_step_forward.restype = i
+        L.gdn_step_forward.argtypes = [vp] * 10 + [i] * 8 + [vp]
+        L.gdn_block_norm_forward.restype = i
+        L.gdn_block_norm_forward.argtypes = [vp] * 7 + [i] * 3 + [fl] * 2 + [i, vp]
+        L.gdn_block_norm_workspace_bytes.restype = sz
+        L.gdn_block_norm_workspace_bytes.argtypes = [i] * 3
+        L.gdn_block_norm_backward.restype = i
+        L.gdn_block_norm_backward.argtypes = [vp] * 12 + [i] * 3 + [fl] * 2 + [i, vp, sz, vp]
+        _fns = L
+    return _fns
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _call(name, dev, *args):
+    """The C call with the current stream of `dev` behind its other arguments."""
+    fn = getattr(_lib(), name)
+    stream = torch.cuda.current_stream(dev).cuda_stream
+    if torch.cuda.current_device() == dev.index:
+        rc = fn(*args, stream)
+    else:
+        with torch.cuda.device(dev):
+            rc = fn(*args, stream)
+    if rc != GDN_OK:
+        raise GdnError(name, rc)
+
+
+def _need(name, t, shape, dtype, dev):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a tensor, got {type(t).__name__}")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if tuple(t.shape) != shape:
+        raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
+    if t.device != dev:
+        raise ValueError(f"{name} must be on {dev}, got {t.device}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+
+
+def _element(name, t):
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a tensor, got {type(t).__name__}")
+    if t.dtype not in (torch.bfloat16, torch.float32):
+        raise TypeError(f"{name} must be bfloat16 or float32, got {t.dtype}")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} must be on a GPU, got {t.device}")
+    return t.dtype, t.device
+
+
+def _dims(name, t, dims, text):
+    if t.dim() != dims:
+        raise ValueError(f"{name} must be {text}, got {list(t.shape)}")
+    return tuple(t.shape)
+
+
+def step(q, k, v, alpha, beta, state, *, slots=None, lengths=None, out=None, state_out=None, stream=None):
+    """The recurrent form of ``forward``: up to L new tokens of N sequences, against
+    states kept in a pool.
+
+    q, k [N, L, Hk, Dk] and v [N, L, H, Dv], bf16 or fp32, with Hk a divisor of H (H / Hk
+    consecutive heads share a key head); alpha, beta [N, L, H] fp32; state
+    [P, H, Dk, Dv] fp32.  slots [N] int32 names each row's state (None: row n has
+    slot n), lengths [N] int32 how many of its L tokens are there (None: all).  The
+    states are updated in place unless state_out, a pool of the same shape, is
+    given.  A negative slot is padding: nothing of its row is written.  Tokens
+    past a row's length, and slots that no row names, are left as they were (an out
+    that is allocated here is zero there).  A slot beyond the pool, or named by an earlier row too,
+    makes the row's out NaN and writes no state.  Returns (out [N, L, H, Dv] like v, state_out)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return step(q, k, v, alpha, beta, state, slots=slots, lengths=lengths, out=out, state_out=state_out)
+    dt, dev = _element("q", q)
+    N, L, Hk, Dk = _dims("q", q, 4, "[N, L, Hk, Dk]")
+    H, Dv = _dims("v", v, 4, "[N, L, H, Dv]")[2:]
+    P = _dims("state", state, 4, "[P, H, Dk, Dv]")[0]
+    _need("q", q, (N, L, Hk, Dk), dt, dev)
+    _need("k", k, (N, L, Hk, Dk), dt, dev)
+    _need("v", v, (N, L, H, Dv), dt, dev)
+    _need("alpha", alpha, (N, L, H), torch.float32, dev)
+    _need("beta", beta, (N, L, H), torch.float32, dev)
+    _need("state", state, (P, H, Dk, Dv), torch.float32, dev)
+    if slots is not None:
+        _need("slots", slots, (N,), torch.int32, dev)
+    if lengths is not None:
+        _need("lengths", lengths, (N,), torch.int32, dev)
+    if out is None:
+        # every element is written unless a row may be short or padding
+        new = torch.empty if slots is None and lengths is None else torch.zeros
+        out = new((N, L, H, Dv), dtype=dt, device=dev)
+    else:
+        _need("out", out, (N, L, H, Dv), dt, dev)
+    if state_out is None:
+        state_out = state
+    else:
+        _need("state_out", state_out, (P, H, Dk, Dv), torch.float32, dev)
+    _call("gdn_step_forward", dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), alpha.data_ptr(), beta.data_ptr(),
+          state.data_ptr(), _ptr(slots), _ptr(lengths), out.data_ptr(), state_out.data_ptr(), N, L, P, Hk, H, Dk, Dv,
+          1 if dt == torch.bfloat16 else 0)
+    return out, state_out
+
+
+def block_norm_workspace(rows, channels, gate_tokens, device):
+    """Workspace tensor for block_norm_backward on `rows` tokens of `channels`."""
+    n = _lib().gdn_block_norm_workspace_bytes(rows, channels, gate_tokens)
+    if n == 0:
+        raise ValueError("unsupported shape for the block norm")
+    return torch.empty(n, dtype=torch.uint8, device=device)
+
+
+def _block_inputs(x, y, gate, w_post, w_pre, gate_tokens):
+    dt, dev = _element("x", x)
+    B, T, C = _dims("x", x, 3, "[B, T, C]")
+    gt = int(gate_tokens)
+    if gt < 1 or T % gt:
+        raise ValueError("T must be a whole number of runs of gate_tokens tokens")
+    _need("x", x, (B, T, C), dt, dev)
+    _need("y", y, (B, T, C), dt, dev)
+    if gate is not None:
+        _need("gate", gate, (B, T // gt, C), dt, dev)
+    _need("w_post", w_post, (C,), torch.float32, dev)
+    _need("w_pre", w_pre, (C,), torch.float32, dev)
+    return dt, dev, B, T, C, gt
+
+
+def _given(name, t, shape, dtype, dev):
+    if t is None:
+        return torch.empty(shape, dtype=dtype, device=dev)
+    _need(name, t, shape, dtype, dev)
+    return t
+
+
+def block_norm(x, y, gate, w_post, w_pre, *, gate_tokens=1, res_scale=1.0, eps=1e-6, r=None, u=None, stream=None):
+    """The border between two blocks: with the residual stream x and a block's output y
+    (both [B, T, C], bf16 or fp32),
+
+        r = res_scale x + gate o RMSNorm(y; w_post),     u = RMSNorm(r; w_pre).
+
+    gate [B, T / gate_tokens, C] (like x, or None for ones) has one row for each run of
+    gate_tokens consecutive tokens: 1 per token, T per sample; w_post, w_pre [C]
+    fp32; C at most 8192.  r (the next residual stream) and u (the next block's
+    input) are allocated unless given; r may be x or y, u may be y.  Returns (r, u)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return block_norm(x, y, gate, w_post, w_pre, gate_tokens=gate_tokens, res_scale=res_scale, eps=eps, r=r, u=u)
+    dt, dev, B, T, C, gt = _block_inputs(x, y, gate, w_post, w_pre, gate_tokens)
+    r = _given("r", r, (B, T, C), dt, dev)
+    u = _given("u", u, (B, T, C), dt, dev)
+    _call("gdn_block_norm_forward", dev, x.data_ptr(), y.data_ptr(), _ptr(gate), w_post.data_ptr(), w_pre.data_ptr(),
+          r.data_ptr(), u.data_ptr(), B * T, C, gt, float(res_scale), float(eps), 1 if dt == torch.bfloat16 else 0)
+    return r, u
+
+
+def block_norm_backward(x, y, gate, w_post, w_pre, du, dr=None, *, gate_tokens=1, res_scale=1.0, eps=1e-6, dx=None,
+                        dy=None, dgate=None, dw_post=None, dw_pre=None, ws=None, stream=None):
+    """Gradient of ``block_norm`` from du = dL/du and dr = dL/dr ([B, T, C] like x; dr None:
+    zero).  The other arguments are those of the forward call.  dx may be dr or du, dy
+    may be y or the other of them.  Returns (dx, dy, dgate, dw_post, dw_pre); dgate is
+    None where gate is."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return block_norm_backward(x, y, gate, w_post, w_pre, du, dr, gate_tokens=gate_tokens, res_scale=res_scale,
+                                       eps=eps, dx=dx, dy=dy, dgate=dgate, dw_post=dw_post, dw_pre=dw_pre, ws=ws)
+    dt, dev, B, T, C, gt = _block_inputs(x, y, gate, w_post, w_pre, gate_tokens)
+    _need("du", du, (B, T, C), dt, dev)
+    if dr is not None:
+        _need("dr", dr, (B, T, C), dt, dev)
+    dx = _given("dx", dx, (B, T, C), dt, dev)
+    dy = _given("dy", dy, (B, T, C), dt, dev)
+    if gate is not None:
+        dgate = _given("dgate", dgate, (B, T // gt, C), dt, dev)
+    elif dgate is not None:
+        raise ValueError("dgate without gate")
+    dw_post = _given("dw_post", dw_post, (C,), torch.float32, dev)
+    dw_pre = _given("dw_pre", dw_pre, (C,), torch.float32, dev)
+    if ws is None:
+        ws = block_norm_workspace(B * T, C, gt, dev)
+    elif ws.device != dev or ws.dtype != torch.uint8 or not ws.is_contiguous():
+        raise ValueError(f"ws must be a contiguous uint8 tensor on {dev}")
+    _call("gdn_block_norm_backward", dev, x.data_ptr(), y.data_ptr(), _ptr(gate), w_post.data_ptr(), w_pre.data_ptr(),
+          du.data_ptr(), _ptr(dr), dx.data_ptr(), dy.data_ptr(), _ptr(dgate), dw_post.data_ptr(), dw_pre.data_ptr(),
+          B * T, C, gt, float(res_scale), float(eps), 1 if dt == torch.bfloat16 else 0, ws.data_ptr(), ws.numel())
+    return dx, dy, dgate, dw_post, dw_pre

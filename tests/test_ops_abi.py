@@ -1,0 +1,108 @@
+"""Host-side checks of the operators in gdn_ops.h: exported symbols, workspace sizes and
+refused arguments (no kernel is launched: addresses are made up, or the tensors
+are on the host)."""
+import ctypes
+import os
+import re
+
+import pytest
+import torch
+
+import paper_2605_30409_amd as gdn
+from paper_2605_30409_amd import ops
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+NULL, SHAPE, UNSUPPORTED, WORKSPACE, ALIGN, ALIAS = -1, -2, -3, -4, -6, -7
+BASE, MB = 1 << 40, 1 << 20
+
+
+def test_exported():
+    src = re.sub(r"/\*.*?\*/", "", open(os.path.join(ROOT, "include", "gdn_ops.h")).read(), flags=re.S)
+    names = sorted(set(re.findall(r"\b(gdn_[a-z0-9_]+)\s*\(", src)))
+    assert "gdn_step_forward" in names and "gdn_block_norm_backward" in names
+    lib = ctypes.CDLL(gdn.LIB_PATH)
+    for n in names:
+        assert hasattr(lib, n), n
+
+
+def addr(i):
+    return BASE + i * 64 * MB
+
+
+STEP = dict(q=addr(0), k=addr(1), v=addr(2), alpha=addr(3), beta=addr(4), state_in=addr(5), slots=addr(6),
+            lengths=addr(7), out=addr(8), state_out=addr(9), N=3, L=2, P=4, Hk=2, H=4, Dk=64, Dv=128, bf16=1)
+
+
+def step(**kw):
+    a = dict(STEP, **kw)
+    return ops._lib().gdn_step_forward(*a.values(), None)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(q=None), NULL), (dict(k=None), NULL), (dict(v=None), NULL), (dict(alpha=None), NULL),
+    (dict(beta=None), NULL), (dict(state_in=None), NULL), (dict(out=None), NULL), (dict(state_out=None), NULL),
+    (dict(N=0), SHAPE), (dict(L=0), SHAPE), (dict(P=0), SHAPE), (dict(Hk=0), SHAPE), (dict(H=0), SHAPE),
+    (dict(H=3), SHAPE), (dict(N=-1), SHAPE), (dict(slots=None, N=5), SHAPE), (dict(N=1 << 20, H=1 << 12), SHAPE),
+    (dict(Dk=96), UNSUPPORTED), (dict(Dv=32), UNSUPPORTED),
+    (dict(q=addr(0) + 8), ALIGN), (dict(state_out=addr(9) + 4), ALIGN), (dict(slots=addr(6) + 2), ALIGN),
+    (dict(lengths=addr(7) + 1), ALIGN),
+    (dict(out=addr(2)), ALIAS), (dict(out=addr(5)), ALIAS), (dict(out=addr(6)), ALIAS), (dict(state_out=addr(8)), ALIAS),
+    (dict(state_out=addr(5) + 16), ALIAS), (dict(state_out=addr(0)), ALIAS), (dict(state_out=addr(7)), ALIAS)])
+def test_step_refusals(kw, want):
+    assert step(**kw) == want
+
+
+NORM = dict(x=addr(0), y=addr(1), gate=addr(2), w_post=addr(3), w_pre=addr(4), r=addr(5), u=addr(6), R=12, C=40, gt=4,
+            rs=1.0, eps=1e-6, bf16=1)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(x=None), NULL), (dict(y=None), NULL), (dict(w_post=None), NULL), (dict(w_pre=None), NULL), (dict(r=None), NULL),
+    (dict(u=None), NULL), (dict(R=0), SHAPE), (dict(C=0), SHAPE), (dict(gt=0), SHAPE), (dict(gt=5), SHAPE),
+    (dict(C=8193), UNSUPPORTED), (dict(x=addr(0) + 2), ALIGN), (dict(gate=addr(2) + 8), ALIGN),
+    (dict(r=addr(6)), ALIAS), (dict(u=addr(0)), ALIAS), (dict(r=addr(0) + 16), ALIAS), (dict(u=addr(1) + 16), ALIAS),
+    (dict(r=addr(2)), ALIAS), (dict(u=addr(3)), ALIAS)])
+def test_norm_refusals(kw, want):
+    assert ops._lib().gdn_block_norm_forward(*dict(NORM, **kw).values(), None) == want
+
+
+GRAD = dict(x=addr(0), y=addr(1), gate=addr(2), w_post=addr(3), w_pre=addr(4), du=addr(5), dr=addr(6), dx=addr(7),
+            dy=addr(8), dgate=addr(9), dw_post=addr(10), dw_pre=addr(11), R=12, C=40, gt=4, rs=1.0, eps=1e-6, bf16=1,
+            ws=addr(12), ws_bytes=MB)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(x=None), NULL), (dict(du=None), NULL), (dict(dx=None), NULL), (dict(dw_pre=None), NULL),
+    (dict(gate=None), NULL), (dict(dgate=None), NULL), (dict(R=13), SHAPE), (dict(C=9000), UNSUPPORTED),
+    (dict(dy=addr(8) + 8), ALIGN), (dict(dr=addr(6) + 4), ALIGN), (dict(ws=None), WORKSPACE),
+    (dict(ws=addr(12) + 128), WORKSPACE), (dict(ws_bytes=1000), WORKSPACE), (dict(dx=addr(0)), ALIAS),
+    (dict(dx=addr(1)), ALIAS), (dict(dy=addr(0)), ALIAS), (dict(dx=addr(8)), ALIAS), (dict(dgate=addr(2)), ALIAS),
+    (dict(dw_pre=addr(10)), ALIAS), (dict(ws=addr(5)), ALIAS), (dict(ws=addr(11)), ALIAS),
+    (dict(dx=addr(5) + 16), ALIAS)])
+def test_norm_gradient_refusals(kw, want):
+    assert ops._lib().gdn_block_norm_backward(*dict(GRAD, **kw).values(), None) == want
+
+
+def test_norm_workspace():
+    f = ops._lib().gdn_block_norm_workspace_bytes
+    assert f(12, 40, 5) == 0 and f(0, 40, 1) == 0 and f(12, 8193, 1) == 0
+    for R, C, gt in ((1, 1, 1), (12, 40, 4), (10560, 2048, 3520), (100000, 8, 1), (99999, 16, 3), (700, 64, 700)):
+        n = f(R, C, gt)
+        rows = -(-R // 512)
+        assert 0 < n <= 12 * C * (R // max(1, min(rows, gt)) + R // gt + 1) + 1024
+
+
+def test_host_tensors_are_refused():
+    """No fallback: a tensor that is not on a GPU is an error."""
+    z = torch.zeros
+    q, v = z(1, 1, 2, 64), z(1, 1, 2, 64)
+    with pytest.raises(ValueError, match="GPU"):
+        gdn.step(q, q, v, z(1, 1, 2), z(1, 1, 2), z(1, 2, 64, 64))
+    with pytest.raises(TypeError, match="bfloat16"):
+        gdn.step(q.half(), q, v, z(1, 1, 2), z(1, 1, 2), z(1, 2, 64, 64))
+    with pytest.raises(ValueError, match="GPU"):
+        gdn.block_norm(z(1, 2, 8), z(1, 2, 8), None, z(8), z(8))
+    with pytest.raises(ValueError, match="GPU"):
+        gdn.block_norm_backward(z(1, 2, 8), z(1, 2, 8), None, z(8), z(8), z(1, 2, 8))
+    with pytest.raises(TypeError, match="tensor"):
+        gdn.block_norm([1.0], z(1, 2, 8), None, z(8), z(8))
