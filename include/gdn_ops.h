@@ -1,7 +1,8 @@
 /*
  * gdn_ops.h -- C ABI of the operators around the gated delta-rule forward of
- * gdn.h: the recurrent step of a decoding batch, and the norms, gate and scaled
- * residual between two blocks with their gradient.  Same library, same
+ * gdn.h: the recurrent step of a decoding batch, the gradient of the token-wise
+ * chunk forward, and the norms, gate and scaled residual between two blocks with
+ * their gradient.  Same library, same
  * conventions (device pointers on the current HIP device, 16-byte aligned and
  * contiguous unless said otherwise; asynchronous on `stream`; arguments checked
  * on the host, nothing enqueued on an error; values not checked) and the same
@@ -48,6 +49,37 @@ int gdn_step_forward(const void *q, const void *k, const void *v, const float *a
                      const float *state_in, const int *slots, const int *lengths, void *out,
                      float *state_out, int N, int L, int P, int Hk, int H, int Dk, int Dv, int is_bf16,
                      void *stream);
+
+/*
+ * Gradient of gdn_chunk_forward: from dout = dL/d(out) and dstate_out =
+ * dL/d(state_out) (NULL: zero), with the inputs of the forward call,
+ *
+ *   dq, dk [B][T][H][Dk], dv [B][T][H][Dv]   E
+ *   dalpha, dbeta [B][T][H]                  fp32
+ *   dstate_in [B][H][Dk][Dv]                 fp32, or NULL to drop it
+ *
+ * dout is E [B][T][H][Dv], dstate_out fp32 [B][H][Dk][Dv]; the other inputs, the
+ * sizes and chunk are those of gdn_chunk_forward.  Nothing of the forward call is
+ * needed but its inputs: states and pseudo-values are formed again.  All
+ * gradients are those of the recurrence itself: alpha and beta of 0 have theirs
+ * too (alpha below 1.2e-38 acts as that value, as in the forward).  Sums, states
+ * and their gradients are fp32; on the bf16 path the operands of products that are
+ * not inputs keep 16 bits of mantissa (a pair of bf16), so that the fp32 results
+ * are good to about 1e-5 of their size.  Results are deterministic.
+ *
+ * Outputs may not overlap inputs or each other, except dstate_in == dstate_out.
+ * `ws`: caller-owned device buffer, 256-byte aligned, of at least
+ * gdn_chunk_backward_workspace_bytes(...) bytes (0 for arguments that the call
+ * refuses; 321 KB a chunk and head at Dk = Dv = 128).  Calls that run at once need
+ * one each.
+ */
+size_t gdn_chunk_backward_workspace_bytes(int B, int H, int T, int Dk, int Dv, int chunk, int is_bf16);
+
+int gdn_chunk_backward(const void *q, const void *k, const void *v, const float *alpha, const float *beta,
+                       const float *state_in, const void *dout, const float *dstate_out, void *dq,
+                       void *dk, void *dv, float *dalpha, float *dbeta, float *dstate_in, int B, int H,
+                       int T, int Dk, int Dv, int chunk, int is_bf16, void *ws, size_t ws_bytes,
+                       void *stream);
 
 /*
  * The border between two blocks, for R rows (tokens) of C channels: the norm

@@ -9,7 +9,7 @@ bidirectional frame-wise forward (``frame_forward_bidir``) and the fused
 operator with its prologue and epilogue (``frame_forward_fused``).
 
 Around it (``include/gdn_ops.h``, :mod:`.ops`): the recurrent step of a decoding
-batch (``step``) and the norms, gate and scaled residual between two blocks
+batch (``step``), the gradient of ``forward`` (``backward``), and the norms, gate and scaled residual between two blocks
 (``block_norm``, ``block_norm_backward``).
 """
 from .gdn import (CHUNK, FRAME_STAGE_NAMES, STAGE_NAMES, GdnError, LIB_PATH,  # noqa: F401
@@ -22,4 +22,5 @@ from .gdn import (CHUNK, FRAME_STAGE_NAMES, STAGE_NAMES, GdnError, LIB_PATH,  # 
                   gdn_frame_token_splits, gdn_frame_workspace_bytes, gdn_profile_stages,
                   gdn_scan_group_size, gdn_status_string, gdn_workspace_bytes,
                   gdn_workspace_bytes_ex, lib, workspace)
-from .ops import block_norm, block_norm_backward, block_norm_workspace, step  # noqa: F401
+from .ops import (backward, backward_workspace, block_norm, block_norm_backward,  # noqa: F401
+                  block_norm_workspace, step)

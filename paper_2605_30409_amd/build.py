@@ -9,8 +9,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libgdn.so")
 SOURCES = [os.path.join(CSRC, f) for f in ("gdn_api.hip", "gdn_ops_api.hip")]
-HEADERS = [os.path.join(CSRC, f) for f in ("gdn_device.h", "gdn_frame.h", "gdn_kernels.h", "gdn_norm.h",
-                                           "gdn_step.h")] + \
+HEADERS = [os.path.join(CSRC, f) for f in ("gdn_backward.h", "gdn_device.h", "gdn_frame.h",
+                                           "gdn_kernels.h", "gdn_norm.h", "gdn_step.h")] + \
           [os.path.join(INCLUDE, f) for f in ("gdn.h", "gdn_ops.h")]
 
 HIPCC_FLAGS = [

@@ -4,7 +4,10 @@
 
 #include <cstdint>
 #include <initializer_list>
+#include <mutex>
+#include <type_traits>
 
+#include "gdn_backward.h"
 #include "gdn_norm.h"
 #include "gdn_ops.h"
 #include "gdn_step.h"
@@ -30,6 +33,8 @@ int launch(void (*fn)(P), dim3 grid, dim3 block, size_t lds, hipStream_t s, cons
 }
 
 bool dims_ok(int Dk, int Dv) { return (Dk == 64 || Dk == 128) && (Dv == 64 || Dv == 128); }
+
+size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 // ---------------------------------------------------------------------------
 // Recurrent step.
@@ -124,11 +129,144 @@ template <class E> int dispatch_norm(const gdn::NormParams<E> &p, bool grad, hip
     }
 }
 
-size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
+// ---------------------------------------------------------------------------
+// Gradient of the chunk forward.
+
+// Byte offsets of the workspace regions (the records of gdn_backward.h).
+struct BackWs {
+    size_t gates, Tf, Tt, Kt, Qt, N0, Gd, Hs, Gs, eT, vT, total;
+};
+
+BackWs back_layout(int B, int H, int T, int Dk, int Dv, size_t esz) {
+    using gdn::kChunk;
+    const size_t n = (size_t)B * H * (((size_t)T + kChunk - 1) / kChunk);
+    BackWs L;
+    size_t off = 0;
+    auto region = [&](size_t bytes) {
+        const size_t at = off;
+        off = align256(off + n * bytes);
+        return at;
+    };
+    L.gates = region(4 * gdn::kBackGateRec);
+    L.Tf = region(4 * kChunk * kChunk);
+    L.Tt = region(4 * kChunk * kChunk);
+    L.Kt = region(esz * Dk * kChunk);
+    L.Qt = region(esz * Dk * kChunk);
+    L.N0 = region(4 * kChunk * Dv);
+    L.Gd = region(4 * kChunk * Dv);
+    L.Hs = region(4 * (size_t)Dk * Dv);
+    L.Gs = region(4 * (size_t)Dk * Dv);
+    L.eT = region(4 * kChunk * Dv);
+    L.vT = region(4 * kChunk * Dv);
+    L.total = off;
+    return L;
+}
+
+bool back_shape_ok(int B, int H, int T) {
+    // the launches' grids: chunks x heads below 2^31
+    return B >= 1 && H >= 1 && T >= 1 && (long long)B * H <= 65535 &&
+           (long long)B * H * ((T + (long long)gdn::kChunk - 1) / gdn::kChunk) < (1LL << 31);
+}
+
+template <class E, int DK, int DV> int launch_backward(const gdn::BackParams<E> &p, hipStream_t s) {
+    using P = gdn::PrepLds<E, DK, DV>;
+    using G = gdn::GradLds<E, DK, DV>;
+    static std::once_flag once;
+    static hipError_t attr = hipSuccess;
+    std::call_once(once, [] {
+        attr = hipFuncSetAttribute((const void *)gdn::gdn_back_prep_kernel<E, DK, DV>,
+                                   hipFuncAttributeMaxDynamicSharedMemorySize, (int)P::bytes);
+        if (attr == hipSuccess)
+            attr = hipFuncSetAttribute((const void *)gdn::gdn_back_grad_kernel<E, DK, DV>,
+                                       hipFuncAttributeMaxDynamicSharedMemorySize, (int)G::bytes);
+    });
+    if (attr != hipSuccess) return GDN_ERR_HIP;
+    const unsigned bh = (unsigned)(p.B * p.H), n = bh * (unsigned)p.NC;
+    int st = launch(gdn::gdn_back_prep_kernel<E, DK, DV>, dim3(n), dim3(64 * gdn::kPrepWaves), P::bytes, s, p);
+    if (st == GDN_OK)
+        st = launch(gdn::gdn_back_scan_kernel<E, DK, DV>, dim3((bh + 7) / 8 * 8 * (DV / 16), 2),
+                    dim3(64 * gdn::kBackScanWaves), 0, s, p);
+    if (st == GDN_OK)
+        st = launch(gdn::gdn_back_grad_kernel<E, DK, DV>, dim3(n), dim3(64 * G::NW), G::bytes, s, p);
+    return st;
+}
+
+template <class E> int dispatch_backward(const gdn::BackParams<E> &p, int Dk, int Dv, hipStream_t s) {
+    if (Dk == 128) return Dv == 128 ? launch_backward<E, 128, 128>(p, s) : launch_backward<E, 128, 64>(p, s);
+    return Dv == 128 ? launch_backward<E, 64, 128>(p, s) : launch_backward<E, 64, 64>(p, s);
+}
 
 }  // namespace
 
 extern "C" {
+
+size_t gdn_chunk_backward_workspace_bytes(int B, int H, int T, int Dk, int Dv, int chunk, int is_bf16) {
+    if (!back_shape_ok(B, H, T) || !dims_ok(Dk, Dv) || chunk != gdn::kChunk) return 0;
+    return back_layout(B, H, T, Dk, Dv, is_bf16 ? 2 : 4).total;
+}
+
+int gdn_chunk_backward(const void *q, const void *k, const void *v, const float *alpha, const float *beta,
+                       const float *state_in, const void *dout, const float *dstate_out, void *dq,
+                       void *dk, void *dv, float *dalpha, float *dbeta, float *dstate_in, int B, int H,
+                       int T, int Dk, int Dv, int chunk, int is_bf16, void *ws, size_t ws_bytes,
+                       void *stream) {
+    if (!q || !k || !v || !alpha || !beta || !dout || !dq || !dk || !dv || !dalpha || !dbeta) return GDN_ERR_NULL;
+    if (!back_shape_ok(B, H, T)) return GDN_ERR_SHAPE;
+    if (!dims_ok(Dk, Dv) || chunk != gdn::kChunk) return GDN_ERR_UNSUPPORTED;
+    for (const void *p : {q, k, v, (const void *)alpha, (const void *)beta, (const void *)state_in, dout,
+                          (const void *)dstate_out, (const void *)dq, (const void *)dk, (const void *)dv,
+                          (const void *)dalpha, (const void *)dbeta, (const void *)dstate_in})
+        if (misaligned(p)) return GDN_ERR_ALIGN;
+    const size_t esz = is_bf16 ? 2 : 4, n = (size_t)B * T * H, sb = (size_t)B * H * Dk * Dv * 4;
+    const BackWs L = back_layout(B, H, T, Dk, Dv, esz);
+    if (!ws || misaligned(ws, 256) || ws_bytes < L.total) return GDN_ERR_WORKSPACE;
+    const Range in[] = {Range(q, n * Dk * esz), Range(k, n * Dk * esz), Range(v, n * Dv * esz), Range(alpha, n * 4),
+                        Range(beta, n * 4), Range(state_in, sb), Range(dout, n * Dv * esz), Range(dstate_out, sb)};
+    const Range outs[] = {Range(dq, n * Dk * esz), Range(dk, n * Dk * esz), Range(dv, n * Dv * esz), Range(dalpha, n * 4),
+                          Range(dbeta, n * 4), Range(dstate_in, sb), Range(ws, L.total)};
+    for (int i = 0; i < 7; ++i) {
+        for (int j = 0; j < 8; ++j)
+            if (outs[i].overlaps(in[j]) && !(i == 5 && j == 7 && outs[i].same(in[j]))) return GDN_ERR_ALIAS;
+        for (int j = 0; j < i; ++j)
+            if (outs[i].overlaps(outs[j])) return GDN_ERR_ALIAS;
+    }
+    auto run = [&](auto *e) {
+        using E = std::remove_pointer_t<decltype(e)>;
+        unsigned char *base = (unsigned char *)ws;
+        gdn::BackParams<E> p;
+        p.q = (const E *)q;
+        p.k = (const E *)k;
+        p.v = (const E *)v;
+        p.dout = (const E *)dout;
+        p.alpha = alpha;
+        p.beta = beta;
+        p.state_in = state_in;
+        p.dstate_out = dstate_out;
+        p.dq = (E *)dq;
+        p.dk = (E *)dk;
+        p.dv = (E *)dv;
+        p.dalpha = dalpha;
+        p.dbeta = dbeta;
+        p.dstate_in = dstate_in;
+        p.B = B;
+        p.H = H;
+        p.T = T;
+        p.NC = (int)((T + (long long)gdn::kChunk - 1) / gdn::kChunk);
+        p.gates = (float *)(base + L.gates);
+        p.N0 = (float *)(base + L.N0);
+        p.Tf = (E *)(base + L.Tf);
+        p.Tt = (E *)(base + L.Tt);
+        p.Kt = (E *)(base + L.Kt);
+        p.Qt = (E *)(base + L.Qt);
+        p.Gd = (E *)(base + L.Gd);
+        p.Hs = (E *)(base + L.Hs);
+        p.Gs = (E *)(base + L.Gs);
+        p.eT = (E *)(base + L.eT);
+        p.vT = (E *)(base + L.vT);
+        return dispatch_backward<E>(p, Dk, Dv, (hipStream_t)stream);
+    };
+    return is_bf16 ? run((uint16_t *)nullptr) : run((float *)nullptr);
+}
 
 int gdn_step_forward(const void *q, const void *k, const void *v, const float *alpha, const float *beta,
                      const float *state_in, const int *slots, const int *lengths, void *out,

@@ -1,6 +1,6 @@
 """The operators around the gated delta-rule forward (include/gdn_ops.h): the
-recurrent step of a decoding batch, and the norms, gate and scaled residual
-between two blocks with their gradient.
+recurrent step of a decoding batch, the gradient of the token-wise chunk forward,
+and the norms, gate and scaled residual between two blocks with their gradient.
 
 Thin binding like :mod:`.gdn`: argument checks and marshalling only.  Outputs and
 workspaces that are not given are allocated on the stream the call runs on.
@@ -22,6 +22,10 @@ def _lib():
         vp, i, sz, fl = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t, ctypes.c_float
         L.gdn_step_forward.restype = i
         L.gdn_step_forward.argtypes = [vp] * 10 + [i] * 8 + [vp]
+        L.gdn_chunk_backward_workspace_bytes.restype = sz
+        L.gdn_chunk_backward_workspace_bytes.argtypes = [i] * 7
+        L.gdn_chunk_backward.restype = i
+        L.gdn_chunk_backward.argtypes = [vp] * 14 + [i] * 7 + [vp, sz, vp]
         L.gdn_block_norm_forward.restype = i
         L.gdn_block_norm_forward.argtypes = [vp] * 7 + [i] * 3 + [fl] * 2 + [i, vp]
         L.gdn_block_norm_workspace_bytes.restype = sz
@@ -122,6 +126,55 @@ def step(q, k, v, alpha, beta, state, *, slots=None, lengths=None, out=None, sta
           state.data_ptr(), _ptr(slots), _ptr(lengths), out.data_ptr(), state_out.data_ptr(), N, L, P, Hk, H, Dk, Dv,
           1 if dt == torch.bfloat16 else 0)
     return out, state_out
+
+
+def backward_workspace(q, v, chunk=_gdn.CHUNK):
+    """Workspace tensor for backward on inputs shaped like q [B, T, H, Dk] and v [.., Dv]."""
+    B, T, H, Dk = q.shape
+    n = _lib().gdn_chunk_backward_workspace_bytes(B, H, T, Dk, v.shape[-1], chunk, 1 if q.dtype == torch.bfloat16 else 0)
+    if n == 0:
+        raise ValueError("unsupported shape for the GDN chunk backward")
+    return torch.empty(n, dtype=torch.uint8, device=q.device)
+
+
+def backward(q, k, v, alpha, beta, state_in, dout, dstate_out=None, *, dq=None, dk=None, dv=None, dalpha=None,
+             dbeta=None, dstate_in=None, want_dstate=True, ws=None, chunk=_gdn.CHUNK, stream=None):
+    """Gradient of ``forward``: from dout = dL/d(out) [B, T, H, Dv] like v and dstate_out =
+    dL/d(state_out) [B, H, Dk, Dv] fp32 (None: zero), with the forward call's inputs
+    (state_in may be None there and here).  Needs nothing else of that call.
+    dstate_in may be dstate_out.  Returns (dq, dk, dv like q, dalpha, dbeta [B, T, H] fp32,
+    dstate_in [B, H, Dk, Dv] fp32, or None without want_dstate)."""
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return backward(q, k, v, alpha, beta, state_in, dout, dstate_out, dq=dq, dk=dk, dv=dv, dalpha=dalpha,
+                            dbeta=dbeta, dstate_in=dstate_in, want_dstate=want_dstate, ws=ws, chunk=chunk)
+    dt, dev = _element("q", q)
+    B, T, H, Dk = _dims("q", q, 4, "[B, T, H, Dk]")
+    Dv = _dims("v", v, 4, "[B, T, H, Dv]")[3]
+    f32 = torch.float32
+    for name, t, last in (("q", q, Dk), ("k", k, Dk), ("v", v, Dv), ("dout", dout, Dv)):
+        _need(name, t, (B, T, H, last), dt, dev)
+    _need("alpha", alpha, (B, T, H), f32, dev)
+    _need("beta", beta, (B, T, H), f32, dev)
+    for name, t in (("state_in", state_in), ("dstate_out", dstate_out)):
+        if t is not None:
+            _need(name, t, (B, H, Dk, Dv), f32, dev)
+    dq = _given("dq", dq, (B, T, H, Dk), dt, dev)
+    dk = _given("dk", dk, (B, T, H, Dk), dt, dev)
+    dv = _given("dv", dv, (B, T, H, Dv), dt, dev)
+    dalpha = _given("dalpha", dalpha, (B, T, H), f32, dev)
+    dbeta = _given("dbeta", dbeta, (B, T, H), f32, dev)
+    if want_dstate or dstate_in is not None:
+        dstate_in = _given("dstate_in", dstate_in, (B, H, Dk, Dv), f32, dev)
+    if ws is None:
+        ws = backward_workspace(q, v, chunk)
+    elif ws.device != dev or ws.dtype != torch.uint8 or not ws.is_contiguous():
+        raise ValueError(f"ws must be a contiguous uint8 tensor on {dev}")
+    _call("gdn_chunk_backward", dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), alpha.data_ptr(), beta.data_ptr(),
+          _ptr(state_in), dout.data_ptr(), _ptr(dstate_out), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+          dalpha.data_ptr(), dbeta.data_ptr(), _ptr(dstate_in), B, H, T, Dk, Dv, int(chunk),
+          1 if dt == torch.bfloat16 else 0, ws.data_ptr(), ws.numel())
+    return dq, dk, dv, dalpha, dbeta, dstate_in
 
 
 def block_norm_workspace(rows, channels, gate_tokens, device):

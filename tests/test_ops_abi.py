@@ -106,3 +106,34 @@ def test_host_tensors_are_refused():
         gdn.block_norm_backward(z(1, 2, 8), z(1, 2, 8), None, z(8), z(8), z(1, 2, 8))
     with pytest.raises(TypeError, match="tensor"):
         gdn.block_norm([1.0], z(1, 2, 8), None, z(8), z(8))
+
+
+BACK = dict(q=addr(0), k=addr(1), v=addr(2), alpha=addr(3), beta=addr(4), state_in=addr(5), dout=addr(6),
+            dstate_out=addr(7), dq=addr(8), dk=addr(9), dv=addr(10), dalpha=addr(11), dbeta=addr(12), dstate_in=addr(13),
+            B=1, H=2, T=100, Dk=64, Dv=128, chunk=64, bf16=1, ws=addr(14), ws_bytes=32 * MB)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(q=None), NULL), (dict(k=None), NULL), (dict(v=None), NULL), (dict(alpha=None), NULL), (dict(beta=None), NULL),
+    (dict(dout=None), NULL), (dict(dq=None), NULL), (dict(dk=None), NULL), (dict(dv=None), NULL),
+    (dict(dalpha=None), NULL), (dict(dbeta=None), NULL), (dict(B=0), SHAPE), (dict(H=0), SHAPE), (dict(T=0), SHAPE),
+    (dict(B=300, H=300), SHAPE), (dict(B=1, H=65535, T=1 << 30), SHAPE), (dict(Dk=96), UNSUPPORTED),
+    (dict(Dv=256), UNSUPPORTED), (dict(chunk=32), UNSUPPORTED), (dict(dout=addr(6) + 8), ALIGN),
+    (dict(dstate_in=addr(13) + 4), ALIGN), (dict(ws=None), WORKSPACE), (dict(ws=addr(14) + 16), WORKSPACE),
+    (dict(ws_bytes=4096), WORKSPACE), (dict(dq=addr(0)), ALIAS), (dict(dv=addr(6)), ALIAS), (dict(dk=addr(8)), ALIAS),
+    (dict(dalpha=addr(3)), ALIAS), (dict(dstate_in=addr(7) + 16), ALIAS), (dict(dstate_in=addr(5)), ALIAS),
+    (dict(ws=addr(2)), ALIAS), (dict(ws=addr(10)), ALIAS)])
+def test_backward_refusals(kw, want):
+    assert ops._lib().gdn_chunk_backward(*dict(BACK, **kw).values(), None) == want
+
+
+def test_backward_workspace():
+    f = ops._lib().gdn_chunk_backward_workspace_bytes
+    assert f(1, 2, 100, 96, 64, 64, 1) == 0 and f(1, 2, 0, 64, 64, 64, 1) == 0 and f(1, 2, 100, 64, 64, 32, 1) == 0
+    n = 16 * 55
+    per = 4 * (336 + 2 * 64 * 64 + 2 * 64 * 128 + 2 * 128 * 128 + 2 * 64 * 128)
+    for bf16, e in ((1, 2), (0, 4)):
+        want = n * (per + 2 * e * 128 * 64)
+        assert want <= f(1, 16, 3520, 128, 128, 64, bf16) < want + 11 * 256
+    with pytest.raises(ValueError, match="unsupported"):
+        gdn.backward_workspace(torch.zeros(1, 3, 2, 32), torch.zeros(1, 3, 2, 64))
