@@ -63,14 +63,13 @@ int gdn_step_forward(const void *q, const void *k, const void *v, const float *a
  * needed but its inputs: states and pseudo-values are formed again.  All
  * gradients are those of the recurrence itself: alpha and beta of 0 have theirs
  * too (alpha below 1.2e-38 acts as that value, as in the forward).  Sums, states
- * and their gradients are fp32; on the bf16 path the operands of products that are
- * not inputs keep 16 bits of mantissa (a pair of bf16), so that the fp32 results
- * are good to about 1e-5 of their size.  Results are deterministic.
+ * and their gradients are fp32, and on the bf16 path too the operands of products
+ * that lead to fp32 results keep fp32's mantissa.  Results are deterministic.
  *
  * Outputs may not overlap inputs or each other, except dstate_in == dstate_out.
  * `ws`: caller-owned device buffer, 256-byte aligned, of at least
  * gdn_chunk_backward_workspace_bytes(...) bytes (0 for arguments that the call
- * refuses; 321 KB a chunk and head at Dk = Dv = 128).  Calls that run at once need
+ * refuses; 305 KB a chunk and head at Dk = Dv = 128).  Calls that run at once need
  * one each.
  */
 size_t gdn_chunk_backward_workspace_bytes(int B, int H, int T, int Dk, int Dv, int chunk, int is_bf16);

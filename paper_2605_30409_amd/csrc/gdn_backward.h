@@ -28,106 +28,138 @@
 // backward side by side (gdn_back_scan_kernel); per chunk all that remains
 // (gdn_back_grad_kernel).
 //
-// Precision: gate gradients and states are fp32 results, and so every operand
-// that is not itself an input keeps 16 bits of mantissa or more.  On the bf16
-// path such a "wide" operand is a pair of bf16 planes, x = hi + lo with hi = bf16(x)
-// and lo = bf16(x - hi) (off by at most 2^-18 |x|); a product with an input takes two bf16
-// MFMAs and one of two wide operands three (the fourth, lo lo, is below what lo
-// was rounded by).  On the fp32 path it is fp32 and all products are fp32 MFMAs.
+// Precision: gate gradients and states are fp32 results, so what leads to them
+// keeps fp32's mantissa.  On the bf16 path an operand that is not itself an input
+// is cut into three bf16 planes, x = hi + mid + lo exactly (8 bits of mantissa
+// each, denormals aside); a product with an input takes three bf16 MFMAs and one of two
+// such operands six (the terms left out are below 2^-25).  That is 48 and 96 cycles where
+// fp32 MFMAs take 256.  Two planes, tried first, left 2e-6 to 4e-6 of error in
+// the fp32 results; fp32 evaluation has 2e-7 to 3e-7.  Only the last products of dQ and dK,
+// whose results are rounded to bf16, take G1 and G2 in two planes (2^-17).  On the fp32 path
+// operands are fp32 and all products fp32 MFMAs.
 #pragma once
 
 #include "gdn_device.h"
 
 namespace gdn {
 
-// A wide operand fragment: 8 consecutive k per lane, like Tr<E>::frag.
-template <class E> struct Wide;
-template <> struct Wide<uint16_t> {
+// An operand fragment in P planes (8 consecutive k per lane, like Tr<E>::frag).
+template <class E, int P> struct Wide;
+template <int P> struct Wide<uint16_t, P> {
     using T = Tr<uint16_t>;
+    static constexpr int planes = P;
     struct frag {
-        u32x4 hi, lo;
+        u32x4 pl[P];
     };
-    static constexpr int planes = 2;
-    static __device__ __forceinline__ f32x4 hi_of(u32x2 h) { return T::to_f32(h); }
-    static __device__ __forceinline__ void store4(uint16_t *p, size_t plane, f32x4 x) {
-        const u32x2 h = T::from_f32(x);
-        T::store(p, h);
-        T::store(p + plane, T::from_f32(x - T::to_f32(h)));
+    static __device__ __forceinline__ void store4(uint16_t *p, int plane, f32x4 x) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            const u32x2 h = T::from_f32(x);
+            T::store(p + i * plane, h);
+            x -= T::to_f32(h);
+        }
     }
-    static __device__ __forceinline__ void store1(uint16_t *p, size_t plane, float x) {
-        const uint32_t h = pack_bf16x2(x, 0.f);
-        p[0] = (uint16_t)h;
-        p[plane] = (uint16_t)pack_bf16x2(x - __uint_as_float(h << 16), 0.f);
+    static __device__ __forceinline__ void store1(uint16_t *p, int plane, float x) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            const uint32_t h = pack_bf16x2(x, 0.f);
+            p[i * plane] = (uint16_t)h;
+            x -= __uint_as_float(h << 16);
+        }
     }
     static __device__ __forceinline__ frag split(f32x4 a, f32x4 b) {
-        const u32x2 ha = T::from_f32(a), hb = T::from_f32(b);
-        return frag{T::cat(ha, hb), T::cat(T::from_f32(a - T::to_f32(ha)), T::from_f32(b - T::to_f32(hb)))};
+        frag f;
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
+            const u32x2 ha = T::from_f32(a), hb = T::from_f32(b);
+            f.pl[i] = T::cat(ha, hb);
+            a -= T::to_f32(ha);
+            b -= T::to_f32(hb);
+        }
+        return f;
     }
-    static __device__ __forceinline__ frag load8(const uint16_t *p, size_t plane) {
-        return frag{T::load8(p), T::load8(p + plane)};
+    template <class I> static __device__ __forceinline__ frag load8(const uint16_t *p, I plane) {
+        frag f;
+#pragma unroll
+        for (int i = 0; i < P; ++i) f.pl[i] = T::load8(p + i * plane);
+        return f;
     }
-    static __device__ __forceinline__ void store8(uint16_t *p, size_t plane, frag f) {
-        T::store8(p, f.hi);
-        T::store8(p + plane, f.lo);
+    template <class I> static __device__ __forceinline__ void store8(uint16_t *p, I plane, frag f) {
+#pragma unroll
+        for (int i = 0; i < P; ++i) T::store8(p + i * plane, f.pl[i]);
     }
-    static __device__ __forceinline__ frag tr(const uint16_t *M, size_t plane, int ld, int row0, int col, int li, int lg) {
-        return frag{tr_frag<uint16_t>(M, ld, row0, col, false, 0, li, lg),
-                    tr_frag<uint16_t>(M + plane, ld, row0, col, false, 0, li, lg)};
+    static __device__ __forceinline__ frag tr(const uint16_t *M, int plane, int ld, int row0, int col, int li, int lg) {
+        frag f;
+#pragma unroll
+        for (int i = 0; i < P; ++i) f.pl[i] = tr_frag<uint16_t>(M + i * plane, ld, row0, col, false, 0, li, lg);
+        return f;
     }
-    static __device__ __forceinline__ void values(frag f, f32x4 &a, f32x4 &b) {
-        a = T::to_f32(T::lo(f.hi)) + T::to_f32(T::lo(f.lo));
-        b = T::to_f32(T::hi(f.hi)) + T::to_f32(T::hi(f.lo));
+    // products, the smallest terms first: e an input's fragment, w one in planes
+    static __device__ __forceinline__ f32x4 ew(u32x4 a, const frag &b, f32x4 c) {
+#pragma unroll
+        for (int i = P - 1; i >= 0; --i) c = T::mma(a, b.pl[i], c);
+        return c;
     }
-    static __device__ __forceinline__ f32x4 ew(u32x4 a, frag b, f32x4 c) { return T::mma(a, b.hi, T::mma(a, b.lo, c)); }
-    static __device__ __forceinline__ f32x4 we(frag a, u32x4 b, f32x4 c) { return T::mma(a.hi, b, T::mma(a.lo, b, c)); }
-    static __device__ __forceinline__ f32x4 ww(frag a, frag b, f32x4 c) {
-        return T::mma(a.hi, b.hi, T::mma(a.hi, b.lo, T::mma(a.lo, b.hi, c)));
+    static __device__ __forceinline__ f32x4 we(const frag &a, u32x4 b, f32x4 c) {
+#pragma unroll
+        for (int i = P - 1; i >= 0; --i) c = T::mma(a.pl[i], b, c);
+        return c;
     }
-    // the value rounded to the storage type, as an output fragment
-    static __device__ __forceinline__ u32x4 rounded(frag f) { return f.hi; }
+    static __device__ __forceinline__ f32x4 ww(const frag &a, const frag &b, f32x4 c) {
+#pragma unroll
+        for (int s = P - 1; s >= 0; --s)
+#pragma unroll
+            for (int i = 0; i <= s; ++i) c = T::mma(a.pl[i], b.pl[s - i], c);
+        return c;
+    }
+    // the value rounded to the storage type
+    static __device__ __forceinline__ u32x4 rounded(const frag &f) { return f.pl[0]; }
 };
-template <> struct Wide<float> {
+template <int P> struct Wide<float, P> {
     using T = Tr<float>;
     using frag = f32x8;
     static constexpr int planes = 1;
-    static __device__ __forceinline__ void store4(float *p, size_t, f32x4 x) { T::store(p, x); }
-    static __device__ __forceinline__ void store1(float *p, size_t, float x) { *p = x; }
+    static __device__ __forceinline__ void store4(float *p, int, f32x4 x) { T::store(p, x); }
+    static __device__ __forceinline__ void store1(float *p, int, float x) { *p = x; }
     static __device__ __forceinline__ frag split(f32x4 a, f32x4 b) { return T::cat(a, b); }
-    static __device__ __forceinline__ frag load8(const float *p, size_t) { return T::load8(p); }
-    static __device__ __forceinline__ void store8(float *p, size_t, frag f) { T::store8(p, f); }
-    static __device__ __forceinline__ frag tr(const float *M, size_t, int ld, int row0, int col, int li, int lg) {
+    template <class I> static __device__ __forceinline__ frag load8(const float *p, I) { return T::load8(p); }
+    template <class I> static __device__ __forceinline__ void store8(float *p, I, frag f) { T::store8(p, f); }
+    static __device__ __forceinline__ frag tr(const float *M, int, int ld, int row0, int col, int li, int lg) {
         return tr_frag<float>(M, ld, row0, col, false, 0, li, lg);
     }
-    static __device__ __forceinline__ void values(frag f, f32x4 &a, f32x4 &b) { a = T::lo(f), b = T::hi(f); }
     static __device__ __forceinline__ f32x4 ew(frag a, frag b, f32x4 c) { return T::mma(a, b, c); }
     static __device__ __forceinline__ f32x4 we(frag a, frag b, f32x4 c) { return T::mma(a, b, c); }
     static __device__ __forceinline__ f32x4 ww(frag a, frag b, f32x4 c) { return T::mma(a, b, c); }
     static __device__ __forceinline__ frag rounded(frag f) { return f; }
 };
+template <class E> using Full = Wide<E, 3>;    // fp32's mantissa
+template <class E> using Half = Wide<E, 2>;    // 16 bits of it
+
+__device__ __forceinline__ float elem_f32(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
+__device__ __forceinline__ float elem_f32(float x) { return x; }
 
 // Gate record of a chunk, in floats: g as 64 doubles, gam, tail and beta, e^{g_C}.
 constexpr int kBackGam = 128, kBackTail = 192, kBackBeta = 256, kBackGC = 320, kBackGateRec = 336;
 
-// Workspace records per (b*H + h, chunk).  "Wide" regions take 4 bytes an element on
-// either path (two planes of bf16, the second n elements behind the first, or fp32).
+// Workspace records per (b*H + h, chunk); "planes": three of bf16, each behind the
+// whole of the one before, on the bf16 path, fp32 on the other.
 //   gates [336] fp32
-//   Tf, Tt  64 x 64   wide, fragments: [4 row tile][2 k block][64 lane][8] of T and T^T
+//   Tf, Tt  64 x 64   planes, fragments [4 row tile][2 k block][64 lane][8] of T and T^T
 //   Kt, Qt  Dk x 64   E, fragments [Dk/16][2][64][8] of K^T and Q^T
 //   N0      64 x Dv   fp32, beta A^T dO as accumulator tiles [Dv/16][4][64 lane][4]
-//   Gd      64 x Dv   wide, gam dO as fragments [Dv/16][2][64][8] (k = token)
-//   Hs, Gs  Dk x Dv   wide, row-major: H and G of the chunk
-//   eT, vT  Dv x 64   wide, row-major: e^T and dV^T
+//   Hs, Gs  Dk x Dv   fp32, row-major: H and G of the chunk
+//   eT, vT  Dv x 64   fp32, row-major: e^T and dV^T
 template <class E> struct BackParams {
     const E *q, *k, *v, *dout;
     const float *alpha, *beta, *state_in, *dstate_out;
     E *dq, *dk, *dv;
     float *dalpha, *dbeta, *dstate_in;
     int B, H, T, NC;
-    float *gates, *N0;
-    E *Tf, *Tt, *Kt, *Qt, *Gd, *Hs, *Gs, *eT, *vT;
+    float *gates, *N0, *Hs, *Gs, *eT, *vT;
+    E *Tf, *Tt, *Kt, *Qt;
 };
 
-template <class E> constexpr int wide_elems(int n) { return n * Wide<E>::planes; }
+template <class E> constexpr int full_elems(int n) { return n * Full<E>::planes; }
 
 // Padded leading dimension of an LDS tile with rows of n elements of E.
 template <class E> constexpr int lds_ld(int n) { return n + 16 / (int)sizeof(E); }
@@ -143,8 +175,8 @@ template <class E, int DK, int DV> struct PrepLds {
     static constexpr size_t oN = oO + sizeof(E) * kChunk * LDV;    // N, fp32
     static constexpr size_t oT = oN + 4 * kChunk * LDA;            // T, fp32
     static constexpr size_t oA = oT + 4 * kChunk * LDA;            // A^T, wide
-    static constexpr size_t oG = oA + sizeof(E) * Wide<E>::planes * kChunk * LDT;
-    static constexpr size_t bytes = oG + 8 * kChunk + 2 * 4 * kChunk;
+    static constexpr size_t oG = oA + sizeof(E) * Full<E>::planes * kChunk * LDT;
+    static constexpr size_t bytes = oG + 8 * kChunk + 4 * kChunk;
 };
 
 constexpr int kPrepWaves = 8;
@@ -172,14 +204,14 @@ template <class E, int DK, int DV>
 __global__ __launch_bounds__(64 * kPrepWaves) void gdn_back_prep_kernel(BackParams<E> p) {
     using L = PrepLds<E, DK, DV>;
     using TR = Tr<E>;
-    using WD = Wide<E>;
+    using WD = Full<E>;
     constexpr int NT = 64 * kPrepWaves;
-    constexpr size_t PA = (size_t)kChunk * L::LDT;      // plane of A^T
+    constexpr int PA = kChunk * L::LDT;      // plane of A^T
     extern __shared__ __align__(16) unsigned char smem[];
     E *sK = (E *)(smem + L::oK), *sQ = (E *)(smem + L::oQ), *sO = (E *)(smem + L::oO), *sA = (E *)(smem + L::oA);
     float *sN = (float *)(smem + L::oN), *sT = (float *)(smem + L::oT);
     double *sg = (double *)(smem + L::oG);
-    float *sb = (float *)(sg + kChunk), *sgam = sb + kChunk;
+    float *sb = (float *)(sg + kChunk);
     const int c = blockIdx.x / (p.B * p.H), bh = blockIdx.x - c * (p.B * p.H);
     const int b = bh / p.H, h = bh - b * p.H;
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, li = l & 15, lg = l >> 4;
@@ -203,12 +235,10 @@ __global__ __launch_bounds__(64 * kPrepWaves) void gdn_back_prep_kernel(BackPara
             if (l >= d) g += o;
         }
         const double gC = __shfl(g, kChunk - 1);
-        const float gam = expf((float)g);
         sg[l] = g;
         sb[l] = be;
-        sgam[l] = gam;
         ((double *)gate)[l] = g;
-        gate[kBackGam + l] = gam;
+        gate[kBackGam + l] = expf((float)g);
         gate[kBackTail + l] = expf((float)(gC - g));
         gate[kBackBeta + l] = be;
         if (l == 0) gate[kBackGC] = expf((float)gC);
@@ -263,14 +293,6 @@ __global__ __launch_bounds__(64 * kPrepWaves) void gdn_back_prep_kernel(BackPara
             TR::store8((which ? Qt : Kt) + (size_t)(t * 2 + kb) * 512 + l * 8,
                        tr_frag<E>(which ? sQ : sK, L::LDK, 32 * kb, 16 * t, false, 0, li, lg));
         }
-        E *Gd = p.Gd + cidx * (size_t)wide_elems<E>(kChunk * DV);
-        for (int f = w - 1; f < (DV / 16) * 2; f += kPrepWaves - 1) {
-            const int kb = f & 1, jt = f >> 1;
-            const typename TR::frag o = tr_frag<E>(sO, L::LDV, 32 * kb, 16 * jt, false, 0, li, lg);
-            const float *gm = sgam + 32 * kb + 8 * lg;
-            WD::store8(Gd + (size_t)(jt * 2 + kb) * 512 + l * 8, (size_t)kChunk * DV,
-                       WD::split(TR::to_f32(TR::lo(o)) * *(const f32x4 *)gm, TR::to_f32(TR::hi(o)) * *(const f32x4 *)(gm + 4)));
-        }
         float *N0 = p.N0 + cidx * (size_t)kChunk * DV;
         for (int f = w - 1; f < (DV / 16) * 4; f += kPrepWaves - 1) {
             const int rt = f & 3, jt = f >> 2;
@@ -313,8 +335,8 @@ __global__ __launch_bounds__(64 * kPrepWaves) void gdn_back_prep_kernel(BackPara
             const int k = 32 * kb + 8 * lg + e, r = 16 * rt + li;
             x[e >> 2][e & 3] = f < 8 ? sT[r * L::LDA + k] : sT[k * L::LDA + r];
         }
-        E *dst = (f < 8 ? p.Tf : p.Tt) + cidx * (size_t)wide_elems<E>(kChunk * kChunk);
-        WD::store8(dst + (size_t)(rt * 2 + kb) * 512 + l * 8, (size_t)kChunk * kChunk, WD::split(x[0], x[1]));
+        E *dst = (f < 8 ? p.Tf : p.Tt) + cidx * (size_t)full_elems<E>(kChunk * kChunk);
+        WD::store8(dst + (rt * 2 + kb) * 512 + l * 8, kChunk * kChunk, WD::split(x[0], x[1]));
     }
 }
 
@@ -323,24 +345,31 @@ __global__ __launch_bounds__(64 * kPrepWaves) void gdn_back_prep_kernel(BackPara
 // state through the chunks: blockIdx.y = 0 the states forward, 1 their gradients
 // backward.  Each product's rows are split over the waves, and its result goes
 // to all of them through LDS (as [column][row], so a result tile is stored in
-// quads and read back as operand rows).
+// quads and read back as operand rows).  A chunk's operands are loaded one chunk
+// ahead, as they are: nothing is computed from a load, and none is under a
+// condition, where it is issued, so that none is waited for there.  Rows past the
+// end of the sequence are read as its last row: their beta is 0, and so is
+// their part in the states and in dV.
 // --------------------------------------------------------------------------
 constexpr int kBackScanWaves = 4;
 
 template <class E, int DK> struct BackScanLds {
     static constexpr int LDH = lds_ld<E>(DK), LDC = lds_ld<E>(kChunk);
-    static constexpr size_t PH = 16 * (size_t)LDH, PC = 16 * (size_t)LDC;     // planes
-    static constexpr size_t oX = sizeof(E) * Wide<E>::planes * PH;            // first exchange
-    static constexpr size_t oY = oX + sizeof(E) * Wide<E>::planes * PC;       // second
-    static constexpr size_t bytes = oY + sizeof(E) * Wide<E>::planes * PC;
+    static constexpr int PH = 16 * LDH, PC = 16 * LDC;                        // planes
+    static constexpr size_t szC = sizeof(E) * Full<E>::planes * PC;
+    static constexpr size_t oX = sizeof(E) * Full<E>::planes * PH;            // T's operand
+    static constexpr size_t oY = oX + szC;                                    // T's result, scaled
+    static constexpr size_t oD = oY + szC;                                    // gam dO (backward)
+    static constexpr size_t bytes = oD + szC;
 };
 
 // Operands of one chunk, loaded ahead of their use.
 template <class E, int DK, bool REV> struct BackOps {
     static constexpr int NT = DK / 64;                  // state row tiles per wave
     typename Tr<E>::frag K[DK / 32], Kt[NT][2], Qt[REV ? NT : 1][2];
-    typename Wide<E>::frag T[2], Gd[REV ? 2 : 1];
-    f32x4 first, scale, out;                            // V or N0; per-token factors
+    typename Full<E>::frag T[2];
+    E vd[4];                                            // V or dO of four tokens
+    f32x4 n0, gam, tail, beta;
     float gC;
 };
 
@@ -348,147 +377,126 @@ template <class E, int DK, int DV, bool REV>
 __device__ __forceinline__ void back_load(const BackParams<E> &p, BackOps<E, DK, REV> &o, int b, int h, int bh, int jt,
                                           int c, int w, int l) {
     using TR = Tr<E>;
-    using WD = Wide<E>;
     const int li = l & 15, lg = l >> 4;
     const size_t cidx = (size_t)bh * p.NC + c;
-    const int t0 = c * kChunk, nvalid = min(kChunk, p.T - t0);
+    const int t0 = c * kChunk, last = min(kChunk, p.T - t0) - 1;
     const size_t row0 = ((size_t)b * p.T + t0) * p.H + h;
-    const int r = 16 * w + li;
+    const E *krow = p.k + (row0 + (size_t)min(16 * w + li, last) * p.H) * DK;
 #pragma unroll
-    for (int kb = 0; kb < DK / 32; ++kb)
-        o.K[kb] = r < nvalid ? load_frag<E>(p.k + (row0 + (size_t)r * p.H) * DK + 32 * kb, lg)
-                             : TR::cat(TR::zero(), TR::zero());
-    const E *Tm = (REV ? p.Tt : p.Tf) + cidx * (size_t)wide_elems<E>(kChunk * kChunk);
+    for (int kb = 0; kb < DK / 32; ++kb) o.K[kb] = load_frag<E>(krow + 32 * kb, lg);
+    const E *Tm = (REV ? p.Tt : p.Tf) + cidx * (size_t)full_elems<E>(kChunk * kChunk);
 #pragma unroll
-    for (int kb = 0; kb < 2; ++kb) o.T[kb] = WD::load8(Tm + (size_t)(w * 2 + kb) * 512 + l * 8, (size_t)kChunk * kChunk);
+    for (int kb = 0; kb < 2; ++kb) o.T[kb] = Full<E>::load8(Tm + (w * 2 + kb) * 512 + l * 8, kChunk * kChunk);
     const E *Kt = p.Kt + cidx * (size_t)DK * kChunk, *Qt = p.Qt + cidx * (size_t)DK * kChunk;
 #pragma unroll
     for (int t = 0; t < DK / 64; ++t)
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-            const size_t at = (size_t)((w * (DK / 64) + t) * 2 + kb) * 512 + l * 8;
+            const int at = ((w * (DK / 64) + t) * 2 + kb) * 512 + l * 8;
             o.Kt[t][kb] = TR::load8(Kt + at);
             if (REV) o.Qt[t][kb] = TR::load8(Qt + at);
         }
-    const float *gate = p.gates + cidx * kBackGateRec + 16 * w + 4 * lg;
-    const f32x4 gam = *(const f32x4 *)(gate + kBackGam), tail = *(const f32x4 *)(gate + kBackTail),
-                be = *(const f32x4 *)(gate + kBackBeta);
-    o.gC = p.gates[cidx * kBackGateRec + kBackGC];
-    if constexpr (REV) {
-        const E *Gd = p.Gd + cidx * (size_t)wide_elems<E>(kChunk * DV);
+    const float *gate = p.gates + cidx * kBackGateRec;
+    o.gam = *(const f32x4 *)(gate + kBackGam + 16 * w + 4 * lg);
+    o.tail = *(const f32x4 *)(gate + kBackTail + 16 * w + 4 * lg);
+    o.beta = *(const f32x4 *)(gate + kBackBeta + 16 * w + 4 * lg);
+    o.gC = gate[kBackGC];
+    if (REV) o.n0 = *(const f32x4 *)(p.N0 + cidx * (size_t)kChunk * DV + (jt * 4 + w) * 256 + l * 4);
+    const E *x = (REV ? p.dout : p.v) + row0 * DV + 16 * jt + li;
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) o.Gd[kb] = WD::load8(Gd + (size_t)(jt * 2 + kb) * 512 + l * 8, (size_t)kChunk * DV);
-        o.first = *(const f32x4 *)(p.N0 + cidx * (size_t)kChunk * DV + (size_t)(jt * 4 + w) * 256 + l * 4);
-        o.scale = be * tail;
-        o.out = -gam;
-    } else {
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int t = 16 * w + 4 * lg + q;
-            float x = 0.f;
-            if (t < nvalid) {
-                const E e = p.v[(row0 + (size_t)t * p.H) * DV + 16 * jt + li];
-                if constexpr (sizeof(E) == 2) x = __uint_as_float((uint32_t)e << 16);
-                else x = e;
-            }
-            o.first[q] = x;
-        }
-        o.scale = -gam;
-        o.out = be * tail;
-    }
-}
-
-// A 16 x 16 tile of LDS matrix X [column][row] (row tile at row0) into memory as
-// [row][column] with row stride ld.
-template <class E>
-__device__ __forceinline__ void store_transposed(const E *X, size_t xplane, int xld, int row0, E *dst, size_t dplane,
-                                                 int ld, int li, int lg) {
-    if constexpr (sizeof(E) == 2) {
-        typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-#pragma unroll
-        for (int pl = 0; pl < 2; ++pl) {
-            // lane li of a 16-lane group receives column li of rows 4 lg .. 4 lg + 3 of X
-            const i16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-                (lds_i16x4 *)(X + pl * xplane + (4 * lg + (li >> 2)) * xld + row0 + 4 * (li & 3)));
-            *(u32x2 *)(dst + pl * dplane + (size_t)(row0 + li) * ld + 4 * lg) = __builtin_bit_cast(u32x2, v);
-        }
-    } else {
-        f32x4 v;
-#pragma unroll
-        for (int q = 0; q < 4; ++q) v[q] = X[(4 * lg + q) * xld + row0 + li];
-        *(f32x4 *)(dst + (size_t)(row0 + li) * ld + 4 * lg) = v;
-    }
+    for (int q = 0; q < 4; ++q) o.vd[q] = x[(size_t)min(16 * w + 4 * lg + q, last) * p.H * DV];
 }
 
 template <class E, int DK, int DV, bool REV>
 __device__ __forceinline__ void back_scan(const BackParams<E> &p, unsigned char *smem, int bh, int jt) {
     using L = BackScanLds<E, DK>;
-    using WD = Wide<E>;
+    using WD = Full<E>;
     constexpr int NT = DK / 64;
-    E *sH = (E *)smem, *sX = (E *)(smem + L::oX), *sY = (E *)(smem + L::oY);
+    E *sH = (E *)smem, *sX = (E *)(smem + L::oX), *sY = (E *)(smem + L::oY), *sD = (E *)(smem + L::oD);
     const int b = bh / p.H, h = bh - b * p.H;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, li = l & 15, lg = l >> 4;
     const float *init = REV ? p.dstate_out : p.state_in;
-    const size_t sbase = (size_t)bh * DK * DV + 16 * jt + li;
+    const size_t sbase = (size_t)bh * DK * DV;
+    const int scol = 16 * jt + li;                                // element (16 (w NT + t) + 4 lg + q, scol)
     f32x4 st[NT];
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
-            st[t][q] = init ? init[sbase + (size_t)(16 * (w * NT + t) + 4 * lg + q) * DV] : 0.f;
+        for (int q = 0; q < 4; ++q) st[t][q] = init ? init[sbase + (16 * (w * NT + t) + 4 * lg + q) * DV + scol] : 0.f;
 #pragma unroll
     for (int t = 0; t < NT; ++t) WD::store4(sH + li * L::LDH + 16 * (w * NT + t) + 4 * lg, L::PH, st[t]);
 
     auto step = [&](const BackOps<E, DK, REV> &o, int c) {
         const size_t cidx = (size_t)bh * p.NC + c;
+        const int ct = li * L::LDC + 16 * w + 4 * lg;             // this wave's tokens in an exchange
         lds_barrier();
-        // the state that enters this step, for stage 3
-        E *keep = (REV ? p.Gs : p.Hs) + cidx * (size_t)wide_elems<E>(DK * DV) + 16 * jt;
-#pragma unroll
-        for (int t = 0; t < NT; ++t)
-            store_transposed<E>(sH, L::PH, L::LDH, 16 * (w * NT + t), keep, (size_t)DK * DV, DV, li, lg);
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int kb = 0; kb < DK / 32; ++kb)
             x = WD::ew(o.K[kb], WD::load8(sH + li * L::LDH + 32 * kb + 8 * lg, L::PH), x);
-        WD::store4(sX + li * L::LDC + 16 * w + 4 * lg, L::PC, o.first + o.scale * x);
+        f32x4 vd;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) vd[q] = elem_f32(o.vd[q]);
+        if constexpr (REV) {
+            WD::store4(sX + ct, L::PC, o.n0 + o.beta * o.tail * x);
+            // gam dO: rows past the sequence have no part in G
+            f32x4 gd = o.gam * vd;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) gd[q] = c * kChunk + 16 * w + 4 * lg + q < p.T ? gd[q] : 0.f;
+            WD::store4(sD + ct, L::PC, gd);
+        } else {
+            WD::store4(sX + ct, L::PC, vd - o.gam * x);
+        }
+        // the state that entered this step, for stage 3
+        float *keep = (REV ? p.Gs : p.Hs) + cidx * (size_t)(DK * DV) + scol;
+#pragma unroll
+        for (int t = 0; t < NT; ++t)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) keep[(16 * (w * NT + t) + 4 * lg + q) * DV] = st[t][q];
         lds_barrier();
         f32x4 y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
-            if (REV ? kb >= w / 2 : kb <= w / 2)         // T is lower triangular
+            if (REV ? kb >= w / 2 : kb <= w / 2)                  // T is lower triangular
                 y = WD::ww(o.T[kb], WD::load8(sX + li * L::LDC + 32 * kb + 8 * lg, L::PC), y);
-        WD::store4(sY + li * L::LDC + 16 * w + 4 * lg, L::PC, o.out * y);
-        E *res = (REV ? p.vT : p.eT) + cidx * (size_t)wide_elems<E>(kChunk * DV);
-        WD::store4(res + (size_t)(16 * jt + li) * kChunk + 16 * w + 4 * lg, (size_t)kChunk * DV, y);
-        lds_barrier();
+        WD::store4(sY + ct, L::PC, REV ? -o.gam * y : o.beta * o.tail * y);
+        *(f32x4 *)((REV ? p.vT : p.eT) + cidx * (size_t)(kChunk * DV) + scol * kChunk + 16 * w + 4 * lg) = y;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            st[t] *= o.gC;
+        for (int t = 0; t < NT; ++t) st[t] *= o.gC;
+        if constexpr (REV) {
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
-                if constexpr (REV) st[t] = WD::ew(o.Qt[t][kb], o.Gd[kb], st[t]);
-                st[t] = WD::ew(o.Kt[t][kb], WD::load8(sY + li * L::LDC + 32 * kb + 8 * lg, L::PC), st[t]);
+                const typename WD::frag gd = WD::load8(sD + li * L::LDC + 32 * kb + 8 * lg, L::PC);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) st[t] = WD::ew(o.Qt[t][kb], gd, st[t]);
             }
-            WD::store4(sH + li * L::LDH + 16 * (w * NT + t) + 4 * lg, L::PH, st[t]);
         }
+        lds_barrier();
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const typename WD::frag u = WD::load8(sY + li * L::LDC + 32 * kb + 8 * lg, L::PC);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) st[t] = WD::ew(o.Kt[t][kb], u, st[t]);
+        }
+#pragma unroll
+        for (int t = 0; t < NT; ++t) WD::store4(sH + li * L::LDH + 16 * (w * NT + t) + 4 * lg, L::PH, st[t]);
     };
     auto chunk = [&](int i) { return REV ? p.NC - 1 - i : i; };
     BackOps<E, DK, REV> o0, o1;
     back_load<E, DK, DV, REV>(p, o0, b, h, bh, jt, chunk(0), w, l);
     for (int i = 0; i < p.NC; i += 2) {
-        if (i + 1 < p.NC) back_load<E, DK, DV, REV>(p, o1, b, h, bh, jt, chunk(i + 1), w, l);
+        // (the last loads are of the last chunk again, and unused)
+        back_load<E, DK, DV, REV>(p, o1, b, h, bh, jt, chunk(min(i + 1, p.NC - 1)), w, l);
         step(o0, chunk(i));
         if (i + 1 == p.NC) break;
-        if (i + 2 < p.NC) back_load<E, DK, DV, REV>(p, o0, b, h, bh, jt, chunk(i + 2), w, l);
+        back_load<E, DK, DV, REV>(p, o0, b, h, bh, jt, chunk(min(i + 2, p.NC - 1)), w, l);
         step(o1, chunk(i + 1));
     }
     if (REV && p.dstate_in) {
 #pragma unroll
         for (int t = 0; t < NT; ++t)
 #pragma unroll
-            for (int q = 0; q < 4; ++q)
-                p.dstate_in[sbase + (size_t)(16 * (w * NT + t) + 4 * lg + q) * DV] = st[t][q];
+            for (int q = 0; q < 4; ++q) p.dstate_in[sbase + (16 * (w * NT + t) + 4 * lg + q) * DV + scol] = st[t][q];
     }
 }
 
@@ -505,100 +513,154 @@ void gdn_back_scan_kernel(BackParams<E> p) {
 }
 
 // --------------------------------------------------------------------------
-// Stage 3, per chunk and head: dQ, dK, dV, dalpha and dbeta.  Wave w has the 16
-// key channels from 16 w on in the products over Dk; the 64 x 64 products are
-// dealt out as tiles.
+// Stage 3, per chunk and head: dQ, dK, dV, dalpha and dbeta.  Four waves, two
+// workgroups to a CU.  Wave w has the Dk / 4 key channels from (Dk / 4) w on in the
+// products over Dk; the 64 x 64 products are dealt out as lower tiles.  The value
+// channels go through LDS 64 at a time; once they are done, G1, G2 and X take their
+// place there.
 // --------------------------------------------------------------------------
-template <class E, int DK, int DV> struct GradLds {
-    static constexpr int LDC = lds_ld<E>(kChunk);
-    static constexpr size_t PV = (size_t)DV * LDC, PC = (size_t)kChunk * LDC;
-    static constexpr int NW = DK / 16;
-    static constexpr size_t szV = sizeof(E) * Wide<E>::planes * PV, szC = sizeof(E) * Wide<E>::planes * PC;
-    static constexpr size_t oE = 0;                     // e^T
-    static constexpr size_t oV = oE + szV;              // dV^T
-    static constexpr size_t oG1 = oV + szV;             // G1^T
-    static constexpr size_t oX = oG1 + szC;             // X^T, its row 0 the exit state's
-    static constexpr size_t oG2 = oX + szC;             // G2 + G2^T
-    static constexpr size_t oD = oG2 + szC;             // D_{t-1,j}
-    static constexpr size_t oGate = oD + szC;           // the gate record
+constexpr int kGradWaves = 4;
+
+template <class E> struct GradLds {
+    static constexpr int LDC = lds_ld<E>(kChunk), PC = kChunk * LDC;
+    static constexpr size_t szF = sizeof(E) * Full<E>::planes * PC, szH = sizeof(E) * Half<E>::planes * PC;
+    static constexpr size_t oE = 0;                     // e^T, 64 value channels
+    static constexpr size_t oV = oE + szF;              // dV^T
+    static constexpr size_t oO = oV + szF;              // dO, [token][value channel]
+    static constexpr size_t endA = oO + sizeof(E) * PC;
+    static constexpr size_t oX = 0;                     // X^T, its column 0 the exit state's
+    static constexpr size_t oG1 = oX + szF;             // G1^T
+    static constexpr size_t oG2 = oG1 + szH;            // G2 + G2^T
+    static constexpr size_t endB = oG2 + szH;
+    static constexpr size_t oGate = endA > endB ? endA : endB;
     static constexpr size_t oRed = oGate + 4 * kBackGateRec;
-    // floats behind oRed: [NW][64] X_i,-1, [NW][64] k.PE, [4][64] column sums of dbeta, [4][64] of
-    // dalpha, [64] X_i,-1 summed, [64] exit-state part of dalpha, [NW] parts of <G, H>
-    static constexpr size_t bytes = oRed + 4 * (2 * NW * 64 + 10 * 64 + 16);
+    // floats behind oRed: [4][64] X_i,-1, [4][64] k.PE, [4][64] column sums of dbeta, [64] X_i,-1
+    // summed, [4] parts of <G, H>
+    static constexpr size_t bytes = oRed + 4 * (12 * 64 + 64 + 4);
 };
 
 template <class E, int DK, int DV>
-__global__ __launch_bounds__(64 * (DK / 16)) void gdn_back_grad_kernel(BackParams<E> p) {
-    using L = GradLds<E, DK, DV>;
+__global__ __launch_bounds__(64 * kGradWaves) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void gdn_back_grad_kernel(BackParams<E> p) {
+    using L = GradLds<E>;
     using TR = Tr<E>;
-    using WD = Wide<E>;
+    using WD = Full<E>;
+    using WH = Half<E>;
     using frag = typename TR::frag;
     using wfrag = typename WD::frag;
-    constexpr int NW = L::NW, NT = 64 * NW;
+    constexpr int NW = kGradWaves, NT = 64 * NW, NK = DK / 64;     // NK: channel tiles per wave
+    constexpr int VE = 16 / (int)sizeof(E);
+    constexpr int NST = kChunk * 64 / 4 / NT, NSO = kChunk * 64 / VE / NT;   // staged quads / vectors per thread
     extern __shared__ __align__(16) unsigned char smem[];
-    E *sE = (E *)(smem + L::oE), *sV = (E *)(smem + L::oV), *sG1 = (E *)(smem + L::oG1), *sX = (E *)(smem + L::oX),
-      *sG2 = (E *)(smem + L::oG2), *sD = (E *)(smem + L::oD);
+    E *sE = (E *)(smem + L::oE), *sV = (E *)(smem + L::oV), *sO = (E *)(smem + L::oO), *sX = (E *)(smem + L::oX),
+      *sG1 = (E *)(smem + L::oG1), *sG2 = (E *)(smem + L::oG2);
     const double *sg = (const double *)(smem + L::oGate);
     const float *gate = (const float *)(smem + L::oGate);
     const float *gam = gate + kBackGam, *tail = gate + kBackTail, *beta = gate + kBackBeta;
-    float *rX = (float *)(smem + L::oRed), *rE = rX + NW * 64, *cb = rE + NW * 64, *ca = cb + 4 * 64, *xm = ca + 4 * 64,
-          *cC = xm + 64, *gh = cC + 64;
+    float *rX = (float *)(smem + L::oRed), *rE = rX + 4 * 64, *cb = rE + 4 * 64, *xm = cb + 4 * 64, *gh = xm + 64;
     const int c = blockIdx.x / (p.B * p.H), bh = blockIdx.x - c * (p.B * p.H);
     const int b = bh / p.H, h = bh - b * p.H;
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, li = l & 15, lg = l >> 4;
     const int t0 = c * kChunk, nvalid = min(kChunk, p.T - t0);
     const size_t cidx = (size_t)bh * p.NC + c;
     const size_t row0 = ((size_t)b * p.T + t0) * p.H + h;
-    auto rows = [&](const E *base, int D, int r, int kb) {          // row fragment of an input
-        return r < nvalid ? load_frag<E>(base + (row0 + (size_t)r * p.H) * D + 32 * kb, lg) : TR::cat(TR::zero(), TR::zero());
+    // row fragments of K and Q; rows past the end read the last one, whose products
+    // with them meet beta = 0, dO = 0 or dV = 0
+    auto rows = [&](const E *base, int r, int kb) {
+        return load_frag<E>(base + (row0 + (size_t)min(r, nvalid - 1) * p.H) * DK + 32 * kb, lg);
     };
-
-    // e^T and dV^T, gates; G1^T and X^T are zero where no tile writes them
-    {
-        constexpr int VE = 16 / (int)sizeof(E), NV = wide_elems<E>(kChunk * DV) / VE;
-        const E *ge = p.eT + cidx * (size_t)wide_elems<E>(kChunk * DV), *gv = p.vT + cidx * (size_t)wide_elems<E>(kChunk * DV);
-#pragma unroll 4
-        for (int i = tid; i < NV; i += NT) {
-            const int r = i / (kChunk / VE), cv = i % (kChunk / VE), pl = r / DV;    // rows of plane 0, then 1
-            const size_t at = (size_t)pl * L::PV + (size_t)(r - pl * DV) * L::LDC + cv * VE;
-            *(uint4 *)(sE + at) = *(const uint4 *)(ge + (size_t)i * VE);
-            *(uint4 *)(sV + at) = *(const uint4 *)(gv + (size_t)i * VE);
+    const float *ge = p.eT + cidx * (size_t)(kChunk * DV), *gv = p.vT + cidx * (size_t)(kChunk * DV);
+    auto stage_part = [&](int dv0) {                               // 64 value channels into LDS
+        f32x4 re[NST], rv[NST];
+        uint4 ro[NSO];
+#pragma unroll
+        for (int i = 0; i < NST; ++i) {
+            re[i] = *(const f32x4 *)(ge + dv0 * kChunk + (tid + i * NT) * 4);
+            rv[i] = *(const f32x4 *)(gv + dv0 * kChunk + (tid + i * NT) * 4);
         }
-        for (int i = tid; i < kBackGateRec; i += NT) ((float *)(smem + L::oGate))[i] = p.gates[cidx * kBackGateRec + i];
-        for (int i = tid; i < (int)(2 * L::szC / 4); i += NT) ((float *)(smem + L::oG1))[i] = 0.f;
-    }
-    lds_barrier();
+#pragma unroll
+        for (int i = 0; i < NSO; ++i) {
+            const int idx = tid + i * NT, r = idx / (64 / VE), cv = idx % (64 / VE);
+            ro[i] = *(const uint4 *)(p.dout + (row0 + (size_t)min(r, nvalid - 1) * p.H) * DV + dv0 + cv * VE);
+        }
+#pragma unroll
+        for (int i = 0; i < NST; ++i) {
+            const int idx = tid + i * NT, at = (idx >> 4) * L::LDC + (idx & 15) * 4;
+            WD::store4(sE + at, L::PC, re[i]);
+            WD::store4(sV + at, L::PC, rv[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < NSO; ++i) {
+            const int idx = tid + i * NT, r = idx / (64 / VE), cv = idx % (64 / VE);
+            *(uint4 *)(sO + r * L::LDC + cv * VE) = r < nvalid ? ro[i] : make_uint4(0u, 0u, 0u, 0u);
+        }
+    };
+    for (int i = tid; i < kBackGateRec; i += NT) ((float *)(smem + L::oGate))[i] = p.gates[cidx * kBackGateRec + i];
 
-    // D_{t-1,j}: thread (t, 8 j)
-    for (int i = tid; i < 64 * 8; i += NT) {
-        const int t = i >> 3, j0 = 8 * (i & 7);
-        f32x4 x[2];
+    // PQ, PV, PE transposed, tiles [16 key channels][16 tokens]; Z and F
+    constexpr int NTI = 3;                                         // lower tiles w, w + 4, w + 8 of ten
+    f32x4 pq[NK][4], pv[NK][4], pe[NK][4], z[NTI], f[NTI], dot = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e >> 2][e & 3] = j0 + e < t ? expf((float)(sg[t > 0 ? t - 1 : 0] - sg[j0 + e])) : 0.f;
-        WD::store8(sD + t * L::LDC + j0, L::PC, WD::split(x[0], x[1]));
-    }
-
-    // PQ, PV, PE transposed: tiles [16 key channels][16 tokens]
-    f32x4 pq[4], pv[4], pe[4];
+    for (int n = 0; n < NTI; ++n) z[n] = f[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int rt = 0; rt < 4; ++rt) pq[rt] = pv[rt] = pe[rt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    {
-        const size_t sb = cidx * (size_t)wide_elems<E>(DK * DV) + (size_t)(16 * w + li) * DV + 8 * lg;
-        f32x4 dot = {0.f, 0.f, 0.f, 0.f};
+    for (int n = 0; n < NK; ++n)
 #pragma unroll
-        for (int kb = 0; kb < DV / 32; ++kb) {
-            const wfrag H = WD::load8(p.Hs + sb + 32 * kb, (size_t)DK * DV), G = WD::load8(p.Gs + sb + 32 * kb, (size_t)DK * DV);
-            f32x4 ha, hb, ga, gb;
-            WD::values(H, ha, hb);
-            WD::values(G, ga, gb);
-            dot += ha * ga + hb * gb;
+        for (int rt = 0; rt < 4; ++rt) pq[n][rt] = pv[n][rt] = pe[n][rt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const size_t sb = cidx * (size_t)(DK * DV) + (size_t)(16 * NK * w + li) * DV + 8 * lg;
+#pragma unroll 1
+    for (int dv0 = 0; dv0 < DV; dv0 += 64) {
+        if (dv0) lds_barrier();
+        stage_part(dv0);
+        lds_barrier();
+#pragma unroll 1
+        for (int kb = 0; kb < 2; ++kb) {
+            const size_t at = sb + dv0 + 32 * kb;
+            f32x4 h[NK][2];
+            wfrag S[NK];
+#pragma unroll
+            for (int n = 0; n < NK; ++n) {
+                h[n][0] = *(const f32x4 *)(p.Hs + at + (size_t)16 * n * DV);
+                h[n][1] = *(const f32x4 *)(p.Hs + at + (size_t)16 * n * DV + 4);
+                S[n] = WD::split(h[n][0], h[n][1]);
+            }
 #pragma unroll
             for (int rt = 0; rt < 4; ++rt) {
-                pq[rt] = WD::we(H, rows(p.dout, DV, 16 * rt + li, kb), pq[rt]);
-                pv[rt] = WD::ww(H, WD::tr(sV, L::PV, L::LDC, 32 * kb, 16 * rt, li, lg), pv[rt]);
-                pe[rt] = WD::ww(G, WD::tr(sE, L::PV, L::LDC, 32 * kb, 16 * rt, li, lg), pe[rt]);
+                const frag o = load_frag<E>(sO + (16 * rt + li) * L::LDC + 32 * kb, lg);
+                const wfrag dv = WD::tr(sV, L::PC, L::LDC, 32 * kb, 16 * rt, li, lg);
+#pragma unroll
+                for (int n = 0; n < NK; ++n) {
+                    pq[n][rt] = WD::we(S[n], o, pq[n][rt]);
+                    pv[n][rt] = WD::ww(S[n], dv, pv[n][rt]);
+                }
+                // dV: wave rt stores the rows it has at hand
+                if (w == rt && 16 * rt + li < nvalid)
+                    TR::store8(p.dv + (row0 + (size_t)(16 * rt + li) * p.H) * DV + dv0 + 32 * kb + 8 * lg, WD::rounded(dv));
+            }
+#pragma unroll
+            for (int n = 0; n < NK; ++n) {
+                const f32x4 ga = *(const f32x4 *)(p.Gs + at + (size_t)16 * n * DV),
+                            gb = *(const f32x4 *)(p.Gs + at + (size_t)16 * n * DV + 4);
+                dot += h[n][0] * ga + h[n][1] * gb;
+                S[n] = WD::split(ga, gb);
+            }
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt) {
+                const wfrag e = WD::tr(sE, L::PC, L::LDC, 32 * kb, 16 * rt, li, lg);
+#pragma unroll
+                for (int n = 0; n < NK; ++n) pe[n][rt] = WD::ww(S[n], e, pe[n][rt]);
+            }
+#pragma unroll
+            for (int n = 0; n < NTI; ++n) {
+                if (w + 4 * n >= 10) continue;
+                int bi, bj;
+                lower_tile(w + 4 * n, bi, bj);
+                const wfrag ej = WD::tr(sE, L::PC, L::LDC, 32 * kb, 16 * bj, li, lg);
+                z[n] = WD::ew(load_frag<E>(sO + (16 * bi + li) * L::LDC + 32 * kb, lg), ej, z[n]);
+                f[n] = WD::ww(WD::tr(sV, L::PC, L::LDC, 32 * kb, 16 * bi, li, lg), ej, f[n]);
             }
         }
+    }
+    {
         float s = dot[0] + dot[1] + dot[2] + dot[3];
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) s += __shfl_xor(s, d);
@@ -609,17 +671,18 @@ __global__ __launch_bounds__(64 * (DK / 16)) void gdn_back_grad_kernel(BackParam
 #pragma unroll
     for (int rt = 0; rt < 4; ++rt) {
         const int t = 16 * rt + li;
-        f32x4 q4 = {0.f, 0.f, 0.f, 0.f}, k4 = q4;
-        if (t < nvalid) {
-            const size_t at = (row0 + (size_t)t * p.H) * DK + 16 * w + 4 * lg;
-            q4 = TR::to_f32(TR::load(p.q + at));
-            k4 = TR::to_f32(TR::load(p.k + at));
-        }
         float x = 0.f, y = 0.f;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            x += q4[q] * pq[rt][q] - k4[q] * pv[rt][q];
-            y += k4[q] * pe[rt][q];
+        for (int n = 0; n < NK; ++n) {
+            const size_t at = (row0 + (size_t)min(t, nvalid - 1) * p.H) * DK + 16 * (NK * w + n) + 4 * lg;
+            const f32x4 q4 = TR::to_f32(TR::load(p.q + at)), k4 = TR::to_f32(TR::load(p.k + at));
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                x += q4[q] * pq[n][rt][q] - k4[q] * pv[n][rt][q];
+                y += k4[q] * pe[n][rt][q];
+            }
+            pq[n][rt] *= gam[t];
+            pe[n][rt] = pe[n][rt] * (tail[t] * beta[t]) - pv[n][rt] * gam[t];
         }
         x += __shfl_xor(x, 16);
         x += __shfl_xor(x, 32);
@@ -629,53 +692,48 @@ __global__ __launch_bounds__(64 * (DK / 16)) void gdn_back_grad_kernel(BackParam
             rX[w * 64 + t] = x;
             rE[w * 64 + t] = y;
         }
-        pq[rt] *= gam[t];
-        pe[rt] = pe[rt] * (tail[t] * beta[t]) - pv[rt] * gam[t];
     }
-    // The 64 x 64 products, lower tiles: element (i, j) with i = 16 bi + 4 lg + q, j = 16 bj + li.
-    for (int t = w; t < 10; t += NW) {
+    lds_barrier();
+    // The 64 x 64 matrices: element (i, j) with i = 16 bi + 4 lg + q, j = 16 bj + li.  The six
+    // tiles above the diagonal of G1 and X are zero.
+#pragma unroll
+    for (int n = 0; n < NTI; ++n) {
+        if (w + 4 * n >= 10) continue;
         int bi, bj;
-        lower_tile(t, bi, bj);
-        f32x4 sqk = {0.f, 0.f, 0.f, 0.f}, skk = sqk, z = sqk, f = sqk;
-#pragma unroll
-        for (int kb = 0; kb < DK / 32; ++kb) {
-            const frag kj = rows(p.k, DK, 16 * bj + li, kb);
-            sqk = TR::mma(rows(p.q, DK, 16 * bi + li, kb), kj, sqk);
-            skk = TR::mma(rows(p.k, DK, 16 * bi + li, kb), kj, skk);
-        }
-#pragma unroll
-        for (int kb = 0; kb < DV / 32; ++kb) {
-            const wfrag ej = WD::tr(sE, L::PV, L::LDC, 32 * kb, 16 * bj, li, lg);
-            z = WD::ew(rows(p.dout, DV, 16 * bi + li, kb), ej, z);
-            f = WD::ww(WD::tr(sV, L::PV, L::LDC, 32 * kb, 16 * bi, li, lg), ej, f);
-        }
+        lower_tile(w + 4 * n, bi, bj);
         const int j = 16 * bj + li, i0 = 16 * bi + 4 * lg;
         const float bj_ = beta[j];
-        f32x4 g1, g2, xx;
+        f32x4 sqk = {0.f, 0.f, 0.f, 0.f}, skk = sqk, g1, g2, xx;
+#pragma unroll
+        for (int kb = 0; kb < DK / 32; ++kb) {
+            const frag kj = rows(p.k, 16 * bj + li, kb);
+            sqk = TR::mma(rows(p.q, 16 * bi + li, kb), kj, sqk);
+            skk = TR::mma(rows(p.k, 16 * bi + li, kb), kj, skk);
+        }
         float cs = 0.f;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const int i = i0 + q;
             const float d = i >= j ? expf((float)(sg[i] - sg[j])) : 0.f;
-            const float dz = d * z[q], df = i > j ? d * f[q] : 0.f;
+            const float dz = d * z[n][q], df = i > j ? d * f[n][q] : 0.f;
             g1[q] = dz * bj_;
             g2[q] = df * bj_;
-            xx[q] = i > j ? bj_ * (sqk[q] * z[q] - skk[q] * f[q]) : 0.f;
+            xx[q] = i > j ? bj_ * (sqk[q] * z[n][q] - skk[q] * f[n][q]) : 0.f;
             cs += sqk[q] * dz - skk[q] * df;
         }
-        WD::store4(sG1 + j * L::LDC + i0, L::PC, g1);
+        WH::store4(sG1 + j * L::LDC + i0, L::PC, g1);
         WD::store4(sX + j * L::LDC + i0, L::PC, xx);
         if (bi != bj) {
-            WD::store4(sG2 + j * L::LDC + i0, L::PC, g2);
+            WH::store4(sG2 + j * L::LDC + i0, L::PC, g2);
+            const f32x4 none = {0.f, 0.f, 0.f, 0.f};
+            WH::store4(sG1 + (16 * bi + li) * L::LDC + 16 * bj + 4 * lg, L::PC, none);
+            WD::store4(sX + (16 * bi + li) * L::LDC + 16 * bj + 4 * lg, L::PC, none);
+        }
 #pragma unroll
-            for (int q = 0; q < 4; ++q) WD::store1(sG2 + (i0 + q) * L::LDC + j, L::PC, g2[q]);
-        } else {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                if (i0 + q < j) continue;                // written from below the diagonal
-                WD::store1(sG2 + (i0 + q) * L::LDC + j, L::PC, g2[q]);
-                if (i0 + q > j) WD::store1(sG2 + j * L::LDC + i0 + q, L::PC, g2[q]);
-            }
+        for (int q = 0; q < 4; ++q) {
+            if (i0 + q < j) continue;                              // written from below the diagonal
+            WH::store1(sG2 + (i0 + q) * L::LDC + j, L::PC, g2[q]);
+            if (bi == bj && i0 + q > j) WH::store1(sG2 + j * L::LDC + i0 + q, L::PC, g2[q]);
         }
         cs += __shfl_xor(cs, 16);
         cs += __shfl_xor(cs, 32);
@@ -700,73 +758,86 @@ __global__ __launch_bounds__(64 * (DK / 16)) void gdn_back_grad_kernel(BackParam
     // dQ += G1 K;  dK += G1^T Q - (G2 + G2^T) K
     {
         const E *Kt = p.Kt + cidx * (size_t)DK * kChunk + l * 8, *Qt = p.Qt + cidx * (size_t)DK * kChunk + l * 8;
-        frag kt[2], qt[2], km[2];
+        frag kt[NK][2], qt[NK][2];
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            kt[kb] = TR::load8(Kt + (size_t)(w * 2 + kb) * 512);
-            qt[kb] = TR::load8(Qt + (size_t)(w * 2 + kb) * 512);
-            if constexpr (sizeof(E) == 2) km[kb] = kt[kb] ^ 0x80008000u;     // -K^T
-            else km[kb] = -kt[kb];
-        }
-#pragma unroll
-        for (int rt = 0; rt < 4; ++rt) {
-            f32x4 dq = pq[rt], dk = pe[rt];
+        for (int n = 0; n < NK; ++n)
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
-                if (kb <= rt / 2) dq = WD::ew(kt[kb], WD::tr(sG1, L::PC, L::LDC, 32 * kb, 16 * rt, li, lg), dq);
-                if (kb >= rt / 2) dk = WD::ew(qt[kb], WD::load8(sG1 + (16 * rt + li) * L::LDC + 32 * kb + 8 * lg, L::PC), dk);
-                dk = WD::ew(km[kb], WD::load8(sG2 + (16 * rt + li) * L::LDC + 32 * kb + 8 * lg, L::PC), dk);
+                kt[n][kb] = TR::load8(Kt + ((w * NK + n) * 2 + kb) * 512);
+                qt[n][kb] = TR::load8(Qt + ((w * NK + n) * 2 + kb) * 512);
+            }
+#pragma unroll
+        for (int rt = 0; rt < 4; ++rt) {
+            f32x4 gk[NK];
+#pragma unroll
+            for (int n = 0; n < NK; ++n) gk[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                const int at = (16 * rt + li) * L::LDC + 32 * kb + 8 * lg;
+                const typename WH::frag g2 = WH::load8(sG2 + at, L::PC);
+#pragma unroll
+                for (int n = 0; n < NK; ++n) gk[n] = WH::ew(kt[n][kb], g2, gk[n]);
+                if (kb <= rt / 2) {
+                    const typename WH::frag g1 = WH::tr(sG1, L::PC, L::LDC, 32 * kb, 16 * rt, li, lg);
+#pragma unroll
+                    for (int n = 0; n < NK; ++n) pq[n][rt] = WH::ew(kt[n][kb], g1, pq[n][rt]);
+                }
+                if (kb >= rt / 2) {
+                    const typename WH::frag g1 = WH::load8(sG1 + at, L::PC);
+#pragma unroll
+                    for (int n = 0; n < NK; ++n) pe[n][rt] = WH::ew(qt[n][kb], g1, pe[n][rt]);
+                }
             }
             const int t = 16 * rt + li;
             if (t < nvalid) {
-                const size_t at = (row0 + (size_t)t * p.H) * DK + 16 * w + 4 * lg;
-                TR::store(p.dq + at, TR::from_f32(dq));
-                TR::store(p.dk + at, TR::from_f32(dk));
+#pragma unroll
+                for (int n = 0; n < NK; ++n) {
+                    const size_t at = (row0 + (size_t)t * p.H) * DK + 16 * (NK * w + n) + 4 * lg;
+                    TR::store(p.dq + at, TR::from_f32(pq[n][rt]));
+                    TR::store(p.dk + at, TR::from_f32(pe[n][rt] - gk[n]));
+                }
             }
         }
     }
-    // dV from its transpose
-    for (int f = w; f < 4 * (DV / 32); f += NW) {
-        const int rt = f & 3, kb = f >> 2, t = 16 * rt + li;
-        const frag x = WD::rounded(WD::tr(sV, L::PV, L::LDC, 32 * kb, 16 * rt, li, lg));
-        if (t < nvalid) TR::store8(p.dv + (row0 + (size_t)t * p.H) * DV + 32 * kb + 8 * lg, x);
-    }
     lds_barrier();
     // dalpha: M_it = sum_j X_ij D_{t-1,j}, then D_it M_it summed over rows; row 0 of X is the
-    // exit state's (its own has no j < 0), so row tile 0 is needed for every t
-    for (int f = w; f < 16; f += NW) {
-        const int bi = f >> 2, bt = f & 3;
-        if (bt > bi && bi != 0) continue;
-        f32x4 m = {0.f, 0.f, 0.f, 0.f};
+    // exit state's (its own has no j < 0), so row tile 0 is needed for every t.  Wave w has the
+    // tokens t of tile w.
+    {
+        const int t = 16 * w + li;
+        const double gt1 = t > 0 ? sg[t - 1] : 0.0;
+        wfrag D[2];
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-            if (kb <= bt / 2)
-                m = WD::ww(WD::tr(sX, L::PC, L::LDC, 32 * kb, 16 * bi, li, lg),
-                           WD::load8(sD + (16 * bt + li) * L::LDC + 32 * kb + 8 * lg, L::PC), m);
-        const int t = 16 * bt + li, i0 = 16 * bi + 4 * lg;
-        const float gb = t > 0 ? gam[t - 1] : 1.f;
-        if (bi == 0 && lg == 0) {
-            float s = 0.f;
+        for (int kb = 0; kb < 2; ++kb) {
+            if (kb > w / 2) continue;
+            f32x4 x[2];
 #pragma unroll
-            for (int i = 0; i < NW; ++i) s += gh[i];
-            cC[t] = tail[t] * (m[0] + s * gb);
+            for (int e = 0; e < 8; ++e) {
+                const int j = 32 * kb + 8 * lg + e;
+                x[e >> 2][e & 3] = j < t ? expf((float)(gt1 - sg[j])) : 0.f;
+            }
+            D[kb] = WD::split(x[0], x[1]);
         }
+        const float gb = t > 0 ? gam[t - 1] : 1.f, s = gh[0] + gh[1] + gh[2] + gh[3];
         float cs = 0.f;
+        for (int bi = 0; bi < 4; ++bi) {
+            if (bi < w && bi != 0) continue;
+            f32x4 m = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int i = i0 + q;
-            if (i == 0) m[q] = 0.f;
-            if (i >= t) cs += expf((float)(sg[i] - sg[t])) * (m[q] + xm[i] * gb);
+            for (int kb = 0; kb < 2; ++kb)
+                if (kb <= w / 2) m = WD::ww(WD::tr(sX, L::PC, L::LDC, 32 * kb, 16 * bi, li, lg), D[kb], m);
+            const int i0 = 16 * bi + 4 * lg;
+            if (i0 == 0) {
+                cs += tail[t] * (m[0] + s * gb);
+                m[0] = 0.f;
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                if (i0 + q >= t) cs += expf((float)(sg[i0 + q] - sg[t])) * (m[q] + xm[i0 + q] * gb);
         }
         cs += __shfl_xor(cs, 16);
         cs += __shfl_xor(cs, 32);
-        if (lg == 0 && bt <= bi) ca[bi * 64 + t] = cs;
-    }
-    lds_barrier();
-    if (tid < nvalid) {
-        float d = cC[tid];
-        for (int bi = tid >> 4; bi < 4; ++bi) d += ca[bi * 64 + tid];
-        p.dalpha[row0 + (size_t)tid * p.H] = d;
+        if (lg == 0 && t < nvalid) p.dalpha[row0 + (size_t)t * p.H] = cs;
     }
 }
 

@@ -134,11 +134,12 @@ template <class E> int dispatch_norm(const gdn::NormParams<E> &p, bool grad, hip
 
 // Byte offsets of the workspace regions (the records of gdn_backward.h).
 struct BackWs {
-    size_t gates, Tf, Tt, Kt, Qt, N0, Gd, Hs, Gs, eT, vT, total;
+    size_t gates, Tf, Tt, Kt, Qt, N0, Hs, Gs, eT, vT, total;
 };
 
 BackWs back_layout(int B, int H, int T, int Dk, int Dv, size_t esz) {
     using gdn::kChunk;
+    const size_t full = esz == 2 ? 6 : 4;     // bytes of an element in planes
     const size_t n = (size_t)B * H * (((size_t)T + kChunk - 1) / kChunk);
     BackWs L;
     size_t off = 0;
@@ -148,12 +149,11 @@ BackWs back_layout(int B, int H, int T, int Dk, int Dv, size_t esz) {
         return at;
     };
     L.gates = region(4 * gdn::kBackGateRec);
-    L.Tf = region(4 * kChunk * kChunk);
-    L.Tt = region(4 * kChunk * kChunk);
+    L.Tf = region(full * kChunk * kChunk);
+    L.Tt = region(full * kChunk * kChunk);
     L.Kt = region(esz * Dk * kChunk);
     L.Qt = region(esz * Dk * kChunk);
     L.N0 = region(4 * kChunk * Dv);
-    L.Gd = region(4 * kChunk * Dv);
     L.Hs = region(4 * (size_t)Dk * Dv);
     L.Gs = region(4 * (size_t)Dk * Dv);
     L.eT = region(4 * kChunk * Dv);
@@ -170,7 +170,7 @@ bool back_shape_ok(int B, int H, int T) {
 
 template <class E, int DK, int DV> int launch_backward(const gdn::BackParams<E> &p, hipStream_t s) {
     using P = gdn::PrepLds<E, DK, DV>;
-    using G = gdn::GradLds<E, DK, DV>;
+    using G = gdn::GradLds<E>;
     static std::once_flag once;
     static hipError_t attr = hipSuccess;
     std::call_once(once, [] {
@@ -187,7 +187,7 @@ template <class E, int DK, int DV> int launch_backward(const gdn::BackParams<E> 
         st = launch(gdn::gdn_back_scan_kernel<E, DK, DV>, dim3((bh + 7) / 8 * 8 * (DV / 16), 2),
                     dim3(64 * gdn::kBackScanWaves), 0, s, p);
     if (st == GDN_OK)
-        st = launch(gdn::gdn_back_grad_kernel<E, DK, DV>, dim3(n), dim3(64 * G::NW), G::bytes, s, p);
+        st = launch(gdn::gdn_back_grad_kernel<E, DK, DV>, dim3(n), dim3(64 * gdn::kGradWaves), G::bytes, s, p);
     return st;
 }
 
@@ -258,11 +258,10 @@ int gdn_chunk_backward(const void *q, const void *k, const void *v, const float 
         p.Tt = (E *)(base + L.Tt);
         p.Kt = (E *)(base + L.Kt);
         p.Qt = (E *)(base + L.Qt);
-        p.Gd = (E *)(base + L.Gd);
-        p.Hs = (E *)(base + L.Hs);
-        p.Gs = (E *)(base + L.Gs);
-        p.eT = (E *)(base + L.eT);
-        p.vT = (E *)(base + L.vT);
+        p.Hs = (float *)(base + L.Hs);
+        p.Gs = (float *)(base + L.Gs);
+        p.eT = (float *)(base + L.eT);
+        p.vT = (float *)(base + L.vT);
         return dispatch_backward<E>(p, Dk, Dv, (hipStream_t)stream);
     };
     return is_bf16 ? run((uint16_t *)nullptr) : run((float *)nullptr);
