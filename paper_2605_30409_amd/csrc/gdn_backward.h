@@ -144,8 +144,8 @@ constexpr int kBackGam = 128, kBackTail = 192, kBackBeta = 256, kBackGC = 320, k
 // Workspace records per (b*H + h, chunk); "planes": three of bf16, each behind the
 // whole of the one before, on the bf16 path, fp32 on the other.
 //   gates [336] fp32
-//   Tf, Tt  64 x 64   planes, fragments [4 row tile][2 k block][64 lane][8] of T and T^T
-//   Kt, Qt  Dk x 64   E, fragments [Dk/16][2][64][8] of K^T and Q^T
+//   Tf, Tt  64 x 64   planes, fragments [4 row tile][2 k block][64 lane][8] of T and T^T (those
+//                     that are all zeros are neither written nor read)
 //   N0      64 x Dv   fp32, beta A^T dO as accumulator tiles [Dv/16][4][64 lane][4]
 //   Hs, Gs  Dk x Dv   fp32, row-major: H and G of the chunk
 //   eT, vT  Dv x 64   fp32, row-major: e^T and dV^T
@@ -156,7 +156,7 @@ template <class E> struct BackParams {
     float *dalpha, *dbeta, *dstate_in;
     int B, H, T, NC;
     float *gates, *N0, *Hs, *Gs, *eT, *vT;
-    E *Tf, *Tt, *Kt, *Qt;
+    E *Tf, *Tt;
 };
 
 template <class E> constexpr int full_elems(int n) { return n * Full<E>::planes; }
@@ -167,16 +167,19 @@ template <class E> constexpr int lds_ld(int n) { return n + 16 / (int)sizeof(E);
 // --------------------------------------------------------------------------
 // Stage 1, per chunk and head: gates, T, and the operands of the scans.
 // --------------------------------------------------------------------------
+// LDS: K rows, Q rows (dO takes their place once A is formed), N below the diagonal and T^T
+// on and above it in one fp32 square, A^T: 80.6 KB on the bf16 path at D = 128, two
+// workgroups a CU.
 template <class E, int DK, int DV> struct PrepLds {
     static constexpr int LDK = lds_ld<E>(DK), LDV = lds_ld<E>(DV), LDA = kChunk + 4, LDT = lds_ld<E>(kChunk);
     static constexpr size_t oK = 0;
-    static constexpr size_t oQ = oK + sizeof(E) * kChunk * LDK;
-    static constexpr size_t oO = oQ + sizeof(E) * kChunk * LDK;
-    static constexpr size_t oN = oO + sizeof(E) * kChunk * LDV;    // N, fp32
-    static constexpr size_t oT = oN + 4 * kChunk * LDA;            // T, fp32
-    static constexpr size_t oA = oT + 4 * kChunk * LDA;            // A^T, wide
+    static constexpr size_t oQ = oK + sizeof(E) * kChunk * LDK;    // Q, then dO
+    static constexpr size_t oN = oQ + sizeof(E) * kChunk * (LDK > LDV ? LDK : LDV);
+    static constexpr size_t oA = oN + 4 * kChunk * LDA;            // A^T, planes
     static constexpr size_t oG = oA + sizeof(E) * Full<E>::planes * kChunk * LDT;
     static constexpr size_t bytes = oG + 8 * kChunk + 4 * kChunk;
+    // waves per SIMD of the eight-wave workgroups that fit a CU
+    static constexpr int waves_per_simd = bytes * 2 <= 160 * 1024 ? 4 : 2;
 };
 
 constexpr int kPrepWaves = 8;
@@ -187,29 +190,40 @@ __device__ __forceinline__ void lower_tile(int t, int &bi, int &bj) {
     bj = t - bi * (bi + 1) / 2;
 }
 
-// 16-byte vectors of a [64][D] tile of token rows into LDS, rows past nvalid as zeros.
-template <class E, int D, int NT>
-__device__ __forceinline__ void stage_rows(const E *src, size_t rstride, int nvalid, E *dst, int ld, int tid) {
-    constexpr int VE = 16 / (int)sizeof(E), NVEC = kChunk * (D / VE);
+// A [64][D] tile of token rows in 16-byte vectors: NT threads read it into registers (rows
+// past nvalid as the last one) and write it to LDS (those rows as zeros).
+template <class E, int D, int NT> struct RowTile {
+    static constexpr int VE = 16 / (int)sizeof(E), N = kChunk * (D / VE) / NT;
+    static_assert(N * NT == kChunk * (D / VE), "whole vectors per thread");
+    uint4 x[N];
+    __device__ __forceinline__ void load(const E *src, size_t rstride, int nvalid, int tid) {
 #pragma unroll
-    for (int i0 = 0; i0 < NVEC; i0 += NT) {
-        const int idx = tid + i0, r = idx / (D / VE), cv = idx % (D / VE);
-        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-        if (r < nvalid) x = *(const uint4 *)(src + r * rstride + cv * VE);
-        *(uint4 *)(dst + r * ld + cv * VE) = x;
+        for (int i = 0; i < N; ++i) {
+            const int idx = tid + i * NT, r = min(idx / (D / VE), nvalid - 1);
+            x[i] = *(const uint4 *)(src + r * rstride + idx % (D / VE) * VE);
+        }
     }
-}
+    __device__ __forceinline__ void store(E *dst, int ld, int nvalid, int tid) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int idx = tid + i * NT, r = idx / (D / VE);
+            *(uint4 *)(dst + r * ld + idx % (D / VE) * VE) = r < nvalid ? x[i] : make_uint4(0u, 0u, 0u, 0u);
+        }
+    }
+};
 
 template <class E, int DK, int DV>
-__global__ __launch_bounds__(64 * kPrepWaves) void gdn_back_prep_kernel(BackParams<E> p) {
+__global__ __launch_bounds__(64 * kPrepWaves)
+__attribute__((amdgpu_waves_per_eu(PrepLds<E, DK, DV>::waves_per_simd)))
+void gdn_back_prep_kernel(BackParams<E> p) {
     using L = PrepLds<E, DK, DV>;
     using TR = Tr<E>;
     using WD = Full<E>;
     constexpr int NT = 64 * kPrepWaves;
     constexpr int PA = kChunk * L::LDT;      // plane of A^T
     extern __shared__ __align__(16) unsigned char smem[];
-    E *sK = (E *)(smem + L::oK), *sQ = (E *)(smem + L::oQ), *sO = (E *)(smem + L::oO), *sA = (E *)(smem + L::oA);
-    float *sN = (float *)(smem + L::oN), *sT = (float *)(smem + L::oT);
+    E *sK = (E *)(smem + L::oK), *sQ = (E *)(smem + L::oQ), *sO = sQ, *sA = (E *)(smem + L::oA);
+    float *sN = (float *)(smem + L::oN);     // N[r][c] at [r][c] (c < r), T[r][c] at [c][r] (c <= r)
     double *sg = (double *)(smem + L::oG);
     float *sb = (float *)(sg + kChunk);
     const int c = blockIdx.x / (p.B * p.H), bh = blockIdx.x - c * (p.B * p.H);
@@ -218,14 +232,19 @@ __global__ __launch_bounds__(64 * kPrepWaves) void gdn_back_prep_kernel(BackPara
     const int t0 = c * kChunk, nvalid = min(kChunk, p.T - t0);
     const size_t cidx = (size_t)bh * p.NC + c;
     const size_t row0 = ((size_t)b * p.T + t0) * p.H + h;
-    float *gate = p.gates + cidx * kBackGateRec;
 
+    float a = 1.f, be = 0.f;
+    if (w == 0 && l < nvalid) {
+        a = p.alpha[row0 + (size_t)l * p.H];
+        be = p.beta[row0 + (size_t)l * p.H];
+    }
+    RowTile<E, DK, NT> kr, qr;
+    RowTile<E, DV, NT> orr;
+    kr.load(p.k + row0 * DK, (size_t)p.H * DK, nvalid, tid);
+    qr.load(p.q + row0 * DK, (size_t)p.H * DK, nvalid, tid);
+    orr.load(p.dout + row0 * DV, (size_t)p.H * DV, nvalid, tid);
     if (w == 0) {
-        float a = 1.f, be = 0.f;
-        if (l < nvalid) {
-            a = p.alpha[row0 + (size_t)l * p.H];
-            be = p.beta[row0 + (size_t)l * p.H];
-        }
+        float *gate = p.gates + cidx * kBackGateRec;
         float la = logf(a);
         la = (la < kLogAlphaMin) ? kLogAlphaMin : la;   // keeps NaN
         double g = (double)la;
@@ -243,11 +262,10 @@ __global__ __launch_bounds__(64 * kPrepWaves) void gdn_back_prep_kernel(BackPara
         gate[kBackBeta + l] = be;
         if (l == 0) gate[kBackGC] = expf((float)gC);
     }
-    stage_rows<E, DK, NT>(p.k + row0 * DK, (size_t)p.H * DK, nvalid, sK, L::LDK, tid);
-    stage_rows<E, DK, NT>(p.q + row0 * DK, (size_t)p.H * DK, nvalid, sQ, L::LDK, tid);
-    stage_rows<E, DV, NT>(p.dout + row0 * DV, (size_t)p.H * DV, nvalid, sO, L::LDV, tid);
-    // the tiles of A^T and T that stay empty are read as zeros
-    for (int i = tid; i < (int)(L::oG - L::oT) / 4; i += NT) ((float *)(smem + L::oT))[i] = 0.f;
+    kr.store(sK, L::LDK, nvalid, tid);
+    qr.store(sQ, L::LDK, nvalid, tid);
+    // the tiles of A^T that stay empty are read as zeros
+    for (int i = tid; i < (int)(L::oG - L::oA) / 16; i += NT) ((uint4 *)(smem + L::oA))[i] = make_uint4(0u, 0u, 0u, 0u);
     lds_barrier();
 
     // N and A^T: ten lower tiles each
@@ -265,15 +283,18 @@ __global__ __launch_bounds__(64 * kPrepWaves) void gdn_back_prep_kernel(BackPara
         for (int q = 0; q < 4; ++q) acc[q] = j <= i0 + q ? acc[q] * expf((float)(sg[i0 + q] - sg[j])) : 0.f;
         if (t < 10) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) sN[(i0 + q) * L::LDA + j] = j < i0 + q ? acc[q] * sb[j] : 0.f;
+            for (int q = 0; q < 4; ++q)
+                if (j < i0 + q) sN[(i0 + q) * L::LDA + j] = acc[q] * sb[j];
         } else {
             WD::store4(sA + j * L::LDT + i0, PA, acc);
         }
     }
     lds_barrier();
+    orr.store(sO, L::LDV, nvalid, tid);
+    lds_barrier();
 
     // T = (I + N)^{-1}: the diagonal blocks by substitution (lane = block * 16 +
-    // column) on wave 0, while the others write the operands that do not need T.
+    // column) on wave 0, while the others form beta A^T dO.
     if (w == 0) {
         const int base = 16 * lg;
         float x[16];
@@ -285,14 +306,9 @@ __global__ __launch_bounds__(64 * kPrepWaves) void gdn_back_prep_kernel(BackPara
             x[r] = acc;
         }
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sT[(base + r) * L::LDA + base + li] = x[r];
+        for (int r = 0; r < 16; ++r)
+            if (r >= li) sN[(base + li) * L::LDA + base + r] = x[r];
     } else {
-        E *Kt = p.Kt + cidx * (size_t)DK * kChunk, *Qt = p.Qt + cidx * (size_t)DK * kChunk;
-        for (int f = w - 1; f < 2 * (DK / 16) * 2; f += kPrepWaves - 1) {
-            const int which = f & 1, kb = (f >> 1) & 1, t = f >> 2;
-            TR::store8((which ? Qt : Kt) + (size_t)(t * 2 + kb) * 512 + l * 8,
-                       tr_frag<E>(which ? sQ : sK, L::LDK, 32 * kb, 16 * t, false, 0, li, lg));
-        }
         float *N0 = p.N0 + cidx * (size_t)kChunk * DV;
         for (int f = w - 1; f < (DV / 16) * 4; f += kPrepWaves - 1) {
             const int rt = f & 3, jt = f >> 2;
@@ -313,28 +329,28 @@ __global__ __launch_bounds__(64 * kPrepWaves) void gdn_back_prep_kernel(BackPara
             const int j = w, i = w + dist;
             f32x4 X = {0.f, 0.f, 0.f, 0.f};
             for (int m = j; m < i; ++m) {
-                const f32x4 a = *(const f32x4 *)(sN + (16 * i + li) * L::LDA + 16 * m + 4 * lg);
+                const f32x4 n = *(const f32x4 *)(sN + (16 * i + li) * L::LDA + 16 * m + 4 * lg);
+                f32x4 t = *(const f32x4 *)(sN + (16 * j + li) * L::LDA + 16 * m + 4 * lg);
 #pragma unroll
-                for (int q = 0; q < 4; ++q) X = mma_f32_k4(a[q], sT[(16 * m + 4 * lg + q) * L::LDA + 16 * j + li], X);
+                for (int q = 0; q < 4; ++q) X = mma_f32_k4(n[q], m > j || 4 * lg + q >= li ? t[q] : 0.f, X);
             }
-            const f32x4 a = *(const f32x4 *)(sT + (16 * i + li) * L::LDA + 16 * i + 4 * lg);
             f32x4 Y = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int q = 0; q < 4; ++q) Y = mma_f32_k4(a[q], X[q], Y);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) sT[(16 * i + 4 * lg + q) * L::LDA + 16 * j + li] = -Y[q];
+            for (int q = 0; q < 4; ++q)
+                Y = mma_f32_k4(li >= 4 * lg + q ? sN[(16 * i + 4 * lg + q) * L::LDA + 16 * i + li] : 0.f, X[q], Y);
+            *(f32x4 *)(sN + (16 * j + li) * L::LDA + 16 * i + 4 * lg) = -Y;
         }
         lds_barrier();
     }
-    // T and T^T as fragments: one of 16 per wave and turn
+    // T and T^T as fragments
     for (int f = w; f < 16; f += kPrepWaves) {
-        const int kb = f & 1, rt = (f >> 1) & 3;
+        const int kb = f & 1, rt = (f >> 1) & 3, r = 16 * rt + li, k0 = 32 * kb + 8 * lg;
+        if (f < 8 ? kb > rt / 2 : kb < rt / 2) continue;
         f32x4 x[2];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int k = 32 * kb + 8 * lg + e, r = 16 * rt + li;
-            x[e >> 2][e & 3] = f < 8 ? sT[r * L::LDA + k] : sT[k * L::LDA + r];
-        }
+        for (int e = 0; e < 8; ++e)
+            x[e >> 2][e & 3] = f < 8 ? (k0 + e <= r ? sN[(k0 + e) * L::LDA + r] : 0.f)
+                                     : (k0 + e >= r ? sN[r * L::LDA + k0 + e] : 0.f);
         E *dst = (f < 8 ? p.Tf : p.Tt) + cidx * (size_t)full_elems<E>(kChunk * kChunk);
         WD::store8(dst + (rt * 2 + kb) * 512 + l * 8, kChunk * kChunk, WD::split(x[0], x[1]));
     }
@@ -356,65 +372,74 @@ constexpr int kBackScanWaves = 4;
 template <class E, int DK> struct BackScanLds {
     static constexpr int LDH = lds_ld<E>(DK), LDC = lds_ld<E>(kChunk);
     static constexpr int PH = 16 * LDH, PC = 16 * LDC;                        // planes
-    static constexpr size_t szC = sizeof(E) * Full<E>::planes * PC;
+    static constexpr size_t szC = sizeof(E) * Full<E>::planes * PC, szR = sizeof(E) * kChunk * LDH;
     static constexpr size_t oX = sizeof(E) * Full<E>::planes * PH;            // T's operand
     static constexpr size_t oY = oX + szC;                                    // T's result, scaled
     static constexpr size_t oD = oY + szC;                                    // gam dO (backward)
-    static constexpr size_t bytes = oD + szC;
+    static constexpr size_t oK = oD + szC;                                    // K rows
+    static constexpr size_t oQ = oK + szR;                                    // Q rows (backward)
+    static constexpr size_t bytes = oQ + szR;
+    // workgroups that fit a CU
+    static constexpr int fit = (int)(160 * 1024 / bytes), waves_per_simd = fit > 3 ? 3 : fit;
 };
 
-// Operands of one chunk, loaded ahead of their use.
+// Operands of one chunk, loaded one chunk ahead of their use, in three parts that
+// are issued in the three phases of the chunk before: together they would hold up
+// its first product by the time the loads take to issue (64 bytes a cycle and CU).
 template <class E, int DK, bool REV> struct BackOps {
-    static constexpr int NT = DK / 64;                  // state row tiles per wave
-    typename Tr<E>::frag K[DK / 32], Kt[NT][2], Qt[REV ? NT : 1][2];
+    typename Tr<E>::frag K[DK / 32], Q[REV ? DK / 32 : 1];    // rows of row tile w
     typename Full<E>::frag T[2];
     E vd[4];                                            // V or dO of four tokens
     f32x4 n0, gam, tail, beta;
     float gC;
 };
 
-template <class E, int DK, int DV, bool REV>
-__device__ __forceinline__ void back_load(const BackParams<E> &p, BackOps<E, DK, REV> &o, int b, int h, int bh, int jt,
-                                          int c, int w, int l) {
-    using TR = Tr<E>;
-    const int li = l & 15, lg = l >> 4;
-    const size_t cidx = (size_t)bh * p.NC + c;
-    const int t0 = c * kChunk, last = min(kChunk, p.T - t0) - 1;
-    const size_t row0 = ((size_t)b * p.T + t0) * p.H + h;
-    const E *krow = p.k + (row0 + (size_t)min(16 * w + li, last) * p.H) * DK;
+template <class E, int DK, int DV, bool REV> struct BackLoader {
+    const BackParams<E> &p;
+    int b, h, bh, jt, w, li, lg, l;
+    using Ops = BackOps<E, DK, REV>;
+    __device__ __forceinline__ size_t row0(int c) const { return ((size_t)b * p.T + c * kChunk) * p.H + h; }
+    __device__ __forceinline__ int last(int c) const { return min(kChunk, p.T - c * kChunk) - 1; }
+    __device__ __forceinline__ void rows(Ops &o, int c) const {
+        const size_t at = (row0(c) + (size_t)min(16 * w + li, last(c)) * p.H) * DK;
 #pragma unroll
-    for (int kb = 0; kb < DK / 32; ++kb) o.K[kb] = load_frag<E>(krow + 32 * kb, lg);
-    const E *Tm = (REV ? p.Tt : p.Tf) + cidx * (size_t)full_elems<E>(kChunk * kChunk);
-#pragma unroll
-    for (int kb = 0; kb < 2; ++kb) o.T[kb] = Full<E>::load8(Tm + (w * 2 + kb) * 512 + l * 8, kChunk * kChunk);
-    const E *Kt = p.Kt + cidx * (size_t)DK * kChunk, *Qt = p.Qt + cidx * (size_t)DK * kChunk;
-#pragma unroll
-    for (int t = 0; t < DK / 64; ++t)
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            const int at = ((w * (DK / 64) + t) * 2 + kb) * 512 + l * 8;
-            o.Kt[t][kb] = TR::load8(Kt + at);
-            if (REV) o.Qt[t][kb] = TR::load8(Qt + at);
+        for (int kb = 0; kb < DK / 32; ++kb) {
+            o.K[kb] = load_frag<E>(p.k + at + 32 * kb, lg);
+            if (REV) o.Q[kb] = load_frag<E>(p.q + at + 32 * kb, lg);
         }
-    const float *gate = p.gates + cidx * kBackGateRec;
-    o.gam = *(const f32x4 *)(gate + kBackGam + 16 * w + 4 * lg);
-    o.tail = *(const f32x4 *)(gate + kBackTail + 16 * w + 4 * lg);
-    o.beta = *(const f32x4 *)(gate + kBackBeta + 16 * w + 4 * lg);
-    o.gC = gate[kBackGC];
-    if (REV) o.n0 = *(const f32x4 *)(p.N0 + cidx * (size_t)kChunk * DV + (jt * 4 + w) * 256 + l * 4);
-    const E *x = (REV ? p.dout : p.v) + row0 * DV + 16 * jt + li;
+    }
+    __device__ __forceinline__ void inverse(Ops &o, int c) const {
+        const E *T = (REV ? p.Tt : p.Tf) + ((size_t)bh * p.NC + c) * (size_t)full_elems<E>(kChunk * kChunk);
 #pragma unroll
-    for (int q = 0; q < 4; ++q) o.vd[q] = x[(size_t)min(16 * w + 4 * lg + q, last) * p.H * DV];
-}
+        for (int kb = 0; kb < 2; ++kb)
+            if (REV ? kb >= w / 2 : kb <= w / 2) o.T[kb] = Full<E>::load8(T + (w * 2 + kb) * 512 + l * 8, kChunk * kChunk);
+    }
+    __device__ __forceinline__ void tokens(Ops &o, int c) const {
+        const size_t cidx = (size_t)bh * p.NC + c;
+        const float *gate = p.gates + cidx * kBackGateRec;
+        o.gam = *(const f32x4 *)(gate + kBackGam + 16 * w + 4 * lg);
+        o.tail = *(const f32x4 *)(gate + kBackTail + 16 * w + 4 * lg);
+        o.beta = *(const f32x4 *)(gate + kBackBeta + 16 * w + 4 * lg);
+        o.gC = gate[kBackGC];
+        if (REV) o.n0 = *(const f32x4 *)(p.N0 + cidx * (size_t)kChunk * DV + (jt * 4 + w) * 256 + l * 4);
+        const E *x = (REV ? p.dout : p.v) + row0(c) * DV + 16 * jt + li;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) o.vd[q] = x[(size_t)min(16 * w + 4 * lg + q, last(c)) * p.H * DV];
+    }
+};
 
 template <class E, int DK, int DV, bool REV>
 __device__ __forceinline__ void back_scan(const BackParams<E> &p, unsigned char *smem, int bh, int jt) {
     using L = BackScanLds<E, DK>;
+    using TR = Tr<E>;
     using WD = Full<E>;
-    constexpr int NT = DK / 64;
-    E *sH = (E *)smem, *sX = (E *)(smem + L::oX), *sY = (E *)(smem + L::oY), *sD = (E *)(smem + L::oD);
+    using wfrag = typename WD::frag;
+    constexpr int NT = DK / 64;                                   // state row tiles per wave
+    E *sH = (E *)smem, *sX = (E *)(smem + L::oX), *sY = (E *)(smem + L::oY), *sD = (E *)(smem + L::oD),
+      *sK = (E *)(smem + L::oK), *sQ = (E *)(smem + L::oQ);
     const int b = bh / p.H, h = bh - b * p.H;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, li = l & 15, lg = l >> 4;
+    const BackLoader<E, DK, DV, REV> in{p, b, h, bh, jt, w, li, lg, l};
     const float *init = REV ? p.dstate_out : p.state_in;
     const size_t sbase = (size_t)bh * DK * DV;
     const int scol = 16 * jt + li;                                // element (16 (w NT + t) + 4 lg + q, scol)
@@ -426,71 +451,89 @@ __device__ __forceinline__ void back_scan(const BackParams<E> &p, unsigned char 
 #pragma unroll
     for (int t = 0; t < NT; ++t) WD::store4(sH + li * L::LDH + 16 * (w * NT + t) + 4 * lg, L::PH, st[t]);
 
-    auto step = [&](const BackOps<E, DK, REV> &o, int c) {
+    // one chunk, c, with the loads for chunk cn
+    auto step = [&](const BackOps<E, DK, REV> &o, BackOps<E, DK, REV> &n, int c, int cn) {
         const size_t cidx = (size_t)bh * p.NC + c;
         const int ct = li * L::LDC + 16 * w + 4 * lg;             // this wave's tokens in an exchange
+        const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
         lds_barrier();
-        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        // K H (backward: K G), two chains
+        f32x4 x[2] = {zero, zero};
 #pragma unroll
         for (int kb = 0; kb < DK / 32; ++kb)
-            x = WD::ew(o.K[kb], WD::load8(sH + li * L::LDH + 32 * kb + 8 * lg, L::PH), x);
+            x[kb & 1] = WD::ew(o.K[kb], WD::load8(sH + li * L::LDH + 32 * kb + 8 * lg, L::PH), x[kb & 1]);
+        x[0] += x[1];
+        in.rows(n, cn);
         f32x4 vd;
 #pragma unroll
         for (int q = 0; q < 4; ++q) vd[q] = elem_f32(o.vd[q]);
         if constexpr (REV) {
-            WD::store4(sX + ct, L::PC, o.n0 + o.beta * o.tail * x);
+            WD::store4(sX + ct, L::PC, o.n0 + o.beta * o.tail * x[0]);
             // gam dO: rows past the sequence have no part in G
             f32x4 gd = o.gam * vd;
 #pragma unroll
             for (int q = 0; q < 4; ++q) gd[q] = c * kChunk + 16 * w + 4 * lg + q < p.T ? gd[q] : 0.f;
             WD::store4(sD + ct, L::PC, gd);
         } else {
-            WD::store4(sX + ct, L::PC, vd - o.gam * x);
+            WD::store4(sX + ct, L::PC, vd - o.gam * x[0]);
         }
-        // the state that entered this step, for stage 3
-        float *keep = (REV ? p.Gs : p.Hs) + cidx * (size_t)(DK * DV) + scol;
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) keep[(16 * (w * NT + t) + 4 * lg + q) * DV] = st[t][q];
+        for (int kb = 0; kb < DK / 32; ++kb) {
+            TR::store8(sK + (16 * w + li) * L::LDH + 32 * kb + 8 * lg, o.K[kb]);
+            if (REV) TR::store8(sQ + (16 * w + li) * L::LDH + 32 * kb + 8 * lg, o.Q[kb]);
+        }
         lds_barrier();
-        f32x4 y = {0.f, 0.f, 0.f, 0.f};
+        f32x4 y[2] = {zero, zero};
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
             if (REV ? kb >= w / 2 : kb <= w / 2)                  // T is lower triangular
-                y = WD::ww(o.T[kb], WD::load8(sX + li * L::LDC + 32 * kb + 8 * lg, L::PC), y);
-        WD::store4(sY + ct, L::PC, REV ? -o.gam * y : o.beta * o.tail * y);
-        *(f32x4 *)((REV ? p.vT : p.eT) + cidx * (size_t)(kChunk * DV) + scol * kChunk + 16 * w + 4 * lg) = y;
+                y[kb] = WD::ww(o.T[kb], WD::load8(sX + li * L::LDC + 32 * kb + 8 * lg, L::PC), y[kb]);
+        y[0] += y[1];
+        WD::store4(sY + ct, L::PC, REV ? -o.gam * y[0] : o.beta * o.tail * y[0]);
+        *(f32x4 *)((REV ? p.vT : p.eT) + cidx * (size_t)(kChunk * DV) + scol * kChunk + 16 * w + 4 * lg) = y[0];
+        in.inverse(n, cn);
+        // the state that entered this step, for stage 3
+        float *keep = (REV ? p.Gs : p.Hs) + cidx * (size_t)(DK * DV) + scol;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) st[t] *= o.gC;
-        if constexpr (REV) {
+        for (int t = 0; t < NT; ++t) {
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb) {
-                const typename WD::frag gd = WD::load8(sD + li * L::LDC + 32 * kb + 8 * lg, L::PC);
+            for (int q = 0; q < 4; ++q) keep[(16 * (w * NT + t) + 4 * lg + q) * DV] = st[t][q];
+            st[t] *= o.gC;
+        }
+        typename TR::frag kt[NT][2];
 #pragma unroll
-                for (int t = 0; t < NT; ++t) st[t] = WD::ew(o.Qt[t][kb], gd, st[t]);
+        for (int kb = 0; kb < 2; ++kb) {
+            wfrag gd;
+            if constexpr (REV) gd = WD::load8(sD + li * L::LDC + 32 * kb + 8 * lg, L::PC);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                kt[t][kb] = tr_frag<E>(sK, L::LDH, 32 * kb, 16 * (w * NT + t), false, 0, li, lg);
+                if constexpr (REV)
+                    st[t] = WD::ew(tr_frag<E>(sQ, L::LDH, 32 * kb, 16 * (w * NT + t), false, 0, li, lg), gd, st[t]);
             }
         }
         lds_barrier();
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-            const typename WD::frag u = WD::load8(sY + li * L::LDC + 32 * kb + 8 * lg, L::PC);
+            const wfrag u = WD::load8(sY + li * L::LDC + 32 * kb + 8 * lg, L::PC);
 #pragma unroll
-            for (int t = 0; t < NT; ++t) st[t] = WD::ew(o.Kt[t][kb], u, st[t]);
+            for (int t = 0; t < NT; ++t) st[t] = WD::ew(kt[t][kb], u, st[t]);
         }
+        in.tokens(n, cn);
 #pragma unroll
         for (int t = 0; t < NT; ++t) WD::store4(sH + li * L::LDH + 16 * (w * NT + t) + 4 * lg, L::PH, st[t]);
     };
-    auto chunk = [&](int i) { return REV ? p.NC - 1 - i : i; };
+    // the i-th chunk of this direction; past the last one the last one again, whose
+    // loads are then not used
+    auto chunk = [&](int i) { return REV ? max(p.NC - 1 - i, 0) : min(i, p.NC - 1); };
     BackOps<E, DK, REV> o0, o1;
-    back_load<E, DK, DV, REV>(p, o0, b, h, bh, jt, chunk(0), w, l);
+    in.rows(o0, chunk(0));
+    in.inverse(o0, chunk(0));
+    in.tokens(o0, chunk(0));
     for (int i = 0; i < p.NC; i += 2) {
-        // (the last loads are of the last chunk again, and unused)
-        back_load<E, DK, DV, REV>(p, o1, b, h, bh, jt, chunk(min(i + 1, p.NC - 1)), w, l);
-        step(o0, chunk(i));
+        step(o0, o1, chunk(i), chunk(i + 1));
         if (i + 1 == p.NC) break;
-        back_load<E, DK, DV, REV>(p, o0, b, h, bh, jt, chunk(min(i + 2, p.NC - 1)), w, l);
-        step(o1, chunk(i + 1));
+        step(o1, o0, chunk(i + 1), chunk(i + 2));
     }
     if (REV && p.dstate_in) {
 #pragma unroll
@@ -501,7 +544,8 @@ __device__ __forceinline__ void back_scan(const BackParams<E> &p, unsigned char 
 }
 
 template <class E, int DK, int DV>
-__global__ __launch_bounds__(64 * kBackScanWaves) __attribute__((amdgpu_waves_per_eu(1, 1)))
+__global__ __launch_bounds__(64 * kBackScanWaves)
+__attribute__((amdgpu_waves_per_eu(BackScanLds<E, DK>::waves_per_simd)))
 void gdn_back_scan_kernel(BackParams<E> p) {
     __shared__ __align__(16) unsigned char smem[BackScanLds<E, DK>::bytes];
     // the column tiles of a head share its operands: they get the same XCD
@@ -568,6 +612,14 @@ void gdn_back_grad_kernel(BackParams<E> p) {
     // with them meet beta = 0, dO = 0 or dV = 0
     auto rows = [&](const E *base, int r, int kb) {
         return load_frag<E>(base + (row0 + (size_t)min(r, nvalid - 1) * p.H) * DK + 32 * kb, lg);
+    };
+    // fragments of K^T and Q^T: channel ch of tokens 32 kb + 8 lg .. + 7
+    auto columns = [&](const E *base, int ch, int kb) {
+        E x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            x[e] = base[(row0 + (size_t)min(32 * kb + 8 * lg + e, nvalid - 1) * p.H) * DK + ch];
+        return __builtin_bit_cast(frag, x);
     };
     const float *ge = p.eT + cidx * (size_t)(kChunk * DV), *gv = p.vT + cidx * (size_t)(kChunk * DV);
     auto stage_part = [&](int dv0) {                               // 64 value channels into LDS
@@ -757,14 +809,13 @@ void gdn_back_grad_kernel(BackParams<E> p) {
     }
     // dQ += G1 K;  dK += G1^T Q - (G2 + G2^T) K
     {
-        const E *Kt = p.Kt + cidx * (size_t)DK * kChunk + l * 8, *Qt = p.Qt + cidx * (size_t)DK * kChunk + l * 8;
         frag kt[NK][2], qt[NK][2];
 #pragma unroll
         for (int n = 0; n < NK; ++n)
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
-                kt[n][kb] = TR::load8(Kt + ((w * NK + n) * 2 + kb) * 512);
-                qt[n][kb] = TR::load8(Qt + ((w * NK + n) * 2 + kb) * 512);
+                kt[n][kb] = columns(p.k, 16 * (NK * w + n) + li, kb);
+                qt[n][kb] = columns(p.q, 16 * (NK * w + n) + li, kb);
             }
 #pragma unroll
         for (int rt = 0; rt < 4; ++rt) {

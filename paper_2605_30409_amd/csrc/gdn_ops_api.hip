@@ -134,7 +134,7 @@ template <class E> int dispatch_norm(const gdn::NormParams<E> &p, bool grad, hip
 
 // Byte offsets of the workspace regions (the records of gdn_backward.h).
 struct BackWs {
-    size_t gates, Tf, Tt, Kt, Qt, N0, Hs, Gs, eT, vT, total;
+    size_t gates, Tf, Tt, N0, Hs, Gs, eT, vT, total;
 };
 
 BackWs back_layout(int B, int H, int T, int Dk, int Dv, size_t esz) {
@@ -151,8 +151,6 @@ BackWs back_layout(int B, int H, int T, int Dk, int Dv, size_t esz) {
     L.gates = region(4 * gdn::kBackGateRec);
     L.Tf = region(full * kChunk * kChunk);
     L.Tt = region(full * kChunk * kChunk);
-    L.Kt = region(esz * Dk * kChunk);
-    L.Qt = region(esz * Dk * kChunk);
     L.N0 = region(4 * kChunk * Dv);
     L.Hs = region(4 * (size_t)Dk * Dv);
     L.Gs = region(4 * (size_t)Dk * Dv);
@@ -256,8 +254,6 @@ int gdn_chunk_backward(const void *q, const void *k, const void *v, const float 
         p.N0 = (float *)(base + L.N0);
         p.Tf = (E *)(base + L.Tf);
         p.Tt = (E *)(base + L.Tt);
-        p.Kt = (E *)(base + L.Kt);
-        p.Qt = (E *)(base + L.Qt);
         p.Hs = (float *)(base + L.Hs);
         p.Gs = (float *)(base + L.Gs);
         p.eT = (float *)(base + L.eT);
