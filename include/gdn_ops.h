@@ -69,7 +69,7 @@ int gdn_step_forward(const void *q, const void *k, const void *v, const float *a
  * Outputs may not overlap inputs or each other, except dstate_in == dstate_out.
  * `ws`: caller-owned device buffer, 256-byte aligned, of at least
  * gdn_chunk_backward_workspace_bytes(...) bytes (0 for arguments that the call
- * refuses; 274 KB a chunk and head at Dk = Dv = 128).  Calls that run at once need
+ * refuses; 338 KB a chunk and head at Dk = Dv = 128).  Calls that run at once need
  * one each.
  */
 size_t gdn_chunk_backward_workspace_bytes(int B, int H, int T, int Dk, int Dv, int chunk, int is_bf16);

@@ -132,21 +132,71 @@ template <int P> struct Wide<float, P> {
     static __device__ __forceinline__ f32x4 ww(frag a, frag b, f32x4 c) { return T::mma(a, b, c); }
     static __device__ __forceinline__ frag rounded(frag f) { return f; }
 };
+// One contraction block of R = 32 or 16 state rows per wave: an input's operand (R / 4
+// consecutive k per lane) and the state's accumulator tiles as the other one in planes.
+template <class E, int R> struct RowBlock;
+template <class E> struct RowBlock<E, 32> {            // tiles in P32 order
+    using in = typename Tr<E>::frag;
+    using planes = typename Wide<E, 3>::frag;
+    static __device__ __forceinline__ planes split(const f32x4 *st) { return Wide<E, 3>::split(st[0], st[1]); }
+    static __device__ __forceinline__ f32x4 product(const planes &a, in b) {
+        return Wide<E, 3>::we(a, b, f32x4{0.f, 0.f, 0.f, 0.f});
+    }
+};
+template <> struct RowBlock<uint16_t, 16> {
+    using T = Tr<uint16_t>;
+    using in = u32x2;
+    struct planes {
+        u32x2 pl[3];
+    };
+    static __device__ __forceinline__ planes split(const f32x4 *st) {
+        planes f;
+        f32x4 x = st[0];
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            f.pl[i] = T::from_f32(x);
+            x -= T::to_f32(f.pl[i]);
+        }
+        return f;
+    }
+    static __device__ __forceinline__ f32x4 product(const planes &a, in b) {
+        f32x4 c = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 2; i >= 0; --i)
+            c = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(i16x4, a.pl[i]), __builtin_bit_cast(i16x4, b), c, 0, 0, 0);
+        return c;
+    }
+};
+template <> struct RowBlock<float, 16> {
+    using in = f32x4;
+    using planes = f32x4;
+    static __device__ __forceinline__ planes split(const f32x4 *st) { return st[0]; }
+    static __device__ __forceinline__ f32x4 product(const planes &a, in b) {
+        f32x4 c = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) c = mma_f32_k4(a[i], b[i], c);
+        return c;
+    }
+};
+
 template <class E> using Full = Wide<E, 3>;    // fp32's mantissa
 template <class E> using Half = Wide<E, 2>;    // 16 bits of it
 
 __device__ __forceinline__ float elem_f32(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
 __device__ __forceinline__ float elem_f32(float x) { return x; }
 
-// Gate record of a chunk, in floats: g as 64 doubles, gam, tail and beta, e^{g_C}.
-constexpr int kBackGam = 128, kBackTail = 192, kBackBeta = 256, kBackGC = 320, kBackGateRec = 336;
+// Gate record of a chunk, in floats: g as 64 doubles, tail, beta; then, what the scans take,
+// gam, beta tail and e^{g_C}.
+constexpr int kBackTail = 128, kBackBeta = 192, kBackGam = 256, kBackBt = 320, kBackGC = 384, kBackGateRec = 400;
+constexpr int kBackScanGates = 132;    // floats of it from kBackGam on that the scans copy
 
 // Workspace records per (b*H + h, chunk); "planes": three of bf16, each behind the
 // whole of the one before, on the bf16 path, fp32 on the other.
-//   gates [336] fp32
+//   gates [400] fp32
 //   Tf, Tt  64 x 64   planes, fragments [4 row tile][2 k block][64 lane][8] of T and T^T (those
 //                     that are all zeros are neither written nor read)
-//   N0      64 x Dv   fp32, beta A^T dO as accumulator tiles [Dv/16][4][64 lane][4]
+//   N0      64 x Dv   fp32, beta A^T dO as transposed accumulator tiles [Dv/16][4 token tile][64 lane][4]
+//   C0      Dk x Dv   fp32, Q^T gam dO as accumulator tiles [Dv/16][4 wave][Dk/64][64 lane][4]
 //   Hs, Gs  Dk x Dv   fp32, row-major: H and G of the chunk
 //   eT, vT  Dv x 64   fp32, row-major: e^T and dV^T
 template <class E> struct BackParams {
@@ -155,7 +205,7 @@ template <class E> struct BackParams {
     E *dq, *dk, *dv;
     float *dalpha, *dbeta, *dstate_in;
     int B, H, T, NC;
-    float *gates, *N0, *Hs, *Gs, *eT, *vT;
+    float *gates, *N0, *C0, *Hs, *Gs, *eT, *vT;
     E *Tf, *Tt;
 };
 
@@ -167,17 +217,17 @@ template <class E> constexpr int lds_ld(int n) { return n + 16 / (int)sizeof(E);
 // --------------------------------------------------------------------------
 // Stage 1, per chunk and head: gates, T, and the operands of the scans.
 // --------------------------------------------------------------------------
-// LDS: K rows, Q rows (dO takes their place once A is formed), N below the diagonal and T^T
+// LDS: K rows (dO takes their place once N and A are formed), Q rows, N below the diagonal and T^T
 // on and above it in one fp32 square, A^T: 80.6 KB on the bf16 path at D = 128, two
 // workgroups a CU.
 template <class E, int DK, int DV> struct PrepLds {
     static constexpr int LDK = lds_ld<E>(DK), LDV = lds_ld<E>(DV), LDA = kChunk + 4, LDT = lds_ld<E>(kChunk);
-    static constexpr size_t oK = 0;
-    static constexpr size_t oQ = oK + sizeof(E) * kChunk * LDK;    // Q, then dO
-    static constexpr size_t oN = oQ + sizeof(E) * kChunk * (LDK > LDV ? LDK : LDV);
+    static constexpr size_t oK = 0;                                // K, then dO
+    static constexpr size_t oQ = oK + sizeof(E) * kChunk * (LDK > LDV ? LDK : LDV);
+    static constexpr size_t oN = oQ + sizeof(E) * kChunk * LDK;
     static constexpr size_t oA = oN + 4 * kChunk * LDA;            // A^T, planes
     static constexpr size_t oG = oA + sizeof(E) * Full<E>::planes * kChunk * LDT;
-    static constexpr size_t bytes = oG + 8 * kChunk + 4 * kChunk;
+    static constexpr size_t bytes = oG + 8 * kChunk + 2 * 4 * kChunk;
     // waves per SIMD of the eight-wave workgroups that fit a CU
     static constexpr int waves_per_simd = bytes * 2 <= 160 * 1024 ? 4 : 2;
 };
@@ -222,10 +272,10 @@ void gdn_back_prep_kernel(BackParams<E> p) {
     constexpr int NT = 64 * kPrepWaves;
     constexpr int PA = kChunk * L::LDT;      // plane of A^T
     extern __shared__ __align__(16) unsigned char smem[];
-    E *sK = (E *)(smem + L::oK), *sQ = (E *)(smem + L::oQ), *sO = sQ, *sA = (E *)(smem + L::oA);
+    E *sK = (E *)(smem + L::oK), *sQ = (E *)(smem + L::oQ), *sO = sK, *sA = (E *)(smem + L::oA);
     float *sN = (float *)(smem + L::oN);     // N[r][c] at [r][c] (c < r), T[r][c] at [c][r] (c <= r)
     double *sg = (double *)(smem + L::oG);
-    float *sb = (float *)(sg + kChunk);
+    float *sb = (float *)(sg + kChunk), *sgam = sb + kChunk;
     const int c = blockIdx.x / (p.B * p.H), bh = blockIdx.x - c * (p.B * p.H);
     const int b = bh / p.H, h = bh - b * p.H;
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, li = l & 15, lg = l >> 4;
@@ -257,9 +307,12 @@ void gdn_back_prep_kernel(BackParams<E> p) {
         sg[l] = g;
         sb[l] = be;
         ((double *)gate)[l] = g;
-        gate[kBackGam + l] = expf((float)g);
-        gate[kBackTail + l] = expf((float)(gC - g));
+        const float gam = expf((float)g), tail = expf((float)(gC - g));
+        sgam[l] = gam;
+        gate[kBackGam + l] = gam;
+        gate[kBackTail + l] = tail;
         gate[kBackBeta + l] = be;
+        gate[kBackBt + l] = be * tail;
         if (l == 0) gate[kBackGC] = expf((float)gC);
     }
     kr.store(sK, L::LDK, nvalid, tid);
@@ -316,10 +369,29 @@ void gdn_back_prep_kernel(BackParams<E> p) {
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb)
                 if (kb >= rt / 2)                        // rows i >= j only
-                    acc = WD::we(WD::load8(sA + (16 * rt + li) * L::LDT + 32 * kb + 8 * lg, PA),
-                                 tr_frag<E>(sO, L::LDV, 32 * kb, 16 * jt, false, 0, li, lg), acc);
-            const f32x4 bq = *(const f32x4 *)(sb + 16 * rt + 4 * lg);
-            *(f32x4 *)(N0 + (size_t)(jt * 4 + rt) * 256 + l * 4) = acc * bq;
+                    acc = WD::ew(tr_frag<E>(sO, L::LDV, 32 * kb, 16 * jt, false, 0, li, lg),
+                                 WD::load8(sA + (16 * rt + li) * L::LDT + 32 * kb + 8 * lg, PA), acc);
+            *(f32x4 *)(N0 + (jt * 4 + rt) * 256 + l * 4) = acc * sb[16 * rt + li];
+        }
+    }
+    // Q^T gam dO: a column tile and every second (or each) row tile per wave
+    {
+        constexpr int NK = DK / 64, NJ = DV / 16, PER = kPrepWaves / NJ;
+        float *C0 = p.C0 + cidx * (size_t)(DK * DV);
+        const int jt = w / PER;
+        typename WD::frag gd[2];
+#pragma unroll
+        for (int kb = 0; kb < 2; ++kb) {
+            const typename TR::frag o = tr_frag<E>(sO, L::LDV, 32 * kb, 16 * jt, false, 0, li, lg);
+            const float *gm = sgam + 32 * kb + 8 * lg;
+            gd[kb] = WD::split(TR::to_f32(TR::lo(o)) * *(const f32x4 *)gm, TR::to_f32(TR::hi(o)) * *(const f32x4 *)(gm + 4));
+        }
+        for (int t = w % PER; t < 4 * NK; t += PER) {    // tile a = t % NK of scan wave t / NK
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+                acc = WD::ew(tr_frag<E>(sQ, L::LDK, 32 * kb, 16 * NK * (t / NK), NK == 2, t % NK, li, lg), gd[kb], acc);
+            *(f32x4 *)(C0 + (jt * 4 * NK + t) * 256 + l * 4) = acc;
         }
     }
     lds_barrier();
@@ -357,203 +429,280 @@ void gdn_back_prep_kernel(BackParams<E> p) {
 }
 
 // --------------------------------------------------------------------------
-// Stage 2: the scans.  A workgroup of four waves carries 16 columns of one
-// state through the chunks: blockIdx.y = 0 the states forward, 1 their gradients
-// backward.  Each product's rows are split over the waves, and its result goes
-// to all of them through LDS (as [column][row], so a result tile is stored in
-// quads and read back as operand rows).  A chunk's operands are loaded one chunk
-// ahead, as they are: nothing is computed from a load, and none is under a
-// condition, where it is issued, so that none is waited for there.  Rows past the
-// end of the sequence are read as its last row: their beta is 0, and so is
-// their part in the states and in dV.
+// Stage 2: the scans.  A workgroup carries 16 columns of one state through the
+// chunks: blockIdx.y = 0 the states forward, 1 their gradients backward.  With X the
+// state and first, before, after, add as in the table, a chunk is
+//   y = T (first + before K X),   X <- e^{g_C} X + add + K^T (after y)
+//                 T    first   before       after       add
+//   forward       T    V       -gam         beta tail   -            y = e
+//   backward      T^T  N0      beta tail    -gam        C0           y = dV
+// Four compute waves; wave w holds rows R w .. R w + R - 1 of the state, R = Dk / 4 (32 of
+// them in P32 order), so that its planes are a product's operand as they stand.  A
+// chunk takes three exchanges through LDS, each ended by a barrier:
+//   1  every wave multiplies its rows into K X for all 64 tokens; wave r adds up the
+//      partial sums of token tile r and forms T's operand there;
+//   2  wave r forms rows 16 r .. of y;
+//   3  every wave adds K^T (after y) to its rows.
+// Two loader waves bring K, first, add and the gates of a chunk into a ring of three
+// slots by asynchronous copies, two chunks ahead, a share of them in each phase (a wave
+// needs some 50 cycles to issue one, and compute waves that load for themselves were
+// held up by that: 2.5 us a chunk); T, which is no LDS operand, goes to registers one
+// chunk ahead.  No load of the compute waves is under a condition: a wait
+// behind a branch that may have loaded waits for everything.  Rows past the end
+// of the sequence are read as its last row: their beta is 0, and so is their part in
+// the states and in dV.
 // --------------------------------------------------------------------------
-constexpr int kBackScanWaves = 4;
+constexpr int kBackScanWaves = 4, kBackLoadWaves = 2;
 
 template <class E, int DK> struct BackScanLds {
-    static constexpr int LDH = lds_ld<E>(DK), LDC = lds_ld<E>(kChunk);
-    static constexpr int PH = 16 * LDH, PC = 16 * LDC;                        // planes
-    static constexpr size_t szC = sizeof(E) * Full<E>::planes * PC, szR = sizeof(E) * kChunk * LDH;
-    static constexpr size_t oX = sizeof(E) * Full<E>::planes * PH;            // T's operand
-    static constexpr size_t oY = oX + szC;                                    // T's result, scaled
-    static constexpr size_t oD = oY + szC;                                    // gam dO (backward)
-    static constexpr size_t oK = oD + szC;                                    // K rows
-    static constexpr size_t oQ = oK + szR;                                    // Q rows (backward)
-    static constexpr size_t bytes = oQ + szR;
-    // workgroups that fit a CU
-    static constexpr int fit = (int)(160 * 1024 / bytes), waves_per_simd = fit > 3 ? 3 : fit;
+    static constexpr int R = DK / 4, NK = R / 16;                             // state rows and row tiles per wave
+    static constexpr int LDC = lds_ld<E>(kChunk);
+    static constexpr int PT = 16 * kChunk, PC = 16 * LDC;                     // planes
+    static constexpr int szK = (int)sizeof(E) * kChunk * DK, szF = 4096, szA = 4096 * NK;
+    static constexpr int oF = szK, oA = oF + szF, oG = oA + szA;              // in a slot: K, first, add, gates
+    static constexpr int SLOT = oG + 4 * kBackScanGates + 16, DEPTH = 3;
+    static constexpr int oP = DEPTH * SLOT;                                   // partial sums of K X
+    static constexpr int oX = oP + 4 * 4 * 4 * 256;                           // T's operand, [token][column]
+    static constexpr int oY = oX + (int)sizeof(E) * Full<E>::planes * PT;     // after y, [column][token]
+    static constexpr size_t bytes = oY + sizeof(E) * Full<E>::planes * PC;
+    static constexpr int threads = 64 * (kBackScanWaves + kBackLoadWaves);
+    // waves per SIMD of the workgroups that share a CU
+    static constexpr int waves_per_simd = bytes * 2 <= 160 * 1024 ? 3 : 2;
+    static_assert(SLOT % 16 == 0 && bytes <= 160 * 1024, "the ring fits the LDS");
 };
 
-// Operands of one chunk, loaded one chunk ahead of their use, in three parts that
-// are issued in the three phases of the chunk before: together they would hold up
-// its first product by the time the loads take to issue (64 bytes a cycle and CU).
-template <class E, int DK, bool REV> struct BackOps {
-    typename Tr<E>::frag K[DK / 32], Q[REV ? DK / 32 : 1];    // rows of row tile w
-    typename Full<E>::frag T[2];
-    E vd[4];                                            // V or dO of four tokens
-    f32x4 n0, gam, tail, beta;
-    float gC;
-};
-
-template <class E, int DK, int DV, bool REV> struct BackLoader {
-    const BackParams<E> &p;
-    int b, h, bh, jt, w, li, lg, l;
-    using Ops = BackOps<E, DK, REV>;
-    __device__ __forceinline__ size_t row0(int c) const { return ((size_t)b * p.T + c * kChunk) * p.H + h; }
-    __device__ __forceinline__ int last(int c) const { return min(kChunk, p.T - c * kChunk) - 1; }
-    __device__ __forceinline__ void rows(Ops &o, int c) const {
-        const size_t at = (row0(c) + (size_t)min(16 * w + li, last(c)) * p.H) * DK;
+// K rows in the ring: a row's 16-byte granules are permuted, granule g stored at g ^ kperm(r), so
+// that the 16 rows of an operand read (one granule each) and the 4 rows of a transposing
+// read (4 granules each) take different banks.
+template <class E, int DK> __device__ __forceinline__ int kperm(int r) {
+    if constexpr (sizeof(E) == 4) return r & 15;
+    else if constexpr (DK == 128) return 4 * (r & 3) + ((r >> 2) & 3);
+    else return 2 * ((r >> 1) & 3);
+}
+template <class E, int DK> __device__ __forceinline__ const E *kaddr(const E *K, int row, int col) {
+    constexpr int VE = 16 / (int)sizeof(E);
+    return K + row * DK + ((col / VE) ^ kperm<E, DK>(row)) * VE + col % VE;
+}
+// R / 4 consecutive channels of a row
+template <class E, int DK, int R> __device__ __forceinline__ typename RowBlock<E, R>::in krow(const E *K, int row, int col) {
+    if constexpr (sizeof(E) == 4 && R == 32)
+        return Tr<E>::cat(*(const f32x4 *)kaddr<E, DK>(K, row, col), *(const f32x4 *)kaddr<E, DK>(K, row, col + 4));
+    else
+        return *(const typename RowBlock<E, R>::in *)kaddr<E, DK>(K, row, col);
+}
+// tr_frag through the permutation
+template <class E, int DK, int NK>
+__device__ __forceinline__ typename Tr<E>::frag kcols(const E *K, int row0, int colbase, int a, int li, int lg) {
+    if constexpr (sizeof(E) == 2) {
+        typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+        const int row = row0 + 8 * lg + (li >> 2);
+        const int col = NK == 2 ? colbase + 8 * (li & 3) + 4 * a : colbase + 4 * (li & 3);
+        const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)kaddr<E, DK>(K, row, col));
+        const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)kaddr<E, DK>(K, row + 4, col));
+        return Tr<E>::cat(__builtin_bit_cast(u32x2, lo), __builtin_bit_cast(u32x2, hi));
+    } else {
+        const int col = NK == 2 ? colbase + p32_row(a, li) : colbase + li;
+        typename Tr<E>::frag f;
 #pragma unroll
-        for (int kb = 0; kb < DK / 32; ++kb) {
-            o.K[kb] = load_frag<E>(p.k + at + 32 * kb, lg);
-            if (REV) o.Q[kb] = load_frag<E>(p.q + at + 32 * kb, lg);
+        for (int q = 0; q < 8; ++q) f[q] = *kaddr<E, DK>(K, row0 + 8 * lg + q, col);
+        return f;
+    }
+}
+
+// The loader waves (part = 0, 1).
+template <class E, int DK, int DV, bool REV>
+__device__ __forceinline__ void back_loader(const BackParams<E> &p, unsigned char *smem, int bh, int jt, int part, int l) {
+    using L = BackScanLds<E, DK>;
+    constexpr int sz = (int)sizeof(E), GPR = DK * sz / 16, RPC = 64 / GPR;   // granules per K row, rows per copy
+    constexpr int NKC = L::szK / 2048;                                       // copies of K per wave
+    constexpr int GPV = sz, RPV = 64 / GPV;                                  // granules per row of 16 columns of V
+    constexpr int NF = REV ? 2 : sz / 2, NA = REV ? L::szA / 2048 : 0;       // of first and add per wave
+    constexpr int ALL = NKC + NF + NA + 1;
+    const int b = bh / p.H, h = bh - b * p.H;
+    const size_t head = (size_t)b * p.T * p.H + h;
+    typedef __attribute__((address_space(3))) void lds_void;
+    auto copy = [](const void *src, unsigned char *dst) { __builtin_amdgcn_global_load_lds(src, (lds_void *)dst, 16, 0, 0); };
+    // chunks in the order of this direction; past the last one the last one again
+    auto chunk = [&](int i) { return REV ? max(p.NC - 1 - i, 0) : min(i, p.NC - 1); };
+    auto rows = [&](int i, int n0, int n1) {                                 // copies n0 .. n1 - 1 of K
+        const int c = chunk(i), last = min(kChunk, p.T - c * kChunk) - 1;
+        const E *k = p.k + (head + (size_t)c * kChunk * p.H) * DK;
+        unsigned char *slot = smem + i % L::DEPTH * L::SLOT;
+#pragma unroll
+        for (int n = n0; n < n1; ++n) {
+            const int r = RPC * (2 * n + part) + l / GPR, g = (l % GPR) ^ kperm<E, DK>(r);
+            copy(k + (size_t)min(r, last) * p.H * DK + g * (16 / sz), slot + 1024 * (2 * n + part));
         }
-    }
-    __device__ __forceinline__ void inverse(Ops &o, int c) const {
-        const E *T = (REV ? p.Tt : p.Tf) + ((size_t)bh * p.NC + c) * (size_t)full_elems<E>(kChunk * kChunk);
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-            if (REV ? kb >= w / 2 : kb <= w / 2) o.T[kb] = Full<E>::load8(T + (w * 2 + kb) * 512 + l * 8, kChunk * kChunk);
-    }
-    __device__ __forceinline__ void tokens(Ops &o, int c) const {
+    };
+    auto rest = [&](int i) {
+        const int c = chunk(i), last = min(kChunk, p.T - c * kChunk) - 1;
         const size_t cidx = (size_t)bh * p.NC + c;
-        const float *gate = p.gates + cidx * kBackGateRec;
-        o.gam = *(const f32x4 *)(gate + kBackGam + 16 * w + 4 * lg);
-        o.tail = *(const f32x4 *)(gate + kBackTail + 16 * w + 4 * lg);
-        o.beta = *(const f32x4 *)(gate + kBackBeta + 16 * w + 4 * lg);
-        o.gC = gate[kBackGC];
-        if (REV) o.n0 = *(const f32x4 *)(p.N0 + cidx * (size_t)kChunk * DV + (jt * 4 + w) * 256 + l * 4);
-        const E *x = (REV ? p.dout : p.v) + row0(c) * DV + 16 * jt + li;
+        unsigned char *slot = smem + i % L::DEPTH * L::SLOT;
+        if constexpr (REV) {
+            const float *n0 = p.N0 + cidx * (size_t)(kChunk * DV) + jt * 1024 + l * 4;
+            const float *c0 = p.C0 + cidx * (size_t)(DK * DV) + jt * (1024 * L::NK) + l * 4;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) o.vd[q] = x[(size_t)min(16 * w + 4 * lg + q, last(c)) * p.H * DV];
+            for (int n = 0; n < NF; ++n) copy(n0 + 256 * (2 * n + part), slot + L::oF + 1024 * (2 * n + part));
+#pragma unroll
+            for (int n = 0; n < NA; ++n) copy(c0 + 256 * (2 * n + part), slot + L::oA + 1024 * (2 * n + part));
+        } else {
+            const E *v = p.v + (head + (size_t)c * kChunk * p.H) * DV + 16 * jt;
+#pragma unroll
+            for (int n = 0; n < NF; ++n) {
+                const int r = RPV * (2 * n + part) + l / GPV;
+                copy(v + (size_t)min(r, last) * p.H * DV + l % GPV * (16 / sz), slot + L::oF + 1024 * (2 * n + part));
+            }
+        }
+        // (by both waves, so that their counts agree)
+        if (l < kBackScanGates / 4) copy(p.gates + cidx * kBackGateRec + kBackGam + 4 * l, slot + L::oG);
+    };
+    rows(0, 0, NKC);
+    rest(0);
+    rows(1, 0, NKC);
+    rest(1);
+    wait_vmcnt<ALL>();
+    lds_only_barrier();                                // chunk 0 is there
+    for (int i = 0; i < p.NC; ++i) {
+        // slot of chunk i + 2: that of chunk i - 1, which no wave reads any more
+        rows(i + 2, 0, NKC / 2);
+        lds_only_barrier();
+        rows(i + 2, NKC / 2, NKC);
+        lds_only_barrier();
+        rest(i + 2);
+        wait_vmcnt<ALL>();                             // chunk i + 1 is there
+        lds_only_barrier();
     }
-};
+    wait_vmcnt<0>();
+}
 
 template <class E, int DK, int DV, bool REV>
-__device__ __forceinline__ void back_scan(const BackParams<E> &p, unsigned char *smem, int bh, int jt) {
+__device__ __forceinline__ void back_scan(const BackParams<E> &p, unsigned char *smem, int bh, int jt, int w, int l) {
     using L = BackScanLds<E, DK>;
     using TR = Tr<E>;
     using WD = Full<E>;
     using wfrag = typename WD::frag;
-    constexpr int NT = DK / 64;                                   // state row tiles per wave
-    E *sH = (E *)smem, *sX = (E *)(smem + L::oX), *sY = (E *)(smem + L::oY), *sD = (E *)(smem + L::oD),
-      *sK = (E *)(smem + L::oK), *sQ = (E *)(smem + L::oQ);
-    const int b = bh / p.H, h = bh - b * p.H;
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, li = l & 15, lg = l >> 4;
-    const BackLoader<E, DK, DV, REV> in{p, b, h, bh, jt, w, li, lg, l};
+    constexpr int R = L::R, NK = L::NK;
+    using RB = RowBlock<E, R>;
+    struct Inverse {
+        wfrag T[2];
+    };
+    const int li = l & 15, lg = l >> 4;
+    float *sP = (float *)(smem + L::oP);                          // [wave][token tile][lane][4]
+    E *sX = (E *)(smem + L::oX), *sY = (E *)(smem + L::oY);
     const float *init = REV ? p.dstate_out : p.state_in;
+    // element (R w + R / 4 lg + 4 a + q, 16 jt + li) is st[a][q]
     const size_t sbase = (size_t)bh * DK * DV;
-    const int scol = 16 * jt + li;                                // element (16 (w NT + t) + 4 lg + q, scol)
-    f32x4 st[NT];
+    const unsigned soff = (R * w + R / 4 * lg) * DV + 16 * jt + li;
+    f32x4 st[NK];
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
+    for (int a = 0; a < NK; ++a)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) st[t][q] = init ? init[sbase + (16 * (w * NT + t) + 4 * lg + q) * DV + scol] : 0.f;
+        for (int q = 0; q < 4; ++q) st[a][q] = init ? init[sbase + soff + (4 * a + q) * DV] : 0.f;
+    auto chunk = [&](int i) { return REV ? max(p.NC - 1 - i, 0) : min(i, p.NC - 1); };
+    // (the zero blocks of T too, which nothing has written and nothing uses)
+    auto load = [&](Inverse &o, int c) {
+        const E *T = (REV ? p.Tt : p.Tf) + ((size_t)bh * p.NC + c) * (size_t)full_elems<E>(kChunk * kChunk);
 #pragma unroll
-    for (int t = 0; t < NT; ++t) WD::store4(sH + li * L::LDH + 16 * (w * NT + t) + 4 * lg, L::PH, st[t]);
-
-    // one chunk, c, with the loads for chunk cn
-    auto step = [&](const BackOps<E, DK, REV> &o, BackOps<E, DK, REV> &n, int c, int cn) {
-        const size_t cidx = (size_t)bh * p.NC + c;
-        const int ct = li * L::LDC + 16 * w + 4 * lg;             // this wave's tokens in an exchange
+        for (int kb = 0; kb < 2; ++kb) o.T[kb] = WD::load8(T + (unsigned)((w * 2 + kb) * 512 + l * 8), kChunk * kChunk);
+    };
+    // the i-th chunk of this direction
+    auto step = [&](const Inverse &o, Inverse &n, int i) {
+        const size_t cidx = (size_t)bh * p.NC + chunk(i);
         const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
-        lds_barrier();
-        // K H (backward: K G), two chains
-        f32x4 x[2] = {zero, zero};
+        const unsigned char *slot = smem + i % L::DEPTH * L::SLOT;
+        const E *K = (const E *)slot;
+        const float *gate = (const float *)(slot + L::oG) - kBackGam;
+        // K X transposed, [column][token]
+        typename RB::in k[4];
 #pragma unroll
-        for (int kb = 0; kb < DK / 32; ++kb)
-            x[kb & 1] = WD::ew(o.K[kb], WD::load8(sH + li * L::LDH + 32 * kb + 8 * lg, L::PH), x[kb & 1]);
-        x[0] += x[1];
-        in.rows(n, cn);
-        f32x4 vd;
+        for (int rt = 0; rt < 4; ++rt) k[rt] = krow<E, DK, R>(K, 16 * rt + li, R * w + R / 4 * lg);
+        {
+            const typename RB::planes H = RB::split(st);
+            f32x4 part[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) vd[q] = elem_f32(o.vd[q]);
-        if constexpr (REV) {
-            WD::store4(sX + ct, L::PC, o.n0 + o.beta * o.tail * x[0]);
-            // gam dO: rows past the sequence have no part in G
-            f32x4 gd = o.gam * vd;
+            for (int rt = 0; rt < 4; ++rt) part[rt] = RB::product(H, k[rt]);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) gd[q] = c * kChunk + 16 * w + 4 * lg + q < p.T ? gd[q] : 0.f;
-            WD::store4(sD + ct, L::PC, gd);
-        } else {
-            WD::store4(sX + ct, L::PC, vd - o.gam * x[0]);
+            for (int rt = 0; rt < 4; ++rt) *(f32x4 *)(sP + (w * 4 + rt) * 256 + l * 4) = part[rt];
         }
+        f32x4 first;
+        if constexpr (REV) first = *(const f32x4 *)(slot + L::oF + (w * 64 + l) * 16);
+        else first = TR::to_f32(TR::load((const E *)(slot + L::oF) + (16 * w + li) * 16 + 4 * lg));
+        const float before = REV ? gate[kBackBt + 16 * w + li] : -gate[kBackGam + 16 * w + li];
+        lds_only_barrier();
+        f32x4 x = zero;
 #pragma unroll
-        for (int kb = 0; kb < DK / 32; ++kb) {
-            TR::store8(sK + (16 * w + li) * L::LDH + 32 * kb + 8 * lg, o.K[kb]);
-            if (REV) TR::store8(sQ + (16 * w + li) * L::LDH + 32 * kb + 8 * lg, o.Q[kb]);
-        }
-        lds_barrier();
+        for (int j = 0; j < 4; ++j) x += *(const f32x4 *)(sP + (j * 4 + w) * 256 + l * 4);
+        WD::store4(sX + (16 * w + li) * 16 + 4 * lg, L::PT, first + before * x);
+        load(n, chunk(i + 1));
+        typename TR::frag kt[NK][2];
+#pragma unroll
+        for (int a = 0; a < NK; ++a)
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) kt[a][kb] = kcols<E, DK, NK>(K, 32 * kb, R * w, a, li, lg);
+        const f32x4 after = REV ? -*(const f32x4 *)(gate + kBackGam + 16 * w + 4 * lg) : *(const f32x4 *)(gate + kBackBt + 16 * w + 4 * lg);
+        const float gC = gate[kBackGC];
+        lds_only_barrier();
         f32x4 y[2] = {zero, zero};
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
             if (REV ? kb >= w / 2 : kb <= w / 2)                  // T is lower triangular
-                y[kb] = WD::ww(o.T[kb], WD::load8(sX + li * L::LDC + 32 * kb + 8 * lg, L::PC), y[kb]);
+                y[kb] = WD::ww(o.T[kb], WD::tr(sX, L::PT, 16, 32 * kb, 0, li, lg), y[kb]);
         y[0] += y[1];
-        WD::store4(sY + ct, L::PC, REV ? -o.gam * y[0] : o.beta * o.tail * y[0]);
-        *(f32x4 *)((REV ? p.vT : p.eT) + cidx * (size_t)(kChunk * DV) + scol * kChunk + 16 * w + 4 * lg) = y[0];
-        in.inverse(n, cn);
-        // the state that entered this step, for stage 3
-        float *keep = (REV ? p.Gs : p.Hs) + cidx * (size_t)(DK * DV) + scol;
+        WD::store4(sY + li * L::LDC + 16 * w + 4 * lg, L::PC, after * y[0]);
+        *(f32x4 *)((REV ? p.vT : p.eT) + cidx * (size_t)(kChunk * DV) + (unsigned)((16 * jt + li) * kChunk + 16 * w + 4 * lg)) = y[0];
+        // the state that entered this chunk, for stage 3
+        float *keep = (REV ? p.Gs : p.Hs) + cidx * (size_t)(DK * DV);
 #pragma unroll
-        for (int t = 0; t < NT; ++t) {
+        for (int a = 0; a < NK; ++a) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) keep[(16 * (w * NT + t) + 4 * lg + q) * DV] = st[t][q];
-            st[t] *= o.gC;
+            for (int q = 0; q < 4; ++q) keep[soff + (4 * a + q) * DV] = st[a][q];
+            st[a] *= gC;
+            if constexpr (REV) st[a] += *(const f32x4 *)(slot + L::oA + ((w * NK + a) * 64 + l) * 16);
         }
-        typename TR::frag kt[NT][2];
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-            wfrag gd;
-            if constexpr (REV) gd = WD::load8(sD + li * L::LDC + 32 * kb + 8 * lg, L::PC);
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                kt[t][kb] = tr_frag<E>(sK, L::LDH, 32 * kb, 16 * (w * NT + t), false, 0, li, lg);
-                if constexpr (REV)
-                    st[t] = WD::ew(tr_frag<E>(sQ, L::LDH, 32 * kb, 16 * (w * NT + t), false, 0, li, lg), gd, st[t]);
-            }
-        }
-        lds_barrier();
+        lds_only_barrier();
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
             const wfrag u = WD::load8(sY + li * L::LDC + 32 * kb + 8 * lg, L::PC);
 #pragma unroll
-            for (int t = 0; t < NT; ++t) st[t] = WD::ew(kt[t][kb], u, st[t]);
+            for (int a = 0; a < NK; ++a) st[a] = WD::ew(kt[a][kb], u, st[a]);
         }
-        in.tokens(n, cn);
-#pragma unroll
-        for (int t = 0; t < NT; ++t) WD::store4(sH + li * L::LDH + 16 * (w * NT + t) + 4 * lg, L::PH, st[t]);
     };
-    // the i-th chunk of this direction; past the last one the last one again, whose
-    // loads are then not used
-    auto chunk = [&](int i) { return REV ? max(p.NC - 1 - i, 0) : min(i, p.NC - 1); };
-    BackOps<E, DK, REV> o0, o1;
-    in.rows(o0, chunk(0));
-    in.inverse(o0, chunk(0));
-    in.tokens(o0, chunk(0));
+    Inverse o0, o1;
+    load(o0, chunk(0));
+    // (vmcnt(0): loads pending from before the loop would be taken for pending at
+    // the start of every turn, and the waits there for all loads of the turn before)
+    __builtin_amdgcn_s_waitcnt(0x0f70);
+    lds_only_barrier();
     for (int i = 0; i < p.NC; i += 2) {
-        step(o0, o1, chunk(i), chunk(i + 1));
+        step(o0, o1, i);
         if (i + 1 == p.NC) break;
-        step(o1, o0, chunk(i + 1), chunk(i + 2));
+        step(o1, o0, i + 1);
     }
     if (REV && p.dstate_in) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
+        for (int a = 0; a < NK; ++a)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) p.dstate_in[sbase + (16 * (w * NT + t) + 4 * lg + q) * DV + scol] = st[t][q];
+            for (int q = 0; q < 4; ++q) p.dstate_in[sbase + soff + (4 * a + q) * DV] = st[a][q];
     }
 }
 
 template <class E, int DK, int DV>
-__global__ __launch_bounds__(64 * kBackScanWaves)
+__global__ __launch_bounds__((BackScanLds<E, DK>::threads))
 __attribute__((amdgpu_waves_per_eu(BackScanLds<E, DK>::waves_per_simd)))
 void gdn_back_scan_kernel(BackParams<E> p) {
-    __shared__ __align__(16) unsigned char smem[BackScanLds<E, DK>::bytes];
+    extern __shared__ __align__(16) unsigned char smem[];
     // the column tiles of a head share its operands: they get the same XCD
     constexpr int NJ = DV / 16;
     const int u = blockIdx.x >> 3, jt = u % NJ, bh = (u / NJ) * 8 + (blockIdx.x & 7);
     if (bh >= p.B * p.H) return;
-    if (blockIdx.y == 0) back_scan<E, DK, DV, false>(p, smem, bh, jt);
-    else back_scan<E, DK, DV, true>(p, smem, bh, jt);
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
+    if (w >= kBackScanWaves) {
+        if (blockIdx.y == 0) back_loader<E, DK, DV, false>(p, smem, bh, jt, w - kBackScanWaves, l);
+        else back_loader<E, DK, DV, true>(p, smem, bh, jt, w - kBackScanWaves, l);
+    } else {
+        if (blockIdx.y == 0) back_scan<E, DK, DV, false>(p, smem, bh, jt, w, l);
+        else back_scan<E, DK, DV, true>(p, smem, bh, jt, w, l);
+    }
 }
 
 // --------------------------------------------------------------------------

@@ -134,7 +134,7 @@ template <class E> int dispatch_norm(const gdn::NormParams<E> &p, bool grad, hip
 
 // Byte offsets of the workspace regions (the records of gdn_backward.h).
 struct BackWs {
-    size_t gates, Tf, Tt, N0, Hs, Gs, eT, vT, total;
+    size_t gates, Tf, Tt, N0, C0, Hs, Gs, eT, vT, total;
 };
 
 BackWs back_layout(int B, int H, int T, int Dk, int Dv, size_t esz) {
@@ -152,6 +152,7 @@ BackWs back_layout(int B, int H, int T, int Dk, int Dv, size_t esz) {
     L.Tf = region(full * kChunk * kChunk);
     L.Tt = region(full * kChunk * kChunk);
     L.N0 = region(4 * kChunk * Dv);
+    L.C0 = region(4 * (size_t)Dk * Dv);
     L.Hs = region(4 * (size_t)Dk * Dv);
     L.Gs = region(4 * (size_t)Dk * Dv);
     L.eT = region(4 * kChunk * Dv);
@@ -168,22 +169,27 @@ bool back_shape_ok(int B, int H, int T) {
 
 template <class E, int DK, int DV> int launch_backward(const gdn::BackParams<E> &p, hipStream_t s) {
     using P = gdn::PrepLds<E, DK, DV>;
+    using S = gdn::BackScanLds<E, DK>;
     using G = gdn::GradLds<E>;
     static std::once_flag once;
     static hipError_t attr = hipSuccess;
     std::call_once(once, [] {
-        attr = hipFuncSetAttribute((const void *)gdn::gdn_back_prep_kernel<E, DK, DV>,
-                                   hipFuncAttributeMaxDynamicSharedMemorySize, (int)P::bytes);
-        if (attr == hipSuccess)
-            attr = hipFuncSetAttribute((const void *)gdn::gdn_back_grad_kernel<E, DK, DV>,
-                                       hipFuncAttributeMaxDynamicSharedMemorySize, (int)G::bytes);
+        const struct {
+            const void *fn;
+            size_t bytes;
+        } dyn[] = {{(const void *)gdn::gdn_back_prep_kernel<E, DK, DV>, P::bytes},
+                   {(const void *)gdn::gdn_back_scan_kernel<E, DK, DV>, S::bytes},
+                   {(const void *)gdn::gdn_back_grad_kernel<E, DK, DV>, G::bytes}};
+        for (const auto &d : dyn)
+            if (attr == hipSuccess)
+                attr = hipFuncSetAttribute(d.fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)d.bytes);
     });
     if (attr != hipSuccess) return GDN_ERR_HIP;
     const unsigned bh = (unsigned)(p.B * p.H), n = bh * (unsigned)p.NC;
     int st = launch(gdn::gdn_back_prep_kernel<E, DK, DV>, dim3(n), dim3(64 * gdn::kPrepWaves), P::bytes, s, p);
     if (st == GDN_OK)
         st = launch(gdn::gdn_back_scan_kernel<E, DK, DV>, dim3((bh + 7) / 8 * 8 * (DV / 16), 2),
-                    dim3(64 * gdn::kBackScanWaves), 0, s, p);
+                    dim3(S::threads), S::bytes, s, p);
     if (st == GDN_OK)
         st = launch(gdn::gdn_back_grad_kernel<E, DK, DV>, dim3(n), dim3(64 * gdn::kGradWaves), G::bytes, s, p);
     return st;
@@ -252,6 +258,7 @@ int gdn_chunk_backward(const void *q, const void *k, const void *v, const float 
         p.NC = (int)((T + (long long)gdn::kChunk - 1) / gdn::kChunk);
         p.gates = (float *)(base + L.gates);
         p.N0 = (float *)(base + L.N0);
+        p.C0 = (float *)(base + L.C0);
         p.Tf = (E *)(base + L.Tf);
         p.Tt = (E *)(base + L.Tt);
         p.Hs = (float *)(base + L.Hs);

@@ -131,9 +131,9 @@ def test_backward_workspace():
     f = ops._lib().gdn_chunk_backward_workspace_bytes
     assert f(1, 2, 100, 96, 64, 64, 1) == 0 and f(1, 2, 0, 64, 64, 64, 1) == 0 and f(1, 2, 100, 64, 64, 32, 1) == 0
     n = 16 * 55
-    per = 4 * (336 + 64 * 128 + 2 * 128 * 128 + 2 * 64 * 128)       # gates, N0, states, e and dV
+    per = 4 * (400 + 64 * 128 + 3 * 128 * 128 + 2 * 64 * 128)       # gates, N0, C0 and states, e and dV
     for bf16, planes in ((1, 6), (0, 4)):
         want = n * (per + 2 * planes * 64 * 64)
-        assert want <= f(1, 16, 3520, 128, 128, 64, bf16) < want + 11 * 256
+        assert want <= f(1, 16, 3520, 128, 128, 64, bf16) < want + 12 * 256
     with pytest.raises(ValueError, match="unsupported"):
         gdn.backward_workspace(torch.zeros(1, 3, 2, 32), torch.zeros(1, 3, 2, 64))
