@@ -39,6 +39,8 @@
 // operands are fp32 and all products fp32 MFMAs.
 #pragma once
 
+#include <type_traits>
+
 #include "gdn_device.h"
 
 namespace gdn {
@@ -179,6 +181,29 @@ template <> struct RowBlock<float, 16> {
     }
 };
 
+// Transposes the 4 x 4 values that 4 neighbouring lanes hold in 4 elements each.
+__device__ __forceinline__ f32x4 quad_transpose(f32x4 x, int l) {
+    auto other = [](float v, auto sel) {                   // the value of lane ^ 1 (0xb1) or lane ^ 2 (0x4e)
+        return __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), decltype(sel)::value, 0xf, 0xf, true));
+    };
+    const std::integral_constant<int, 0xb1> one{};
+    const std::integral_constant<int, 0x4e> two{};
+    const bool o = l & 1, h = l & 2;
+#pragma unroll
+    for (int r = 0; r < 4; r += 2) {
+        const float t = other(o ? x[r] : x[r + 1], one);
+        x[r] = o ? t : x[r];
+        x[r + 1] = o ? x[r + 1] : t;
+    }
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const float t = other(h ? x[r] : x[r + 2], two);
+        x[r] = h ? t : x[r];
+        x[r + 2] = h ? x[r + 2] : t;
+    }
+    return x;
+}
+
 template <class E> using Full = Wide<E, 3>;    // fp32's mantissa
 template <class E> using Half = Wide<E, 2>;    // 16 bits of it
 
@@ -197,7 +222,8 @@ constexpr int kBackScanGates = 132;    // floats of it from kBackGam on that the
 //                     that are all zeros are neither written nor read)
 //   N0      64 x Dv   fp32, beta A^T dO as transposed accumulator tiles [Dv/16][4 token tile][64 lane][4]
 //   C0      Dk x Dv   fp32, Q^T gam dO as accumulator tiles [Dv/16][4 wave][Dk/64][64 lane][4]
-//   Hs, Gs  Dk x Dv   fp32, row-major: H and G of the chunk
+//   Hs, Gs  Dk x Dv   fp32: H and G of the chunk, [Dv/16][Dk rows][16], the rows of each wave's 32 (Dk =
+//                     128) in P32 order, tile after tile
 //   eT, vT  Dv x 64   fp32, row-major: e^T and dV^T
 template <class E> struct BackParams {
     const E *q, *k, *v, *dout;
@@ -650,12 +676,14 @@ __device__ __forceinline__ void back_scan(const BackParams<E> &p, unsigned char 
         y[0] += y[1];
         WD::store4(sY + li * L::LDC + 16 * w + 4 * lg, L::PC, after * y[0]);
         *(f32x4 *)((REV ? p.vT : p.eT) + cidx * (size_t)(kChunk * DV) + (unsigned)((16 * jt + li) * kChunk + 16 * w + 4 * lg)) = y[0];
-        // the state that entered this chunk, for stage 3
-        float *keep = (REV ? p.Gs : p.Hs) + cidx * (size_t)(DK * DV);
+        // The state that entered this chunk, for stage 3: lane (li, lg) stores 4 columns of row
+        // 4 lg + li % 4 of a tile, 1 KB in a row from a wave (a store of 4 bytes a lane takes as
+        // long to issue, and eight of them held up the wave for 700 cycles).
+        float *keep = (REV ? p.Gs : p.Hs) + cidx * (size_t)(DK * DV) +
+                      (unsigned)((jt * DK + R * w + 4 * lg + (li & 3)) * 16 + (li & 12));
 #pragma unroll
         for (int a = 0; a < NK; ++a) {
-#pragma unroll
-            for (int q = 0; q < 4; ++q) keep[soff + (4 * a + q) * DV] = st[a][q];
+            *(f32x4 *)(keep + 256 * a) = quad_transpose(st[a], li);
             st[a] *= gC;
             if constexpr (REV) st[a] += *(const f32x4 *)(slot + L::oA + ((w * NK + a) * 64 + l) * 16);
         }
@@ -807,7 +835,11 @@ void gdn_back_grad_kernel(BackParams<E> p) {
     for (int n = 0; n < NK; ++n)
 #pragma unroll
         for (int rt = 0; rt < 4; ++rt) pq[n][rt] = pv[n][rt] = pe[n][rt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const size_t sb = cidx * (size_t)(DK * DV) + (size_t)(16 * NK * w + li) * DV + 8 * lg;
+    // row li of tile n stands for channel 32 w + p32_row(n, li) (Dk = 64: 16 w + li): a lane gets
+    // 4 NK consecutive channels in its NK results
+    auto channel = [&](int n) { return NK == 2 ? 32 * w + p32_row(n, li) : 16 * w + li; };
+    const int ch0 = NK == 2 ? 32 * w + 8 * lg : 16 * w + 4 * lg;
+    const size_t sb = cidx * (size_t)(DK * DV) + (size_t)((lg >> 1) * DK + 16 * NK * w + li) * 16 + 8 * (lg & 1);
 #pragma unroll 1
     for (int dv0 = 0; dv0 < DV; dv0 += 64) {
         if (dv0) lds_barrier();
@@ -815,13 +847,13 @@ void gdn_back_grad_kernel(BackParams<E> p) {
         lds_barrier();
 #pragma unroll 1
         for (int kb = 0; kb < 2; ++kb) {
-            const size_t at = sb + dv0 + 32 * kb;
+            const size_t at = sb + (size_t)((dv0 >> 4) + 2 * kb) * (DK * 16);
             f32x4 h[NK][2];
             wfrag S[NK];
 #pragma unroll
             for (int n = 0; n < NK; ++n) {
-                h[n][0] = *(const f32x4 *)(p.Hs + at + (size_t)16 * n * DV);
-                h[n][1] = *(const f32x4 *)(p.Hs + at + (size_t)16 * n * DV + 4);
+                h[n][0] = *(const f32x4 *)(p.Hs + at + 256 * n);
+                h[n][1] = *(const f32x4 *)(p.Hs + at + 256 * n + 4);
                 S[n] = WD::split(h[n][0], h[n][1]);
             }
 #pragma unroll
@@ -839,8 +871,8 @@ void gdn_back_grad_kernel(BackParams<E> p) {
             }
 #pragma unroll
             for (int n = 0; n < NK; ++n) {
-                const f32x4 ga = *(const f32x4 *)(p.Gs + at + (size_t)16 * n * DV),
-                            gb = *(const f32x4 *)(p.Gs + at + (size_t)16 * n * DV + 4);
+                const f32x4 ga = *(const f32x4 *)(p.Gs + at + 256 * n),
+                            gb = *(const f32x4 *)(p.Gs + at + 256 * n + 4);
                 dot += h[n][0] * ga + h[n][1] * gb;
                 S[n] = WD::split(ga, gb);
             }
@@ -875,7 +907,7 @@ void gdn_back_grad_kernel(BackParams<E> p) {
         float x = 0.f, y = 0.f;
 #pragma unroll
         for (int n = 0; n < NK; ++n) {
-            const size_t at = (row0 + (size_t)min(t, nvalid - 1) * p.H) * DK + 16 * (NK * w + n) + 4 * lg;
+            const size_t at = (row0 + (size_t)min(t, nvalid - 1) * p.H) * DK + ch0 + 4 * n;
             const f32x4 q4 = TR::to_f32(TR::load(p.q + at)), k4 = TR::to_f32(TR::load(p.k + at));
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -963,8 +995,8 @@ void gdn_back_grad_kernel(BackParams<E> p) {
         for (int n = 0; n < NK; ++n)
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
-                kt[n][kb] = columns(p.k, 16 * (NK * w + n) + li, kb);
-                qt[n][kb] = columns(p.q, 16 * (NK * w + n) + li, kb);
+                kt[n][kb] = columns(p.k, channel(n), kb);
+                qt[n][kb] = columns(p.q, channel(n), kb);
             }
 #pragma unroll
         for (int rt = 0; rt < 4; ++rt) {
@@ -990,11 +1022,13 @@ void gdn_back_grad_kernel(BackParams<E> p) {
             }
             const int t = 16 * rt + li;
             if (t < nvalid) {
-#pragma unroll
-                for (int n = 0; n < NK; ++n) {
-                    const size_t at = (row0 + (size_t)t * p.H) * DK + 16 * (NK * w + n) + 4 * lg;
-                    TR::store(p.dq + at, TR::from_f32(pq[n][rt]));
-                    TR::store(p.dk + at, TR::from_f32(pe[n][rt] - gk[n]));
+                const size_t at = (row0 + (size_t)t * p.H) * DK + ch0;
+                if constexpr (NK == 2) {
+                    TR::store8(p.dq + at, TR::cat(TR::from_f32(pq[0][rt]), TR::from_f32(pq[1][rt])));
+                    TR::store8(p.dk + at, TR::cat(TR::from_f32(pe[0][rt] - gk[0]), TR::from_f32(pe[1][rt] - gk[1])));
+                } else {
+                    TR::store(p.dq + at, TR::from_f32(pq[0][rt]));
+                    TR::store(p.dk + at, TR::from_f32(pe[0][rt] - gk[0]));
                 }
             }
         }
