@@ -10,11 +10,14 @@
 //
 // Both are bound by memory.  A team of TPR threads takes a row at a time and
 // holds it in registers, 8 consecutive channels per thread, so every element is
-// read and written once; the means are wave reductions joined
-// through LDS.  A team's rows are consecutive (a strip): the weights stay in
-// registers, the gate row is read again only where it changes, and the sums
-// over rows are kept in registers until the strip ends.
+// read and written once; the means are wave reductions joined through LDS, and the
+// next row's loads are issued before this row's means are formed.  A team's
+// rows are consecutive (a strip): the weights stay in registers, the gate row is
+// read again only where it changes, and the sums over rows are kept in registers
+// until the strip ends.
 #pragma once
+
+#include <type_traits>
 
 #include "gdn_device.h"
 
@@ -36,13 +39,20 @@ template <class E> struct NormParams {
     float res_scale, eps;
 };
 
-// Vectors of 8 elements at any element alignment (a row of odd length starts
-// at any element): one access per 16 bytes either way.
+// 8 consecutive elements at any element alignment (a row of odd length starts
+// at any element): whole 16-byte accesses either way.
 template <class E> struct Vec8;
 template <> struct Vec8<uint16_t> {
-    typedef u32x4 raw __attribute__((aligned(2)));
-    static __device__ __forceinline__ void load(const uint16_t *p, float *x) {
-        const u32x4 v = *(const raw *)p;
+    typedef u32x4 loose __attribute__((aligned(2)));
+    u32x4 v;
+    __device__ __forceinline__ void load(const uint16_t *p) { v = *(const loose *)p; }
+    __device__ __forceinline__ void load_some(const uint16_t *p, int n) {
+        uint16_t x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = i < n ? p[i] : 0;
+        v = __builtin_bit_cast(u32x4, x);
+    }
+    __device__ __forceinline__ void values(float *x) const {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             x[2 * i] = __uint_as_float(v[i] << 16);
@@ -53,44 +63,75 @@ template <> struct Vec8<uint16_t> {
         u32x4 v;
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
-        *(raw *)p = v;
+        *(loose *)p = v;
     }
-    static __device__ __forceinline__ float one(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
     static __device__ __forceinline__ uint16_t cvt(float v) { return (uint16_t)pack_bf16x2(v, 0.f); }
 };
 template <> struct Vec8<float> {
-    typedef f32x4 raw __attribute__((aligned(4)));
-    static __device__ __forceinline__ void load(const float *p, float *x) {
-        const f32x4 a = *(const raw *)p, b = *(const raw *)(p + 4);
+    typedef f32x4 loose __attribute__((aligned(4)));
+    f32x4 a, b;
+    __device__ __forceinline__ void load(const float *p) { a = *(const loose *)p, b = *(const loose *)(p + 4); }
+    __device__ __forceinline__ void load_some(const float *p, int n) {
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = i < n ? p[i] : 0.f;
+        a = f32x4{x[0], x[1], x[2], x[3]}, b = f32x4{x[4], x[5], x[6], x[7]};
+    }
+    __device__ __forceinline__ void values(float *x) const {
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = a[i], x[4 + i] = b[i];
     }
     static __device__ __forceinline__ void store(float *p, const float *x) {
-        *(raw *)p = f32x4{x[0], x[1], x[2], x[3]};
-        *(raw *)(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
+        *(loose *)p = f32x4{x[0], x[1], x[2], x[3]};
+        *(loose *)(p + 4) = f32x4{x[4], x[5], x[6], x[7]};
     }
-    static __device__ __forceinline__ float one(float v) { return v; }
     static __device__ __forceinline__ float cvt(float v) { return v; }
 };
 
-// 8 channels from c of a row of C; channels past the row's end read as 0 and
-// are not written.
-template <class E> __device__ __forceinline__ void load_row(const E *row, int c, int C, float *x) {
-    if (c + 8 <= C) {
-        Vec8<E>::load(row + c, x);
-    } else {
+// The 8 channels of a thread.  Rows of 8 channels or more: the last ones of the row where
+// its own would reach past the end, so that every access is a whole vector; what
+// another thread has too is left out of the sums (`own`) and written twice, with
+// the same bits.  Shorter rows (SHORT) are thread 0's, element by element.
+template <bool SHORT> struct Channels {
+    int c, n;           // first channel, elements (SHORT)
+    bool own[8];
+    __device__ __forceinline__ Channels(int t, int C) {
+        const int c0 = 8 * t;
+        c = SHORT ? 0 : min(c0, C - 8);
+        n = SHORT && t == 0 ? C : 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = c + i < C ? Vec8<E>::one(row[c + i]) : 0.f;
+        for (int i = 0; i < 8; ++i) own[i] = SHORT ? i < n : c + i >= c0;
     }
-}
-template <class E> __device__ __forceinline__ void store_row(E *row, int c, int C, const float *x) {
-    if (c + 8 <= C) {
-        Vec8<E>::store(row + c, x);
-    } else {
+    template <class E> __device__ __forceinline__ Vec8<E> load(const E *row) const {
+        Vec8<E> v;
+        if constexpr (SHORT) v.load_some(row, n);
+        else v.load(row + c);
+        return v;
+    }
+    template <class E> __device__ __forceinline__ void load(const E *row, float *x) const { load(row).values(x); }
+    template <class E> __device__ __forceinline__ void store(E *row, const float *x) const {
+        if constexpr (SHORT) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (c + i < C) row[c + i] = Vec8<E>::cvt(x[i]);
+            for (int i = 0; i < 8; ++i)
+                if (i < n) row[i] = Vec8<E>::cvt(x[i]);
+        } else {
+            Vec8<E>::store(row + c, x);
+        }
     }
+};
+
+// Sum over the lanes of a wave, in every lane: 16 lanes by cross-lane adds, the four
+// groups of 16 by reading a lane of each.
+__device__ __forceinline__ float wave_sum(float v) {
+    auto add = [&](auto sel) {
+        v += __uint_as_float(__builtin_amdgcn_mov_dpp(__float_as_uint(v), decltype(sel)::value, 0xf, 0xf, true));
+    };
+    add(std::integral_constant<int, 0xb1>{});      // lane ^ 1
+    add(std::integral_constant<int, 0x4e>{});      // lane ^ 2
+    add(std::integral_constant<int, 0x141>{});     // the other 4 of 8
+    add(std::integral_constant<int, 0x140>{});     // the other 8 of 16
+    auto lane = [&](int l) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), l)); };
+    return (lane(0) + lane(16)) + (lane(32) + lane(48));
 }
 
 // Sums of NS values over the TPR threads of a team, in every thread.  `buf`: two
@@ -98,9 +139,7 @@ template <class E> __device__ __forceinline__ void store_row(E *row, int c, int 
 template <int NS, int TPR>
 __device__ __forceinline__ void team_sum(float *v, float *buf, int &turn) {
 #pragma unroll
-    for (int d = 1; d < 64; d <<= 1)
-#pragma unroll
-        for (int s = 0; s < NS; ++s) v[s] += __shfl_xor(v[s], d);
+    for (int s = 0; s < NS; ++s) v[s] = wave_sum(v[s]);
     if constexpr (TPR > 64) {
         constexpr int NW = TPR / 64;
         float *b = buf + turn * 32;
@@ -131,100 +170,110 @@ template <class E> __device__ __forceinline__ int strip_begin(const NormParams<E
     return (int)r0;
 }
 
-template <class E, int TPR>
+template <class E, int TPR, bool SHORT>
 __global__ __launch_bounds__(norm_threads<TPR>()) void gdn_block_norm_kernel(NormParams<E> p) {
     constexpr int TEAMS = norm_threads<TPR>() / TPR;
     __shared__ float buf[64];
     int turn = 0;
-    const int team = threadIdx.x / TPR, c = threadIdx.x % TPR * 8;
-    const int strip = blockIdx.x * TEAMS + team;
-    const long long r0 = (long long)strip * p.strip_rows; // forward strips are plain runs of rows
-    const int C = p.C;
-    const float rc = 1.f / (float)C;
+    const Channels<SHORT> ch(threadIdx.x % TPR, p.C);
+    const long long r0 = ((long long)blockIdx.x * TEAMS + threadIdx.x / TPR) * p.strip_rows;
+    const float rc = 1.f / (float)p.C;
     float wa[8], wb[8], ga[8];
-    load_row<float>(p.w_post, c, C, wa);
-    load_row<float>(p.w_pre, c, C, wb);
+    ch.load(p.w_post, wa);
+    ch.load(p.w_pre, wb);
 #pragma unroll
     for (int i = 0; i < 8; ++i) ga[i] = 1.f;
     int grow = -1;
+    // rows past the end (of the last teams) read the last row again and write nothing
+    auto at = [&](int i) { return (size_t)min(r0 + min(i, p.strip_rows - 1), (long long)p.R - 1) * p.C; };
+    Vec8<E> yn = ch.load(p.y + at(0)), xn = ch.load(p.x + at(0));
     // every team of a workgroup makes the same number of turns (barriers)
     for (int i0 = 0; i0 < p.strip_rows; ++i0) {
-        const long long row = r0 + i0;
-        const bool on = row < p.R;
-        const size_t base = (size_t)(on ? row : 0) * C;
-        float x[8], y[8];
-        float s[1] = {0.f};
-        load_row<E>(p.y + base, c, C, y);
-        load_row<E>(p.x + base, c, C, x);
+        const bool on = r0 + i0 < p.R;
+        const size_t base = at(i0);
+        float x[8], y[8], s[1] = {0.f};
+        yn.values(y);
+        xn.values(x);
         if (p.gate) {
-            const int gr = (int)((on ? row : 0) / p.gate_tokens);
+            const int gr = (int)(min(r0 + i0, (long long)p.R - 1) / p.gate_tokens);
             if (gr != grow) {
                 grow = gr;
-                load_row<E>(p.gate + (size_t)gr * C, c, C, ga);
+                ch.load(p.gate + (size_t)gr * p.C, ga);
             }
         }
+        yn = ch.load(p.y + at(i0 + 1));
+        xn = ch.load(p.x + at(i0 + 1));
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[0] += y[i] * y[i];
+        for (int i = 0; i < 8; ++i) s[0] += ch.own[i] ? y[i] * y[i] : 0.f;
         team_sum<1, TPR>(s, buf, turn);
         const float iy = 1.f / sqrtf(s[0] * rc + p.eps);
         s[0] = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             x[i] = p.res_scale * x[i] + ga[i] * (y[i] * iy * wa[i]);
-            // channels past the row's end stay out of the sum whatever res_scale and iy are
-            if (c + i < C) s[0] += x[i] * x[i];
+            s[0] += ch.own[i] ? x[i] * x[i] : 0.f;
         }
         team_sum<1, TPR>(s, buf, turn);
         const float ir = 1.f / sqrtf(s[0] * rc + p.eps);
         if (!on) continue;
-        store_row<E>(p.r + base, c, C, x);
+        ch.store(p.r + base, x);
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] *= ir * wb[i];
-        store_row<E>(p.u + base, c, C, x);
+        ch.store(p.u + base, x);
     }
 }
 
-template <class E, int TPR>
+template <class E, int TPR, bool SHORT>
 __global__ __launch_bounds__(norm_threads<TPR>()) void gdn_block_norm_grad_kernel(NormParams<E> p) {
     constexpr int TEAMS = norm_threads<TPR>() / TPR;
     __shared__ float buf[64];
     int turn = 0;
-    const int team = threadIdx.x / TPR, c = threadIdx.x % TPR * 8;
-    const int strip = blockIdx.x * TEAMS + team;
+    const Channels<SHORT> ch(threadIdx.x % TPR, p.C);
+    const int strip = blockIdx.x * TEAMS + threadIdx.x / TPR;
     const int C = p.C;
     const float rc = 1.f / (float)C;
     int rows = 0, r0 = 0;
     if (strip < p.strips) r0 = strip_begin(p, strip, rows);
     float wa[8], wb[8], ga[8], sa[8], sb[8], sg[8];
-    load_row<float>(p.w_post, c, C, wa);
-    load_row<float>(p.w_pre, c, C, wb);
+    ch.load(p.w_post, wa);
+    ch.load(p.w_pre, wb);
 #pragma unroll
     for (int i = 0; i < 8; ++i) ga[i] = 1.f, sa[i] = sb[i] = sg[i] = 0.f;
     int left = 0;                                         // rows until the gate row changes
+    // turns past the strip's last row read it again and write nothing
+    auto at = [&](int i) { return (size_t)(r0 + min(i, max(rows - 1, 0))) * C; };
+    Vec8<E> xn, yn, dn, en{};
+    auto fetch = [&](int i) {
+        const size_t base = at(i);
+        yn = ch.load(p.y + base);
+        xn = ch.load(p.x + base);
+        dn = ch.load(p.du + base);
+        if (p.dr) en = ch.load(p.dr + base);
+    };
+    // (1024 threads have no registers for a row ahead)
+    constexpr bool AHEAD = TPR < 1024;
+    if (AHEAD) fetch(0);
     for (int i0 = 0; i0 < p.strip_rows; ++i0) {
         const bool on = i0 < rows;
-        const int row = on ? r0 + i0 : 0;
-        const size_t base = (size_t)row * C;
+        const int row = r0 + i0;
+        const size_t base = at(i0);
         float x[8], y[8], d[8], e[8];
-        load_row<E>(p.y + base, c, C, y);
-        load_row<E>(p.x + base, c, C, x);
-        load_row<E>(p.du + base, c, C, d);
-        if (p.dr) {
-            load_row<E>(p.dr + base, c, C, e);
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) e[i] = 0.f;
-        }
+        if (!AHEAD) fetch(i0);
+        yn.values(y);
+        xn.values(x);
+        dn.values(d);
+        en.values(e);
         if (p.gate && on && left == 0) {
             const int gr = row / p.gate_tokens;
             left = p.gate_tokens - (row - gr * p.gate_tokens);
-            load_row<E>(p.gate + (size_t)gr * C, c, C, ga);
+            ch.load(p.gate + (size_t)gr * C, ga);
 #pragma unroll
             for (int i = 0; i < 8; ++i) sg[i] = 0.f;
         }
+        if (AHEAD) fetch(i0 + 1);
         float s[2] = {0.f, 0.f};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[0] += y[i] * y[i];
+        for (int i = 0; i < 8; ++i) s[0] += ch.own[i] ? y[i] * y[i] : 0.f;
         team_sum<1, TPR>(s, buf, turn);
         const float iy = 1.f / sqrtf(s[0] * rc + p.eps);
         s[0] = s[1] = 0.f;
@@ -232,10 +281,8 @@ __global__ __launch_bounds__(norm_threads<TPR>()) void gdn_block_norm_grad_kerne
         for (int i = 0; i < 8; ++i) {
             y[i] *= iy;                                            // yh
             x[i] = p.res_scale * x[i] + ga[i] * (y[i] * wa[i]);    // r
-            if (c + i < C) {
-                s[0] += x[i] * x[i];
-                s[1] += x[i] * (d[i] * wb[i]);
-            }
+            s[0] += ch.own[i] ? x[i] * x[i] : 0.f;
+            s[1] += ch.own[i] ? x[i] * (d[i] * wb[i]) : 0.f;
         }
         team_sum<2, TPR>(s, buf, turn);
         const float ir = 1.f / sqrtf(s[0] * rc + p.eps);
@@ -253,23 +300,21 @@ __global__ __launch_bounds__(norm_threads<TPR>()) void gdn_block_norm_grad_kerne
                 sg[i] += y[i] * wa[i] * g;
             }
             d[i] = gg * wa[i];                                     // d2
-            if (c + i < C) s[0] += d[i] * y[i];
+            s[0] += ch.own[i] ? d[i] * y[i] : 0.f;
         }
         team_sum<1, TPR>(s, buf, turn);
         const float m2 = s[0] * rc;
         if (!on) continue;
-        store_row<E>(p.dx + base, c, C, x);
+        ch.store(p.dx + base, x);
 #pragma unroll
         for (int i = 0; i < 8; ++i) d[i] = iy * (d[i] - y[i] * m2);
-        store_row<E>(p.dy + base, c, C, d);
-        if (p.gate && --left == 0 && p.per_unit == 1) {
-            store_row<E>(p.dgate + (size_t)(row / p.gate_tokens) * C, c, C, sg);
-        }
+        ch.store(p.dy + base, d);
+        if (p.gate && --left == 0 && p.per_unit == 1) ch.store(p.dgate + (size_t)(row / p.gate_tokens) * C, sg);
     }
     if (strip < p.strips) {
-        store_row<float>(p.part_w + (size_t)strip * 2 * C, c, C, sa);
-        store_row<float>(p.part_w + (size_t)strip * 2 * C + C, c, C, sb);
-        if (p.gate && p.per_unit > 1) store_row<float>(p.part_g + (size_t)strip * C, c, C, sg);
+        ch.store(p.part_w + (size_t)strip * 2 * C, sa);
+        ch.store(p.part_w + (size_t)strip * 2 * C + C, sb);
+        if (p.gate && p.per_unit > 1) ch.store(p.part_g + (size_t)strip * C, sg);
     }
 }
 

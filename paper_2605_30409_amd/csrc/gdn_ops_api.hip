@@ -108,11 +108,11 @@ bool norm_shape_ok(int R, int C, int gate_tokens) {
     return R >= 1 && C >= 1 && gate_tokens >= 1 && R % gate_tokens == 0;
 }
 
-template <class E, int TPR> int launch_norm(const gdn::NormParams<E> &p, bool grad, hipStream_t s) {
+template <class E, int TPR, bool SHORT = false> int launch_norm(const gdn::NormParams<E> &p, bool grad, hipStream_t s) {
     constexpr int threads = gdn::norm_threads<TPR>(), teams = threads / TPR;
     const dim3 grid((unsigned)((p.strips + teams - 1) / teams));
-    if (!grad) return launch(gdn::gdn_block_norm_kernel<E, TPR>, grid, dim3(threads), 0, s, p);
-    const int st = launch(gdn::gdn_block_norm_grad_kernel<E, TPR>, grid, dim3(threads), 0, s, p);
+    if (!grad) return launch(gdn::gdn_block_norm_kernel<E, TPR, SHORT>, grid, dim3(threads), 0, s, p);
+    const int st = launch(gdn::gdn_block_norm_grad_kernel<E, TPR, SHORT>, grid, dim3(threads), 0, s, p);
     if (st != GDN_OK) return st;
     const unsigned gates = p.gate && p.per_unit > 1 ? (unsigned)(p.R / p.gate_tokens) : 0u;
     return launch(gdn::gdn_block_norm_reduce_kernel<E>, dim3((unsigned)((2 * p.C + 63) / 64), 1 + gates),
@@ -120,6 +120,7 @@ template <class E, int TPR> int launch_norm(const gdn::NormParams<E> &p, bool gr
 }
 
 template <class E> int dispatch_norm(const gdn::NormParams<E> &p, bool grad, hipStream_t s) {
+    if (p.C < 8) return launch_norm<E, 64, true>(p, grad, s);
     switch (norm_team(p.C)) {
     case 64: return launch_norm<E, 64>(p, grad, s);
     case 128: return launch_norm<E, 128>(p, grad, s);

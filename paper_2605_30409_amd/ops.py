@@ -43,17 +43,19 @@ def _ptr(t):
 def _call(name, dev, *args):
     """The C call with the current stream of `dev` behind its other arguments."""
     fn = getattr(_lib(), name)
-    stream = torch.cuda.current_stream(dev).cuda_stream
     if torch.cuda.current_device() == dev.index:
-        rc = fn(*args, stream)
+        rc = fn(*args, torch.cuda.current_stream().cuda_stream)
     else:
         with torch.cuda.device(dev):
-            rc = fn(*args, stream)
+            rc = fn(*args, torch.cuda.current_stream().cuda_stream)
     if rc != GDN_OK:
         raise GdnError(name, rc)
 
 
 def _need(name, t, shape, dtype, dev):
+    # one condition for the call that is right: a small call is as long as its checks
+    if type(t) is torch.Tensor and t.dtype is dtype and t.shape == shape and t.device == dev and t.is_contiguous():
+        return
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a tensor, got {type(t).__name__}")
     if t.dtype != dtype:
