@@ -781,7 +781,11 @@ void gdn_back_grad_kernel(BackParams<E> p) {
     float *rX = (float *)(smem + L::oRed), *rE = rX + 4 * 64, *cb = rE + 4 * 64, *xm = cb + 4 * 64, *gh = xm + 64;
     const int c = blockIdx.x / (p.B * p.H), bh = blockIdx.x - c * (p.B * p.H);
     const int b = bh / p.H, h = bh - b * p.H;
-    const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, li = l & 15, lg = l >> 4;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
+    int tid = threadIdx.x, li = l & 15, lg = l >> 4;
+    // What follows computes its addresses anew: kept from the front on, they would take the
+    // registers of the products between.
+    auto forget = [&] { asm volatile("" : "+v"(tid), "+v"(li), "+v"(lg)); };
     const int t0 = c * kChunk, nvalid = min(kChunk, p.T - t0);
     const size_t cidx = (size_t)bh * p.NC + c;
     const size_t row0 = ((size_t)b * p.T + t0) * p.H + h;
@@ -799,31 +803,6 @@ void gdn_back_grad_kernel(BackParams<E> p) {
         return __builtin_bit_cast(frag, x);
     };
     const float *ge = p.eT + cidx * (size_t)(kChunk * DV), *gv = p.vT + cidx * (size_t)(kChunk * DV);
-    auto stage_part = [&](int dv0) {                               // 64 value channels into LDS
-        f32x4 re[NST], rv[NST];
-        uint4 ro[NSO];
-#pragma unroll
-        for (int i = 0; i < NST; ++i) {
-            re[i] = *(const f32x4 *)(ge + dv0 * kChunk + (tid + i * NT) * 4);
-            rv[i] = *(const f32x4 *)(gv + dv0 * kChunk + (tid + i * NT) * 4);
-        }
-#pragma unroll
-        for (int i = 0; i < NSO; ++i) {
-            const int idx = tid + i * NT, r = idx / (64 / VE), cv = idx % (64 / VE);
-            ro[i] = *(const uint4 *)(p.dout + (row0 + (size_t)min(r, nvalid - 1) * p.H) * DV + dv0 + cv * VE);
-        }
-#pragma unroll
-        for (int i = 0; i < NST; ++i) {
-            const int idx = tid + i * NT, at = (idx >> 4) * L::LDC + (idx & 15) * 4;
-            WD::store4(sE + at, L::PC, re[i]);
-            WD::store4(sV + at, L::PC, rv[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < NSO; ++i) {
-            const int idx = tid + i * NT, r = idx / (64 / VE), cv = idx % (64 / VE);
-            *(uint4 *)(sO + r * L::LDC + cv * VE) = r < nvalid ? ro[i] : make_uint4(0u, 0u, 0u, 0u);
-        }
-    };
     for (int i = tid; i < kBackGateRec; i += NT) ((float *)(smem + L::oGate))[i] = p.gates[cidx * kBackGateRec + i];
 
     // PQ, PV, PE transposed, tiles [16 key channels][16 tokens]; Z and F
@@ -838,24 +817,59 @@ void gdn_back_grad_kernel(BackParams<E> p) {
     // row li of tile n stands for channel 32 w + p32_row(n, li) (Dk = 64: 16 w + li): a lane gets
     // 4 NK consecutive channels in its NK results
     auto channel = [&](int n) { return NK == 2 ? 32 * w + p32_row(n, li) : 16 * w + li; };
-    const int ch0 = NK == 2 ? 32 * w + 8 * lg : 16 * w + 4 * lg;
-    const size_t sb = cidx * (size_t)(DK * DV) + (size_t)((lg >> 1) * DK + 16 * NK * w + li) * 16 + 8 * (lg & 1);
-#pragma unroll 1
-    for (int dv0 = 0; dv0 < DV; dv0 += 64) {
-        if (dv0) lds_barrier();
-        stage_part(dv0);
-        lds_barrier();
-#pragma unroll 1
-        for (int kb = 0; kb < 2; ++kb) {
-            const size_t at = sb + (size_t)((dv0 >> 4) + 2 * kb) * (DK * 16);
-            f32x4 h[NK][2];
-            wfrag S[NK];
+    auto ch0 = [&] { return NK == 2 ? 32 * w + 8 * lg : 16 * w + 4 * lg; };
+    auto quads = [&](const float *m, int j0, f32x4 (&x)[NK][2]) {  // 8 columns from j0 on of the rows of NK tiles
+        const float *at = m + cidx * (size_t)(DK * DV) + (j0 >> 4) * (DK * 16) +
+                          (unsigned)(((lg >> 1) * DK + 16 * NK * w + li) * 16 + 8 * (lg & 1));
 #pragma unroll
-            for (int n = 0; n < NK; ++n) {
-                h[n][0] = *(const f32x4 *)(p.Hs + at + 256 * n);
-                h[n][1] = *(const f32x4 *)(p.Hs + at + 256 * n + 4);
-                S[n] = WD::split(h[n][0], h[n][1]);
+        for (int n = 0; n < NK; ++n) {
+            x[n][0] = *(const f32x4 *)(at + 256 * n);
+            x[n][1] = *(const f32x4 *)(at + 256 * n + 4);
+        }
+    };
+    // The scheduling barriers keep each group of loads where it is, a product ahead of its
+    // use: all at the front they do not fit the registers, at their uses every one is waited for.
+    f32x4 hs[NK][2];
+    quads(p.Hs, 0, hs);
+#pragma unroll 1
+    for (int j0 = 0; j0 < DV; j0 += 32) {                          // 32 value channels a turn
+        const int dv0 = j0 & ~63, kb = (j0 >> 5) & 1;
+        forget();
+        if (kb == 0) {
+            if (j0) lds_barrier();
+            f32x4 re[NST], rv[NST];
+            uint4 ro[NSO];
+#pragma unroll
+            for (int i = 0; i < NST; ++i) {
+                re[i] = *(const f32x4 *)(ge + dv0 * kChunk + (tid + i * NT) * 4);
+                rv[i] = *(const f32x4 *)(gv + dv0 * kChunk + (tid + i * NT) * 4);
             }
+#pragma unroll
+            for (int i = 0; i < NSO; ++i) {
+                const int idx = tid + i * NT, r = idx / (64 / VE), cv = idx % (64 / VE);
+                ro[i] = *(const uint4 *)(p.dout + (row0 + (size_t)min(r, nvalid - 1) * p.H) * DV + dv0 + cv * VE);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int i = 0; i < NST; ++i) {
+                const int idx = tid + i * NT, at = (idx >> 4) * L::LDC + (idx & 15) * 4;
+                WD::store4(sE + at, L::PC, re[i]);
+                WD::store4(sV + at, L::PC, rv[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < NSO; ++i) {
+                const int idx = tid + i * NT, r = idx / (64 / VE), cv = idx % (64 / VE);
+                *(uint4 *)(sO + r * L::LDC + cv * VE) = r < nvalid ? ro[i] : make_uint4(0u, 0u, 0u, 0u);
+            }
+            lds_barrier();
+        }
+        {
+            f32x4 g[NK][2];
+            wfrag S[NK];
+            quads(p.Gs, j0, g);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int n = 0; n < NK; ++n) S[n] = WD::split(hs[n][0], hs[n][1]);
 #pragma unroll
             for (int rt = 0; rt < 4; ++rt) {
                 const frag o = load_frag<E>(sO + (16 * rt + li) * L::LDC + 32 * kb, lg);
@@ -868,19 +882,7 @@ void gdn_back_grad_kernel(BackParams<E> p) {
                 // dV: wave rt stores the rows it has at hand
                 if (w == rt && 16 * rt + li < nvalid)
                     TR::store8(p.dv + (row0 + (size_t)(16 * rt + li) * p.H) * DV + dv0 + 32 * kb + 8 * lg, WD::rounded(dv));
-            }
-#pragma unroll
-            for (int n = 0; n < NK; ++n) {
-                const f32x4 ga = *(const f32x4 *)(p.Gs + at + 256 * n),
-                            gb = *(const f32x4 *)(p.Gs + at + 256 * n + 4);
-                dot += h[n][0] * ga + h[n][1] * gb;
-                S[n] = WD::split(ga, gb);
-            }
-#pragma unroll
-            for (int rt = 0; rt < 4; ++rt) {
-                const wfrag e = WD::tr(sE, L::PC, L::LDC, 32 * kb, 16 * rt, li, lg);
-#pragma unroll
-                for (int n = 0; n < NK; ++n) pe[n][rt] = WD::ww(S[n], e, pe[n][rt]);
+                if (rt & 1) __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
             for (int n = 0; n < NTI; ++n) {
@@ -890,9 +892,25 @@ void gdn_back_grad_kernel(BackParams<E> p) {
                 const wfrag ej = WD::tr(sE, L::PC, L::LDC, 32 * kb, 16 * bj, li, lg);
                 z[n] = WD::ew(load_frag<E>(sO + (16 * bi + li) * L::LDC + 32 * kb, lg), ej, z[n]);
                 f[n] = WD::ww(WD::tr(sV, L::PC, L::LDC, 32 * kb, 16 * bi, li, lg), ej, f[n]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+#pragma unroll
+            for (int n = 0; n < NK; ++n) {
+                dot += hs[n][0] * g[n][0] + hs[n][1] * g[n][1];
+                S[n] = WD::split(g[n][0], g[n][1]);
+            }
+            quads(p.Hs, min(j0 + 32, DV - 32), hs);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt) {
+                const wfrag e = WD::tr(sE, L::PC, L::LDC, 32 * kb, 16 * rt, li, lg);
+#pragma unroll
+                for (int n = 0; n < NK; ++n) pe[n][rt] = WD::ww(S[n], e, pe[n][rt]);
+                if (rt & 1) __builtin_amdgcn_sched_barrier(0);
             }
         }
     }
+    forget();
     {
         float s = dot[0] + dot[1] + dot[2] + dot[3];
 #pragma unroll
@@ -907,7 +925,7 @@ void gdn_back_grad_kernel(BackParams<E> p) {
         float x = 0.f, y = 0.f;
 #pragma unroll
         for (int n = 0; n < NK; ++n) {
-            const size_t at = (row0 + (size_t)min(t, nvalid - 1) * p.H) * DK + ch0 + 4 * n;
+            const size_t at = (row0 + (size_t)min(t, nvalid - 1) * p.H) * DK + ch0() + 4 * n;
             const f32x4 q4 = TR::to_f32(TR::load(p.q + at)), k4 = TR::to_f32(TR::load(p.k + at));
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -927,6 +945,7 @@ void gdn_back_grad_kernel(BackParams<E> p) {
         }
     }
     lds_barrier();
+    forget();
     // The 64 x 64 matrices: element (i, j) with i = 16 bi + 4 lg + q, j = 16 bj + li.  The six
     // tiles above the diagonal of G1 and X are zero.
 #pragma unroll
@@ -973,6 +992,7 @@ void gdn_back_grad_kernel(BackParams<E> p) {
         if (lg == 0) cb[bi * 64 + j] = cs;
     }
     lds_barrier();
+    forget();
 
     // Sums over the waves: dbeta, X's border row and column
     if (tid < 64) {
@@ -1022,7 +1042,7 @@ void gdn_back_grad_kernel(BackParams<E> p) {
             }
             const int t = 16 * rt + li;
             if (t < nvalid) {
-                const size_t at = (row0 + (size_t)t * p.H) * DK + ch0;
+                const size_t at = (row0 + (size_t)t * p.H) * DK + ch0();
                 if constexpr (NK == 2) {
                     TR::store8(p.dq + at, TR::cat(TR::from_f32(pq[0][rt]), TR::from_f32(pq[1][rt])));
                     TR::store8(p.dk + at, TR::cat(TR::from_f32(pe[0][rt] - gk[0]), TR::from_f32(pe[1][rt] - gk[1])));
