@@ -210,9 +210,9 @@ template <class E> using Half = Wide<E, 2>;    // 16 bits of it
 __device__ __forceinline__ float elem_f32(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
 __device__ __forceinline__ float elem_f32(float x) { return x; }
 
-// Gate record of a chunk, in floats: g as 64 doubles, tail, beta; then, what the scans take,
-// gam, beta tail and e^{g_C}.
-constexpr int kBackTail = 128, kBackBeta = 192, kBackGam = 256, kBackBt = 320, kBackGC = 384, kBackGateRec = 400;
+// Gate record of a chunk, in floats: g log2(e) as a sum of two, tail, beta; then, what the scans
+// take, gam, beta tail and e^{g_C}.
+constexpr int kBackGHi = 0, kBackGLo = 64, kBackTail = 128, kBackBeta = 192, kBackGam = 256, kBackBt = 320, kBackGC = 384, kBackGateRec = 400;
 constexpr int kBackScanGates = 132;    // floats of it from kBackGam on that the scans copy
 
 // Workspace records per (b*H + h, chunk); "planes": three of bf16, each behind the
@@ -236,6 +236,12 @@ template <class E> struct BackParams {
 };
 
 template <class E> constexpr int full_elems(int n) { return n * Full<E>::planes; }
+
+// D_ij = e^{g_i - g_j} from g log2(e) in two floats: the difference is as exact as its own rounding,
+// where one float would have that of g (5600 after a chunk of alpha ~ 0).
+__device__ __forceinline__ float back_decay(const float *gate, int i, int j) {
+    return __builtin_amdgcn_exp2f((gate[kBackGHi + i] - gate[kBackGHi + j]) + (gate[kBackGLo + i] - gate[kBackGLo + j]));
+}
 
 // Padded leading dimension of an LDS tile with rows of n elements of E.
 template <class E> constexpr int lds_ld(int n) { return n + 16 / (int)sizeof(E); }
@@ -300,8 +306,7 @@ void gdn_back_prep_kernel(BackParams<E> p) {
     extern __shared__ __align__(16) unsigned char smem[];
     E *sK = (E *)(smem + L::oK), *sQ = (E *)(smem + L::oQ), *sO = sK, *sA = (E *)(smem + L::oA);
     float *sN = (float *)(smem + L::oN);     // N[r][c] at [r][c] (c < r), T[r][c] at [c][r] (c <= r)
-    double *sg = (double *)(smem + L::oG);
-    float *sb = (float *)(sg + kChunk), *sgam = sb + kChunk;
+    float *sg = (float *)(smem + L::oG), *sb = sg + 2 * kChunk, *sgam = sb + kChunk;
     const int c = blockIdx.x / (p.B * p.H), bh = blockIdx.x - c * (p.B * p.H);
     const int b = bh / p.H, h = bh - b * p.H;
     const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, li = l & 15, lg = l >> 4;
@@ -330,9 +335,11 @@ void gdn_back_prep_kernel(BackParams<E> p) {
             if (l >= d) g += o;
         }
         const double gC = __shfl(g, kChunk - 1);
-        sg[l] = g;
+        const double g2 = g * 1.4426950408889634;
+        const float ghi = (float)g2, glo = (float)(g2 - (double)ghi);
+        sg[kBackGHi + l] = gate[kBackGHi + l] = ghi;
+        sg[kBackGLo + l] = gate[kBackGLo + l] = glo;
         sb[l] = be;
-        ((double *)gate)[l] = g;
         const float gam = expf((float)g), tail = expf((float)(gC - g));
         sgam[l] = gam;
         gate[kBackGam + l] = gam;
@@ -359,7 +366,7 @@ void gdn_back_prep_kernel(BackParams<E> p) {
                           load_frag<E>(sK + (16 * bj + li) * L::LDK + 32 * kb, lg), acc);
         const int j = 16 * bj + li, i0 = 16 * bi + 4 * lg;
 #pragma unroll
-        for (int q = 0; q < 4; ++q) acc[q] = j <= i0 + q ? acc[q] * expf((float)(sg[i0 + q] - sg[j])) : 0.f;
+        for (int q = 0; q < 4; ++q) acc[q] = j <= i0 + q ? acc[q] * back_decay(sg, i0 + q, j) : 0.f;
         if (t < 10) {
 #pragma unroll
             for (int q = 0; q < 4; ++q)
@@ -755,9 +762,9 @@ template <class E> struct GradLds {
     static constexpr size_t endB = oG2 + szH;
     static constexpr size_t oGate = endA > endB ? endA : endB;
     static constexpr size_t oRed = oGate + 4 * kBackGateRec;
-    // floats behind oRed: [4][64] X_i,-1, [4][64] k.PE, [4][64] column sums of dbeta, [64] X_i,-1
-    // summed, [4] parts of <G, H>
-    static constexpr size_t bytes = oRed + 4 * (12 * 64 + 64 + 4);
+    // floats behind oRed: [4 wave][4 lg][64] parts of X_i,-1, the same of k.PE, [4 row tile][4 lg][64] of
+    // dbeta, [64] X_i,-1, [4] parts of <G, H>
+    static constexpr size_t bytes = oRed + 4 * (48 * 64 + 64 + 4);
 };
 
 template <class E, int DK, int DV>
@@ -775,10 +782,9 @@ void gdn_back_grad_kernel(BackParams<E> p) {
     extern __shared__ __align__(16) unsigned char smem[];
     E *sE = (E *)(smem + L::oE), *sV = (E *)(smem + L::oV), *sO = (E *)(smem + L::oO), *sX = (E *)(smem + L::oX),
       *sG1 = (E *)(smem + L::oG1), *sG2 = (E *)(smem + L::oG2);
-    const double *sg = (const double *)(smem + L::oGate);
     const float *gate = (const float *)(smem + L::oGate);
     const float *gam = gate + kBackGam, *tail = gate + kBackTail, *beta = gate + kBackBeta;
-    float *rX = (float *)(smem + L::oRed), *rE = rX + 4 * 64, *cb = rE + 4 * 64, *xm = cb + 4 * 64, *gh = xm + 64;
+    float *rX = (float *)(smem + L::oRed), *rE = rX + 16 * 64, *cb = rE + 16 * 64, *xm = cb + 16 * 64, *gh = xm + 64;
     const int c = blockIdx.x / (p.B * p.H), bh = blockIdx.x - c * (p.B * p.H);
     const int b = bh / p.H, h = bh - b * p.H;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
@@ -793,14 +799,6 @@ void gdn_back_grad_kernel(BackParams<E> p) {
     // with them meet beta = 0, dO = 0 or dV = 0
     auto rows = [&](const E *base, int r, int kb) {
         return load_frag<E>(base + (row0 + (size_t)min(r, nvalid - 1) * p.H) * DK + 32 * kb, lg);
-    };
-    // fragments of K^T and Q^T: channel ch of tokens 32 kb + 8 lg .. + 7
-    auto columns = [&](const E *base, int ch, int kb) {
-        E x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            x[e] = base[(row0 + (size_t)min(32 * kb + 8 * lg + e, nvalid - 1) * p.H) * DK + ch];
-        return __builtin_bit_cast(frag, x);
     };
     const float *ge = p.eT + cidx * (size_t)(kChunk * DV), *gv = p.vT + cidx * (size_t)(kChunk * DV);
     for (int i = tid; i < kBackGateRec; i += NT) ((float *)(smem + L::oGate))[i] = p.gates[cidx * kBackGateRec + i];
@@ -911,6 +909,33 @@ void gdn_back_grad_kernel(BackParams<E> p) {
         }
     }
     forget();
+    // Row fragments of K and Q for tile n of this wave, and its channels of all tokens, asked
+    // for before they are used (fp32: the second and third tile's where they are used, for want
+    // of registers).
+    constexpr bool AHEAD = sizeof(E) == 2;
+    struct Rows {
+        frag q[DK / 32], k[DK / 32], kj[DK / 32];
+    } ra, rb;
+    auto tile_rows = [&](int n, Rows &x) {
+        int bi, bj;
+        lower_tile(min(w + 4 * n, 9), bi, bj);
+#pragma unroll
+        for (int kb = 0; kb < DK / 32; ++kb) {
+            x.q[kb] = rows(p.q, 16 * bi + li, kb);
+            x.k[kb] = rows(p.k, 16 * bi + li, kb);
+            x.kj[kb] = rows(p.k, 16 * bj + li, kb);
+        }
+    };
+    using own = std::conditional_t<NK == 2, frag, typename TR::quad>;
+    own qo[4], ko[4];
+#pragma unroll
+    for (int rt = 0; rt < 4; ++rt) {
+        const size_t at = (row0 + (size_t)min(16 * rt + li, nvalid - 1) * p.H) * DK + ch0();
+        if constexpr (NK == 2) qo[rt] = TR::load8(p.q + at), ko[rt] = TR::load8(p.k + at);
+        else qo[rt] = TR::load(p.q + at), ko[rt] = TR::load(p.k + at);
+    }
+    if (AHEAD) tile_rows(0, ra);
+    __builtin_amdgcn_sched_barrier(0);
     {
         float s = dot[0] + dot[1] + dot[2] + dot[3];
 #pragma unroll
@@ -925,8 +950,14 @@ void gdn_back_grad_kernel(BackParams<E> p) {
         float x = 0.f, y = 0.f;
 #pragma unroll
         for (int n = 0; n < NK; ++n) {
-            const size_t at = (row0 + (size_t)min(t, nvalid - 1) * p.H) * DK + ch0() + 4 * n;
-            const f32x4 q4 = TR::to_f32(TR::load(p.q + at)), k4 = TR::to_f32(TR::load(p.k + at));
+            f32x4 q4, k4;
+            if constexpr (NK == 2) {
+                q4 = TR::to_f32(n ? TR::hi(qo[rt]) : TR::lo(qo[rt]));
+                k4 = TR::to_f32(n ? TR::hi(ko[rt]) : TR::lo(ko[rt]));
+            } else {
+                q4 = TR::to_f32(qo[rt]);
+                k4 = TR::to_f32(ko[rt]);
+            }
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 x += q4[q] * pq[n][rt][q] - k4[q] * pv[n][rt][q];
@@ -935,22 +966,15 @@ void gdn_back_grad_kernel(BackParams<E> p) {
             pq[n][rt] *= gam[t];
             pe[n][rt] = pe[n][rt] * (tail[t] * beta[t]) - pv[n][rt] * gam[t];
         }
-        x += __shfl_xor(x, 16);
-        x += __shfl_xor(x, 32);
-        y += __shfl_xor(y, 16);
-        y += __shfl_xor(y, 32);
-        if (lg == 0) {
-            rX[w * 64 + t] = x;
-            rE[w * 64 + t] = y;
-        }
+        rX[(w * 4 + lg) * 64 + t] = x;
+        rE[(w * 4 + lg) * 64 + t] = y;
     }
+    if (AHEAD) tile_rows(1, rb);
     lds_barrier();
-    forget();
     // The 64 x 64 matrices: element (i, j) with i = 16 bi + 4 lg + q, j = 16 bj + li.  The six
     // tiles above the diagonal of G1 and X are zero.
-#pragma unroll
-    for (int n = 0; n < NTI; ++n) {
-        if (w + 4 * n >= 10) continue;
+    auto matrices = [&](int n, const Rows &r) {
+        if (w + 4 * n >= 10) return;
         int bi, bj;
         lower_tile(w + 4 * n, bi, bj);
         const int j = 16 * bj + li, i0 = 16 * bi + 4 * lg;
@@ -958,15 +982,14 @@ void gdn_back_grad_kernel(BackParams<E> p) {
         f32x4 sqk = {0.f, 0.f, 0.f, 0.f}, skk = sqk, g1, g2, xx;
 #pragma unroll
         for (int kb = 0; kb < DK / 32; ++kb) {
-            const frag kj = rows(p.k, 16 * bj + li, kb);
-            sqk = TR::mma(rows(p.q, 16 * bi + li, kb), kj, sqk);
-            skk = TR::mma(rows(p.k, 16 * bi + li, kb), kj, skk);
+            sqk = TR::mma(r.q[kb], r.kj[kb], sqk);
+            skk = TR::mma(r.k[kb], r.kj[kb], skk);
         }
         float cs = 0.f;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const int i = i0 + q;
-            const float d = i >= j ? expf((float)(sg[i] - sg[j])) : 0.f;
+            const float d = i >= j ? back_decay(gate, i, j) : 0.f;
             const float dz = d * z[n][q], df = i > j ? d * f[n][q] : 0.f;
             g1[q] = dz * bj_;
             g2[q] = df * bj_;
@@ -987,26 +1010,57 @@ void gdn_back_grad_kernel(BackParams<E> p) {
             WH::store1(sG2 + (i0 + q) * L::LDC + j, L::PC, g2[q]);
             if (bi == bj && i0 + q > j) WH::store1(sG2 + j * L::LDC + i0 + q, L::PC, g2[q]);
         }
-        cs += __shfl_xor(cs, 16);
-        cs += __shfl_xor(cs, 32);
-        if (lg == 0) cb[bi * 64 + j] = cs;
+        cb[(bi * 4 + lg) * 64 + j] = cs;
+    };
+    if (!AHEAD) tile_rows(0, ra);
+    matrices(0, ra);
+    __builtin_amdgcn_sched_barrier(0);
+    if (AHEAD) tile_rows(2, ra);
+    else tile_rows(1, rb);
+    __builtin_amdgcn_sched_barrier(0);
+    matrices(1, rb);
+    __builtin_amdgcn_sched_barrier(0);
+    // K^T and Q^T, as they are, for dQ and dK
+    E kt_[NK][2][8], qt_[NK][2][8];
+    auto columns = [&](const E *base, E (&x)[NK][2][8]) {          // channel of tokens 32 kb + 8 lg .. + 7
+#pragma unroll
+        for (int n = 0; n < NK; ++n)
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    x[n][kb][e] = base[(row0 + (size_t)min(32 * kb + 8 * lg + e, nvalid - 1) * p.H) * DK + channel(n)];
+    };
+    if (AHEAD) {
+        columns(p.k, kt_);
+        columns(p.q, qt_);
+    } else {
+        tile_rows(2, ra);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    matrices(2, ra);
+    __builtin_amdgcn_sched_barrier(0);
+    if (!AHEAD) {
+        columns(p.k, kt_);
+        columns(p.q, qt_);
     }
     lds_barrier();
     forget();
 
-    // Sums over the waves: dbeta, X's border row and column
-    if (tid < 64) {
-        float y = 0.f, x = 0.f;
+    // Sums over the waves: X's border row and column, dbeta
+    if (w == 0) {
+        float x = 0.f;
 #pragma unroll
-        for (int i = 0; i < NW; ++i) {
-            x += rX[i * 64 + tid];
-            y += rE[i * 64 + tid];
-        }
-        xm[tid] = x;
-        float d = tail[tid] * y;
-        for (int bi = tid >> 4; bi < 4; ++bi) d += cb[bi * 64 + tid];
-        if (tid < nvalid) p.dbeta[row0 + (size_t)tid * p.H] = d;
-        WD::store1(sX + tid * L::LDC, L::PC, beta[tid] * y);
+        for (int i = 0; i < 16; ++i) x += rX[i * 64 + l];
+        xm[l] = x;
+    } else if (w == 1) {
+        float y = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) y += rE[i * 64 + l];
+        WD::store1(sX + l * L::LDC, L::PC, beta[l] * y);
+        float d = tail[l] * y;
+        for (int i = l >> 4 << 2; i < 16; ++i) d += cb[i * 64 + l];
+        if (l < nvalid) p.dbeta[row0 + (size_t)l * p.H] = d;
     }
     // dQ += G1 K;  dK += G1^T Q - (G2 + G2^T) K
     {
@@ -1015,8 +1069,8 @@ void gdn_back_grad_kernel(BackParams<E> p) {
         for (int n = 0; n < NK; ++n)
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
-                kt[n][kb] = columns(p.k, channel(n), kb);
-                qt[n][kb] = columns(p.q, channel(n), kb);
+                kt[n][kb] = __builtin_bit_cast(frag, kt_[n][kb]);
+                qt[n][kb] = __builtin_bit_cast(frag, qt_[n][kb]);
             }
 #pragma unroll
         for (int rt = 0; rt < 4; ++rt) {
@@ -1059,7 +1113,7 @@ void gdn_back_grad_kernel(BackParams<E> p) {
     // tokens t of tile w.
     {
         const int t = 16 * w + li;
-        const double gt1 = t > 0 ? sg[t - 1] : 0.0;
+        const float g1hi = t > 0 ? gate[kBackGHi + t - 1] : 0.f, g1lo = t > 0 ? gate[kBackGLo + t - 1] : 0.f;
         wfrag D[2];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
@@ -1068,7 +1122,8 @@ void gdn_back_grad_kernel(BackParams<E> p) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 const int j = 32 * kb + 8 * lg + e;
-                x[e >> 2][e & 3] = j < t ? expf((float)(gt1 - sg[j])) : 0.f;
+                x[e >> 2][e & 3] =
+                    j < t ? __builtin_amdgcn_exp2f((g1hi - gate[kBackGHi + j]) + (g1lo - gate[kBackGLo + j])) : 0.f;
             }
             D[kb] = WD::split(x[0], x[1]);
         }
@@ -1087,7 +1142,7 @@ void gdn_back_grad_kernel(BackParams<E> p) {
             }
 #pragma unroll
             for (int q = 0; q < 4; ++q)
-                if (i0 + q >= t) cs += expf((float)(sg[i0 + q] - sg[t])) * (m[q] + xm[i0 + q] * gb);
+                if (i0 + q >= t) cs += back_decay(gate, i0 + q, t) * (m[q] + xm[i0 + q] * gb);
         }
         cs += __shfl_xor(cs, 16);
         cs += __shfl_xor(cs, 32);
