@@ -600,9 +600,9 @@ __device__ __forceinline__ void back_loader(const BackParams<E> &p, unsigned cha
         rows(i + 2, 0, NKC / 2);
         lds_only_barrier();
         rows(i + 2, NKC / 2, NKC);
+        wait_vmcnt<NKC>();                             // chunk i + 1 is there
         lds_only_barrier();
         rest(i + 2);
-        wait_vmcnt<ALL>();                             // chunk i + 1 is there
         lds_only_barrier();
     }
     wait_vmcnt<0>();
@@ -618,6 +618,7 @@ __device__ __forceinline__ void back_scan(const BackParams<E> &p, unsigned char 
     using RB = RowBlock<E, R>;
     struct Inverse {
         wfrag T[2];
+        typename RB::in k[4];
     };
     const int li = l & 15, lg = l >> 4;
     float *sP = (float *)(smem + L::oP);                          // [wave][token tile][lane][4]
@@ -632,12 +633,19 @@ __device__ __forceinline__ void back_scan(const BackParams<E> &p, unsigned char 
 #pragma unroll
         for (int q = 0; q < 4; ++q) st[a][q] = init ? init[sbase + soff + (4 * a + q) * DV] : 0.f;
     auto chunk = [&](int i) { return REV ? max(p.NC - 1 - i, 0) : min(i, p.NC - 1); };
-    // (the zero blocks of T too, which nothing has written and nothing uses)
+    // (for a zero block of T, which is not used, the other one again)
     auto load = [&](Inverse &o, int c) {
         const E *T = (REV ? p.Tt : p.Tf) + ((size_t)bh * p.NC + c) * (size_t)full_elems<E>(kChunk * kChunk);
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb) o.T[kb] = WD::load8(T + (unsigned)((w * 2 + kb) * 512 + l * 8), kChunk * kChunk);
+        for (int kb = 0; kb < 2; ++kb)
+            o.T[kb] = WD::load8(T + (unsigned)((w * 2 + (REV ? max(kb, w / 2) : min(kb, w / 2))) * 512 + l * 8), kChunk * kChunk);
     };
+    // K's rows for the next chunk, which is in the ring since the barrier before the last, are read
+    // where this chunk's y is on its way, if the workgroup has the CU to itself (103 against 111
+    // us at T = 3520, H = 16, D = 128); where two share it (D = 64) the other one uses that time (253
+    // against 232 us at T = 3520, 80 heads).
+    constexpr bool KAHEAD = L::waves_per_simd == 2;
+    auto rows_of = [&](const E *K, int rt) { return krow<E, DK, R>(K, 16 * rt + li, R * w + R / 4 * lg); };
     // the i-th chunk of this direction
     auto step = [&](const Inverse &o, Inverse &n, int i) {
         const size_t cidx = (size_t)bh * p.NC + chunk(i);
@@ -646,10 +654,10 @@ __device__ __forceinline__ void back_scan(const BackParams<E> &p, unsigned char 
         const E *K = (const E *)slot;
         const float *gate = (const float *)(slot + L::oG) - kBackGam;
         // K X transposed, [column][token]
-        typename RB::in k[4];
-#pragma unroll
-        for (int rt = 0; rt < 4; ++rt) k[rt] = krow<E, DK, R>(K, 16 * rt + li, R * w + R / 4 * lg);
         {
+            typename RB::in k[4];
+#pragma unroll
+            for (int rt = 0; rt < 4; ++rt) k[rt] = KAHEAD ? o.k[rt] : rows_of(K, rt);
             const typename RB::planes H = RB::split(st);
             f32x4 part[4];
 #pragma unroll
@@ -662,9 +670,17 @@ __device__ __forceinline__ void back_scan(const BackParams<E> &p, unsigned char 
         else first = TR::to_f32(TR::load((const E *)(slot + L::oF) + (16 * w + li) * 16 + 4 * lg));
         const float before = REV ? gate[kBackBt + 16 * w + li] : -gate[kBackGam + 16 * w + li];
         lds_only_barrier();
-        f32x4 x = zero;
+        f32x4 xs[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x += *(const f32x4 *)(sP + (j * 4 + w) * 256 + l * 4);
+        for (int j = 0; j < 4; ++j) xs[j] = *(const f32x4 *)(sP + (j * 4 + w) * 256 + l * 4);
+        // The state that entered this chunk, for stage 3: lane (li, lg) stores 4 columns of row
+        // 4 lg + li % 4 of a tile, 1 KB in a row from a wave (a store of 4 bytes a lane takes as
+        // long to issue, and eight of them held up the wave for 700 cycles).
+        float *keep = (REV ? p.Gs : p.Hs) + cidx * (size_t)(DK * DV) +
+                      (unsigned)((jt * DK + R * w + 4 * lg + (li & 3)) * 16 + (li & 12));
+#pragma unroll
+        for (int a = 0; a < NK; ++a) *(f32x4 *)(keep + 256 * a) = quad_transpose(st[a], li);
+        const f32x4 x = (xs[0] + xs[1]) + (xs[2] + xs[3]);
         WD::store4(sX + (16 * w + li) * 16 + 4 * lg, L::PT, first + before * x);
         load(n, chunk(i + 1));
         typename TR::frag kt[NK][2];
@@ -677,22 +693,21 @@ __device__ __forceinline__ void back_scan(const BackParams<E> &p, unsigned char 
         lds_only_barrier();
         f32x4 y[2] = {zero, zero};
 #pragma unroll
+        for (int a = 0; a < NK; ++a) {
+            st[a] *= gC;
+            if constexpr (REV) st[a] += *(const f32x4 *)(slot + L::oA + ((w * NK + a) * 64 + l) * 16);
+        }
+#pragma unroll
         for (int kb = 0; kb < 2; ++kb)
             if (REV ? kb >= w / 2 : kb <= w / 2)                  // T is lower triangular
                 y[kb] = WD::ww(o.T[kb], WD::tr(sX, L::PT, 16, 32 * kb, 0, li, lg), y[kb]);
         y[0] += y[1];
         WD::store4(sY + li * L::LDC + 16 * w + 4 * lg, L::PC, after * y[0]);
         *(f32x4 *)((REV ? p.vT : p.eT) + cidx * (size_t)(kChunk * DV) + (unsigned)((16 * jt + li) * kChunk + 16 * w + 4 * lg)) = y[0];
-        // The state that entered this chunk, for stage 3: lane (li, lg) stores 4 columns of row
-        // 4 lg + li % 4 of a tile, 1 KB in a row from a wave (a store of 4 bytes a lane takes as
-        // long to issue, and eight of them held up the wave for 700 cycles).
-        float *keep = (REV ? p.Gs : p.Hs) + cidx * (size_t)(DK * DV) +
-                      (unsigned)((jt * DK + R * w + 4 * lg + (li & 3)) * 16 + (li & 12));
+        if constexpr (KAHEAD) {
+            const E *Kn = (const E *)(smem + (i + 1) % L::DEPTH * L::SLOT);
 #pragma unroll
-        for (int a = 0; a < NK; ++a) {
-            *(f32x4 *)(keep + 256 * a) = quad_transpose(st[a], li);
-            st[a] *= gC;
-            if constexpr (REV) st[a] += *(const f32x4 *)(slot + L::oA + ((w * NK + a) * 64 + l) * 16);
+            for (int rt = 0; rt < 4; ++rt) n.k[rt] = rows_of(Kn, rt);
         }
         lds_only_barrier();
 #pragma unroll
@@ -708,6 +723,10 @@ __device__ __forceinline__ void back_scan(const BackParams<E> &p, unsigned char 
     // the start of every turn, and the waits there for all loads of the turn before)
     __builtin_amdgcn_s_waitcnt(0x0f70);
     lds_only_barrier();
+    if constexpr (KAHEAD) {
+#pragma unroll
+        for (int rt = 0; rt < 4; ++rt) o0.k[rt] = rows_of((const E *)smem, rt);
+    }
     for (int i = 0; i < p.NC; i += 2) {
         step(o0, o1, i);
         if (i + 1 == p.NC) break;
