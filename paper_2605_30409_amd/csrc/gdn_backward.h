@@ -487,11 +487,12 @@ void gdn_back_prep_kernel(BackParams<E> p) {
 // --------------------------------------------------------------------------
 constexpr int kBackScanWaves = 4, kBackLoadWaves = 2;
 
-template <class E, int DK> struct BackScanLds {
+// DIRECT: the compute waves load first and add themselves, with T.
+template <class E, int DK, bool DIRECT> struct BackScanLds {
     static constexpr int R = DK / 4, NK = R / 16;                             // state rows and row tiles per wave
     static constexpr int LDC = lds_ld<E>(kChunk);
     static constexpr int PT = 16 * kChunk, PC = 16 * LDC;                     // planes
-    static constexpr int szK = (int)sizeof(E) * kChunk * DK, szF = 4096, szA = 4096 * NK;
+    static constexpr int szK = (int)sizeof(E) * kChunk * DK, szF = DIRECT ? 0 : 4096, szA = DIRECT ? 0 : 4096 * NK;
     static constexpr int oF = szK, oA = oF + szF, oG = oA + szA;              // in a slot: K, first, add, gates
     static constexpr int SLOT = oG + 4 * kBackScanGates + 16, DEPTH = 3;
     static constexpr int oP = DEPTH * SLOT;                                   // partial sums of K X
@@ -499,8 +500,10 @@ template <class E, int DK> struct BackScanLds {
     static constexpr int oY = oX + (int)sizeof(E) * Full<E>::planes * PT;     // after y, [column][token]
     static constexpr size_t bytes = oY + sizeof(E) * Full<E>::planes * PC;
     static constexpr int threads = 64 * (kBackScanWaves + kBackLoadWaves);
-    // waves per SIMD of the workgroups that share a CU
-    static constexpr int waves_per_simd = bytes * 2 <= 160 * 1024 ? 3 : 2;
+    // Waves per SIMD: six waves are two on one of the SIMDs, and each workgroup of a CU puts them on
+    // the same one.
+    static constexpr bool shares = bytes * 2 <= 160 * 1024;
+    static constexpr int waves_per_simd = shares ? 4 : 2;
     static_assert(SLOT % 16 == 0 && bytes <= 160 * 1024, "the ring fits the LDS");
 };
 
@@ -543,13 +546,13 @@ __device__ __forceinline__ typename Tr<E>::frag kcols(const E *K, int row0, int 
 }
 
 // The loader waves (part = 0, 1).
-template <class E, int DK, int DV, bool REV>
+template <class E, int DK, int DV, bool REV, bool DIRECT>
 __device__ __forceinline__ void back_loader(const BackParams<E> &p, unsigned char *smem, int bh, int jt, int part, int l) {
-    using L = BackScanLds<E, DK>;
+    using L = BackScanLds<E, DK, DIRECT>;
     constexpr int sz = (int)sizeof(E), GPR = DK * sz / 16, RPC = 64 / GPR;   // granules per K row, rows per copy
     constexpr int NKC = L::szK / 2048;                                       // copies of K per wave
     constexpr int GPV = sz, RPV = 64 / GPV;                                  // granules per row of 16 columns of V
-    constexpr int NF = REV ? 2 : sz / 2, NA = REV ? L::szA / 2048 : 0;       // of first and add per wave
+    constexpr int NF = DIRECT ? 0 : REV ? 2 : sz / 2, NA = REV ? L::szA / 2048 : 0;   // of first and add per wave
     constexpr int ALL = NKC + NF + NA + 1;
     const int b = bh / p.H, h = bh - b * p.H;
     const size_t head = (size_t)b * p.T * p.H + h;
@@ -608,22 +611,25 @@ __device__ __forceinline__ void back_loader(const BackParams<E> &p, unsigned cha
     wait_vmcnt<0>();
 }
 
-template <class E, int DK, int DV, bool REV>
+template <class E, int DK, int DV, bool REV, bool DIRECT>
 __device__ __forceinline__ void back_scan(const BackParams<E> &p, unsigned char *smem, int bh, int jt, int w, int l) {
-    using L = BackScanLds<E, DK>;
+    using L = BackScanLds<E, DK, DIRECT>;
     using TR = Tr<E>;
     using WD = Full<E>;
     using wfrag = typename WD::frag;
     constexpr int R = L::R, NK = L::NK;
     using RB = RowBlock<E, R>;
-    struct Inverse {
+    struct Ahead {
         wfrag T[2];
         typename RB::in k[4];
+        f32x4 n0, add[NK];
+        typename TR::quad v;
     };
     const int li = l & 15, lg = l >> 4;
     float *sP = (float *)(smem + L::oP);                          // [wave][token tile][lane][4]
     E *sX = (E *)(smem + L::oX), *sY = (E *)(smem + L::oY);
     const float *init = REV ? p.dstate_out : p.state_in;
+    const size_t head = (size_t)(bh / p.H) * p.T * p.H + bh % p.H;
     // element (R w + R / 4 lg + 4 a + q, 16 jt + li) is st[a][q]
     const size_t sbase = (size_t)bh * DK * DV;
     const unsigned soff = (R * w + R / 4 * lg) * DV + 16 * jt + li;
@@ -634,20 +640,32 @@ __device__ __forceinline__ void back_scan(const BackParams<E> &p, unsigned char 
         for (int q = 0; q < 4; ++q) st[a][q] = init ? init[sbase + soff + (4 * a + q) * DV] : 0.f;
     auto chunk = [&](int i) { return REV ? max(p.NC - 1 - i, 0) : min(i, p.NC - 1); };
     // (for a zero block of T, which is not used, the other one again)
-    auto load = [&](Inverse &o, int c) {
+    Ahead o;
+    auto load = [&](int c) {
         const E *T = (REV ? p.Tt : p.Tf) + ((size_t)bh * p.NC + c) * (size_t)full_elems<E>(kChunk * kChunk);
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
             o.T[kb] = WD::load8(T + (unsigned)((w * 2 + (REV ? max(kb, w / 2) : min(kb, w / 2))) * 512 + l * 8), kChunk * kChunk);
+        if constexpr (DIRECT && REV) {
+            const size_t cidx = (size_t)bh * p.NC + c;
+            o.n0 = *(const f32x4 *)(p.N0 + cidx * (size_t)(kChunk * DV) + (unsigned)((jt * 4 + w) * 256 + l * 4));
+#pragma unroll
+            for (int a = 0; a < NK; ++a)
+                o.add[a] = *(const f32x4 *)(p.C0 + cidx * (size_t)(DK * DV) + (unsigned)(((jt * 4 + w) * NK + a) * 256 + l * 4));
+        } else if constexpr (DIRECT) {
+            const int last = min(kChunk, p.T - c * kChunk) - 1;
+            o.v = TR::load(p.v + (head + (size_t)c * kChunk * p.H) * DV +
+                           (unsigned)(min(16 * w + li, last) * p.H * DV + 16 * jt + 4 * lg));
+        }
     };
     // K's rows for the next chunk, which is in the ring since the barrier before the last, are read
     // where this chunk's y is on its way, if the workgroup has the CU to itself (103 against 111
     // us at T = 3520, H = 16, D = 128); where two share it (D = 64) the other one uses that time (253
     // against 232 us at T = 3520, 80 heads).
-    constexpr bool KAHEAD = L::waves_per_simd == 2;
+    constexpr bool KAHEAD = !L::shares;
     auto rows_of = [&](const E *K, int rt) { return krow<E, DK, R>(K, 16 * rt + li, R * w + R / 4 * lg); };
     // the i-th chunk of this direction
-    auto step = [&](const Inverse &o, Inverse &n, int i) {
+    auto step = [&](int i) {
         const size_t cidx = (size_t)bh * p.NC + chunk(i);
         const f32x4 zero = {0.f, 0.f, 0.f, 0.f};
         const unsigned char *slot = smem + i % L::DEPTH * L::SLOT;
@@ -666,7 +684,9 @@ __device__ __forceinline__ void back_scan(const BackParams<E> &p, unsigned char 
             for (int rt = 0; rt < 4; ++rt) *(f32x4 *)(sP + (w * 4 + rt) * 256 + l * 4) = part[rt];
         }
         f32x4 first;
-        if constexpr (REV) first = *(const f32x4 *)(slot + L::oF + (w * 64 + l) * 16);
+        if constexpr (DIRECT && REV) first = o.n0;
+        else if constexpr (DIRECT) first = TR::to_f32(o.v);
+        else if constexpr (REV) first = *(const f32x4 *)(slot + L::oF + (w * 64 + l) * 16);
         else first = TR::to_f32(TR::load((const E *)(slot + L::oF) + (16 * w + li) * 16 + 4 * lg));
         const float before = REV ? gate[kBackBt + 16 * w + li] : -gate[kBackGam + 16 * w + li];
         lds_only_barrier();
@@ -682,7 +702,6 @@ __device__ __forceinline__ void back_scan(const BackParams<E> &p, unsigned char 
         for (int a = 0; a < NK; ++a) *(f32x4 *)(keep + 256 * a) = quad_transpose(st[a], li);
         const f32x4 x = (xs[0] + xs[1]) + (xs[2] + xs[3]);
         WD::store4(sX + (16 * w + li) * 16 + 4 * lg, L::PT, first + before * x);
-        load(n, chunk(i + 1));
         typename TR::frag kt[NK][2];
 #pragma unroll
         for (int a = 0; a < NK; ++a)
@@ -695,19 +714,21 @@ __device__ __forceinline__ void back_scan(const BackParams<E> &p, unsigned char 
 #pragma unroll
         for (int a = 0; a < NK; ++a) {
             st[a] *= gC;
-            if constexpr (REV) st[a] += *(const f32x4 *)(slot + L::oA + ((w * NK + a) * 64 + l) * 16);
+            if constexpr (DIRECT && REV) st[a] += o.add[a];
+            else if constexpr (REV) st[a] += *(const f32x4 *)(slot + L::oA + ((w * NK + a) * 64 + l) * 16);
         }
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
             if (REV ? kb >= w / 2 : kb <= w / 2)                  // T is lower triangular
                 y[kb] = WD::ww(o.T[kb], WD::tr(sX, L::PT, 16, 32 * kb, 0, li, lg), y[kb]);
+        load(chunk(i + 1));
         y[0] += y[1];
         WD::store4(sY + li * L::LDC + 16 * w + 4 * lg, L::PC, after * y[0]);
         *(f32x4 *)((REV ? p.vT : p.eT) + cidx * (size_t)(kChunk * DV) + (unsigned)((16 * jt + li) * kChunk + 16 * w + 4 * lg)) = y[0];
         if constexpr (KAHEAD) {
             const E *Kn = (const E *)(smem + (i + 1) % L::DEPTH * L::SLOT);
 #pragma unroll
-            for (int rt = 0; rt < 4; ++rt) n.k[rt] = rows_of(Kn, rt);
+            for (int rt = 0; rt < 4; ++rt) o.k[rt] = rows_of(Kn, rt);
         }
         lds_only_barrier();
 #pragma unroll
@@ -717,21 +738,16 @@ __device__ __forceinline__ void back_scan(const BackParams<E> &p, unsigned char 
             for (int a = 0; a < NK; ++a) st[a] = WD::ew(kt[a][kb], u, st[a]);
         }
     };
-    Inverse o0, o1;
-    load(o0, chunk(0));
+    load(chunk(0));
     // (vmcnt(0): loads pending from before the loop would be taken for pending at
     // the start of every turn, and the waits there for all loads of the turn before)
     __builtin_amdgcn_s_waitcnt(0x0f70);
     lds_only_barrier();
     if constexpr (KAHEAD) {
 #pragma unroll
-        for (int rt = 0; rt < 4; ++rt) o0.k[rt] = rows_of((const E *)smem, rt);
+        for (int rt = 0; rt < 4; ++rt) o.k[rt] = rows_of((const E *)smem, rt);
     }
-    for (int i = 0; i < p.NC; i += 2) {
-        step(o0, o1, i);
-        if (i + 1 == p.NC) break;
-        step(o1, o0, i + 1);
-    }
+    for (int i = 0; i < p.NC; ++i) step(i);
     if (REV && p.dstate_in) {
 #pragma unroll
         for (int a = 0; a < NK; ++a)
@@ -740,9 +756,9 @@ __device__ __forceinline__ void back_scan(const BackParams<E> &p, unsigned char 
     }
 }
 
-template <class E, int DK, int DV>
-__global__ __launch_bounds__((BackScanLds<E, DK>::threads))
-__attribute__((amdgpu_waves_per_eu(BackScanLds<E, DK>::waves_per_simd)))
+template <class E, int DK, int DV, bool DIRECT>
+__global__ __launch_bounds__((BackScanLds<E, DK, DIRECT>::threads))
+__attribute__((amdgpu_waves_per_eu(BackScanLds<E, DK, DIRECT>::waves_per_simd)))
 void gdn_back_scan_kernel(BackParams<E> p) {
     extern __shared__ __align__(16) unsigned char smem[];
     // the column tiles of a head share its operands: they get the same XCD
@@ -751,11 +767,11 @@ void gdn_back_scan_kernel(BackParams<E> p) {
     if (bh >= p.B * p.H) return;
     const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
     if (w >= kBackScanWaves) {
-        if (blockIdx.y == 0) back_loader<E, DK, DV, false>(p, smem, bh, jt, w - kBackScanWaves, l);
-        else back_loader<E, DK, DV, true>(p, smem, bh, jt, w - kBackScanWaves, l);
+        if (blockIdx.y == 0) back_loader<E, DK, DV, false, DIRECT>(p, smem, bh, jt, w - kBackScanWaves, l);
+        else back_loader<E, DK, DV, true, DIRECT>(p, smem, bh, jt, w - kBackScanWaves, l);
     } else {
-        if (blockIdx.y == 0) back_scan<E, DK, DV, false>(p, smem, bh, jt, w, l);
-        else back_scan<E, DK, DV, true>(p, smem, bh, jt, w, l);
+        if (blockIdx.y == 0) back_scan<E, DK, DV, false, DIRECT>(p, smem, bh, jt, w, l);
+        else back_scan<E, DK, DV, true, DIRECT>(p, smem, bh, jt, w, l);
     }
 }
 

@@ -170,7 +170,11 @@ bool back_shape_ok(int B, int H, int T) {
 
 template <class E, int DK, int DV> int launch_backward(const gdn::BackParams<E> &p, hipStream_t s) {
     using P = gdn::PrepLds<E, DK, DV>;
-    using S = gdn::BackScanLds<E, DK>;
+    // bf16, Dk = 128: a workgroup of the scan that brings all its operands through LDS has a CU
+    // to itself; with first and add loaded directly two share one.
+    constexpr bool SHARE = sizeof(E) == 2 && DK == 128;
+    using S = gdn::BackScanLds<E, DK, false>;
+    using D = gdn::BackScanLds<E, DK, SHARE>;
     using G = gdn::GradLds<E>;
     static std::once_flag once;
     static hipError_t attr = hipSuccess;
@@ -179,7 +183,8 @@ template <class E, int DK, int DV> int launch_backward(const gdn::BackParams<E> 
             const void *fn;
             size_t bytes;
         } dyn[] = {{(const void *)gdn::gdn_back_prep_kernel<E, DK, DV>, P::bytes},
-                   {(const void *)gdn::gdn_back_scan_kernel<E, DK, DV>, S::bytes},
+                   {(const void *)gdn::gdn_back_scan_kernel<E, DK, DV, false>, S::bytes},
+                   {(const void *)gdn::gdn_back_scan_kernel<E, DK, DV, SHARE>, D::bytes},
                    {(const void *)gdn::gdn_back_grad_kernel<E, DK, DV>, G::bytes}};
         for (const auto &d : dyn)
             if (attr == hipSuccess)
@@ -188,9 +193,11 @@ template <class E, int DK, int DV> int launch_backward(const gdn::BackParams<E> 
     if (attr != hipSuccess) return GDN_ERR_HIP;
     const unsigned bh = (unsigned)(p.B * p.H), n = bh * (unsigned)p.NC;
     int st = launch(gdn::gdn_back_prep_kernel<E, DK, DV>, dim3(n), dim3(64 * gdn::kPrepWaves), P::bytes, s, p);
-    if (st == GDN_OK)
-        st = launch(gdn::gdn_back_scan_kernel<E, DK, DV>, dim3((bh + 7) / 8 * 8 * (DV / 16), 2),
-                    dim3(S::threads), S::bytes, s, p);
+    const dim3 tiles((bh + 7) / 8 * 8 * (DV / 16), 2);
+    if (st == GDN_OK && SHARE && 2LL * bh * (DV / 16) > 256)
+        st = launch(gdn::gdn_back_scan_kernel<E, DK, DV, SHARE>, tiles, dim3(D::threads), D::bytes, s, p);
+    else if (st == GDN_OK)
+        st = launch(gdn::gdn_back_scan_kernel<E, DK, DV, false>, tiles, dim3(S::threads), S::bytes, s, p);
     if (st == GDN_OK)
         st = launch(gdn::gdn_back_grad_kernel<E, DK, DV>, dim3(n), dim3(64 * gdn::kGradWaves), G::bytes, s, p);
     return st;
