@@ -43,7 +43,7 @@ extern "C" {
  * that row is written.  A slot >= P, or one that an earlier row names already,
  * is refused on the device: the row's out (up to its length) becomes NaN and
  * no state is written for it; the first row that names a slot has it.
- * Dk, Dv in {64, 128}.  The call needs no workspace and may be captured.
+ * N, L, P, Hk, H >= 1; Dk, Dv in {64, 128}.  The call needs no workspace and may be captured.
  */
 int gdn_step_forward(const void *q, const void *k, const void *v, const float *alpha, const float *beta,
                      const float *state_in, const int *slots, const int *lengths, void *out,

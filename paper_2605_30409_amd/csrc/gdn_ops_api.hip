@@ -88,18 +88,18 @@ struct Strips {
 };
 
 Strips norm_strips(int R, int gate_tokens) {
-    int rows = (R + 511) / 512;
+    const int rows = (R - 1) / 512 + 1;
     Strips t;
     if (gate_tokens > rows) {             // a gate row spans strips: partial sums for dgate
-        t.per_unit = (gate_tokens + rows - 1) / rows;
-        t.strip_rows = (gate_tokens + t.per_unit - 1) / t.per_unit;
-        t.per_unit = (gate_tokens + t.strip_rows - 1) / t.strip_rows;
+        t.per_unit = (gate_tokens - 1) / rows + 1;
+        t.strip_rows = (gate_tokens - 1) / t.per_unit + 1;
+        t.per_unit = (gate_tokens - 1) / t.strip_rows + 1;
         t.unit_rows = gate_tokens;
         t.strips = R / gate_tokens * t.per_unit;
     } else {                              // strips of whole gate rows
         t.per_unit = 1;
         t.strip_rows = t.unit_rows = rows / gate_tokens * gate_tokens;
-        t.strips = (R + t.strip_rows - 1) / t.strip_rows;
+        t.strips = (R - 1) / t.strip_rows + 1;
     }
     return t;
 }
@@ -331,8 +331,8 @@ int gdn_block_norm_forward(const void *x, const void *y, const void *gate, const
         p.R = R;
         p.C = C;
         p.gate_tokens = gate_tokens;
-        p.strip_rows = (R + 2047) / 2048;
-        p.strips = (R + p.strip_rows - 1) / p.strip_rows;
+        p.strip_rows = (R - 1) / 2048 + 1;
+        p.strips = (R - 1) / p.strip_rows + 1;
         p.res_scale = res_scale;
         p.eps = eps;
         return dispatch_norm<E>(p, false, (hipStream_t)stream);

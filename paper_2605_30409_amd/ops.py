@@ -52,10 +52,18 @@ def _call(name, dev, *args):
         raise GdnError(name, rc)
 
 
+def _needs(dev, *specs):
+    """_need for each (name, tensor, shape, dtype); one condition where nothing is wrong, since
+    a small call is as long as its checks."""
+    index = dev.index
+    for name, t, shape, dtype in specs:
+        if type(t) is torch.Tensor and t.dtype is dtype and t.get_device() == index and t.shape == shape \
+                and t.is_contiguous():
+            continue
+        _need(name, t, shape, dtype, dev)
+
+
 def _need(name, t, shape, dtype, dev):
-    # one condition for the call that is right: a small call is as long as its checks
-    if type(t) is torch.Tensor and t.dtype is dtype and t.shape == shape and t.device == dev and t.is_contiguous():
-        return
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a tensor, got {type(t).__name__}")
     if t.dtype != dtype:
@@ -66,6 +74,13 @@ def _need(name, t, shape, dtype, dev):
         raise ValueError(f"{name} must be on {dev}, got {t.device}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
+
+
+def _on(stream, t):
+    """Context of a call on `stream`, which has to be one of the tensors' device."""
+    if isinstance(t, torch.Tensor) and t.device.type == "cuda" and stream.device != t.device:
+        raise ValueError(f"stream must be on {t.device}, got {stream.device}")
+    return torch.cuda.stream(stream)
 
 
 def _element(name, t):
@@ -79,9 +94,10 @@ def _element(name, t):
 
 
 def _dims(name, t, dims, text):
-    if t.dim() != dims:
-        raise ValueError(f"{name} must be {text}, got {list(t.shape)}")
-    return tuple(t.shape)
+    shape = t.shape if isinstance(t, torch.Tensor) else ()
+    if len(shape) != dims:
+        raise ValueError(f"{name} must be {text}, got {list(shape)}")
+    return shape
 
 
 def step(q, k, v, alpha, beta, state, *, slots=None, lengths=None, out=None, state_out=None, stream=None):
@@ -98,32 +114,29 @@ def step(q, k, v, alpha, beta, state, *, slots=None, lengths=None, out=None, sta
     that is allocated here is zero there).  A slot beyond the pool, or named by an earlier row too,
     makes the row's out NaN and writes no state.  Returns (out [N, L, H, Dv] like v, state_out)."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream, q):
             return step(q, k, v, alpha, beta, state, slots=slots, lengths=lengths, out=out, state_out=state_out)
     dt, dev = _element("q", q)
     N, L, Hk, Dk = _dims("q", q, 4, "[N, L, Hk, Dk]")
     H, Dv = _dims("v", v, 4, "[N, L, H, Dv]")[2:]
     P = _dims("state", state, 4, "[P, H, Dk, Dv]")[0]
-    _need("q", q, (N, L, Hk, Dk), dt, dev)
-    _need("k", k, (N, L, Hk, Dk), dt, dev)
-    _need("v", v, (N, L, H, Dv), dt, dev)
-    _need("alpha", alpha, (N, L, H), torch.float32, dev)
-    _need("beta", beta, (N, L, H), torch.float32, dev)
-    _need("state", state, (P, H, Dk, Dv), torch.float32, dev)
+    f32, keys, gates = torch.float32, (N, L, Hk, Dk), (N, L, H)
+    _needs(dev, ("q", q, keys, dt), ("k", k, keys, dt), ("v", v, (N, L, H, Dv), dt), ("alpha", alpha, gates, f32),
+           ("beta", beta, gates, f32), ("state", state, (P, H, Dk, Dv), f32))
     if slots is not None:
-        _need("slots", slots, (N,), torch.int32, dev)
+        _needs(dev, ("slots", slots, (N,), torch.int32))
     if lengths is not None:
-        _need("lengths", lengths, (N,), torch.int32, dev)
+        _needs(dev, ("lengths", lengths, (N,), torch.int32))
     if out is None:
         # every element is written unless a row may be short or padding
         new = torch.empty if slots is None and lengths is None else torch.zeros
         out = new((N, L, H, Dv), dtype=dt, device=dev)
     else:
-        _need("out", out, (N, L, H, Dv), dt, dev)
+        _needs(dev, ("out", out, (N, L, H, Dv), dt))
     if state_out is None:
         state_out = state
     else:
-        _need("state_out", state_out, (P, H, Dk, Dv), torch.float32, dev)
+        _needs(dev, ("state_out", state_out, (P, H, Dk, Dv), f32))
     _call("gdn_step_forward", dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), alpha.data_ptr(), beta.data_ptr(),
           state.data_ptr(), _ptr(slots), _ptr(lengths), out.data_ptr(), state_out.data_ptr(), N, L, P, Hk, H, Dk, Dv,
           1 if dt == torch.bfloat16 else 0)
@@ -147,20 +160,19 @@ def backward(q, k, v, alpha, beta, state_in, dout, dstate_out=None, *, dq=None, 
     dstate_in may be dstate_out.  Returns (dq, dk, dv like q, dalpha, dbeta [B, T, H] fp32,
     dstate_in [B, H, Dk, Dv] fp32, or None without want_dstate)."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream, q):
             return backward(q, k, v, alpha, beta, state_in, dout, dstate_out, dq=dq, dk=dk, dv=dv, dalpha=dalpha,
                             dbeta=dbeta, dstate_in=dstate_in, want_dstate=want_dstate, ws=ws, chunk=chunk)
     dt, dev = _element("q", q)
     B, T, H, Dk = _dims("q", q, 4, "[B, T, H, Dk]")
     Dv = _dims("v", v, 4, "[B, T, H, Dv]")[3]
     f32 = torch.float32
-    for name, t, last in (("q", q, Dk), ("k", k, Dk), ("v", v, Dv), ("dout", dout, Dv)):
-        _need(name, t, (B, T, H, last), dt, dev)
-    _need("alpha", alpha, (B, T, H), f32, dev)
-    _need("beta", beta, (B, T, H), f32, dev)
+    keys, values, gates = (B, T, H, Dk), (B, T, H, Dv), (B, T, H)
+    _needs(dev, ("q", q, keys, dt), ("k", k, keys, dt), ("v", v, values, dt), ("dout", dout, values, dt),
+           ("alpha", alpha, gates, f32), ("beta", beta, gates, f32))
     for name, t in (("state_in", state_in), ("dstate_out", dstate_out)):
         if t is not None:
-            _need(name, t, (B, H, Dk, Dv), f32, dev)
+            _needs(dev, (name, t, (B, H, Dk, Dv), f32))
     dq = _given("dq", dq, (B, T, H, Dk), dt, dev)
     dk = _given("dk", dk, (B, T, H, Dk), dt, dev)
     dv = _given("dv", dv, (B, T, H, Dv), dt, dev)
@@ -193,19 +205,17 @@ def _block_inputs(x, y, gate, w_post, w_pre, gate_tokens):
     gt = int(gate_tokens)
     if gt < 1 or T % gt:
         raise ValueError("T must be a whole number of runs of gate_tokens tokens")
-    _need("x", x, (B, T, C), dt, dev)
-    _need("y", y, (B, T, C), dt, dev)
+    f32 = torch.float32
+    _needs(dev, ("x", x, (B, T, C), dt), ("y", y, (B, T, C), dt), ("w_post", w_post, (C,), f32), ("w_pre", w_pre, (C,), f32))
     if gate is not None:
-        _need("gate", gate, (B, T // gt, C), dt, dev)
-    _need("w_post", w_post, (C,), torch.float32, dev)
-    _need("w_pre", w_pre, (C,), torch.float32, dev)
+        _needs(dev, ("gate", gate, (B, T // gt, C), dt))
     return dt, dev, B, T, C, gt
 
 
 def _given(name, t, shape, dtype, dev):
     if t is None:
         return torch.empty(shape, dtype=dtype, device=dev)
-    _need(name, t, shape, dtype, dev)
+    _needs(dev, (name, t, shape, dtype))
     return t
 
 
@@ -220,7 +230,7 @@ def block_norm(x, y, gate, w_post, w_pre, *, gate_tokens=1, res_scale=1.0, eps=1
     fp32; C at most 8192.  r (the next residual stream) and u (the next block's
     input) are allocated unless given; r may be x or y, u may be y.  Returns (r, u)."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream, x):
             return block_norm(x, y, gate, w_post, w_pre, gate_tokens=gate_tokens, res_scale=res_scale, eps=eps, r=r, u=u)
     dt, dev, B, T, C, gt = _block_inputs(x, y, gate, w_post, w_pre, gate_tokens)
     r = _given("r", r, (B, T, C), dt, dev)
@@ -237,13 +247,13 @@ def block_norm_backward(x, y, gate, w_post, w_pre, du, dr=None, *, gate_tokens=1
     may be y or the other of them.  Returns (dx, dy, dgate, dw_post, dw_pre); dgate is
     None where gate is."""
     if stream is not None:
-        with torch.cuda.stream(stream):
+        with _on(stream, x):
             return block_norm_backward(x, y, gate, w_post, w_pre, du, dr, gate_tokens=gate_tokens, res_scale=res_scale,
                                        eps=eps, dx=dx, dy=dy, dgate=dgate, dw_post=dw_post, dw_pre=dw_pre, ws=ws)
     dt, dev, B, T, C, gt = _block_inputs(x, y, gate, w_post, w_pre, gate_tokens)
-    _need("du", du, (B, T, C), dt, dev)
+    _needs(dev, ("du", du, (B, T, C), dt))
     if dr is not None:
-        _need("dr", dr, (B, T, C), dt, dev)
+        _needs(dev, ("dr", dr, (B, T, C), dt))
     dx = _given("dx", dx, (B, T, C), dt, dev)
     dy = _given("dy", dy, (B, T, C), dt, dev)
     if gate is not None:

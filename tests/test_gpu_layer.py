@@ -76,3 +76,24 @@ def test_layer_decodes_as_it_prefills(gdn):
         y, _ = gdn.step(*(x[:, i:i + 1].contiguous() for x in seq), pool, slots=slots)
         _, u = gdn.block_norm(t["x"][:, i:i + 1].contiguous(), y.view(B, 1, H * D), None, *w)
         assert float((u[:, 0] - whole[:, i]).abs().max()) <= 2e-4 * float(whole.abs().max()), i
+
+
+def test_calls_on_two_streams_at_once(gdn):
+    """Each call has a workspace of its own: gradients that run beside each other keep their bits."""
+    import torch
+    a, b = inputs(2, 700, 3, 64, 3), inputs(2, 700, 3, 64, 4)
+
+    def run(t, stream=None):
+        dout = t["du"].view(t["v"].shape)
+        g = gdn.backward(t["q"], t["k"], t["v"], t["alpha"], t["beta"], None, dout, stream=stream)
+        n = gdn.block_norm_backward(t["x"], t["du"], t["gate"], t["w_post"], t["w_pre"], t["x"], gate_tokens=350,
+                                    stream=stream)
+        return g + n
+    ref = run(a), run(b)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream(), torch.cuda.Stream()
+    for _ in range(3):
+        got = run(a, s[0]), run(b, s[1])
+        torch.cuda.synchronize()
+        for x, y in zip(got, ref):
+            assert all(torch.equal(p, q) for p, q in zip(x, y))
