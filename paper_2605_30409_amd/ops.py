@@ -40,14 +40,22 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _raw_stream(index):
+    return torch.cuda.current_stream(index).cuda_stream
+
+
+# (the handle alone: the stream object around it takes as long to make as a launch)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _raw_stream)
+
+
 def _call(name, dev, *args):
     """The C call with the current stream of `dev` behind its other arguments."""
     fn = getattr(_lib(), name)
     if torch.cuda.current_device() == dev.index:
-        rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+        rc = fn(*args, _raw_stream(dev.index))
     else:
         with torch.cuda.device(dev):
-            rc = fn(*args, torch.cuda.current_stream().cuda_stream)
+            rc = fn(*args, _raw_stream(dev.index))
     if rc != GDN_OK:
         raise GdnError(name, rc)
 
@@ -129,8 +137,7 @@ def step(q, k, v, alpha, beta, state, *, slots=None, lengths=None, out=None, sta
         _needs(dev, ("lengths", lengths, (N,), torch.int32))
     if out is None:
         # every element is written unless a row may be short or padding
-        new = torch.empty if slots is None and lengths is None else torch.zeros
-        out = new((N, L, H, Dv), dtype=dt, device=dev)
+        out = torch.empty_like(v) if slots is None and lengths is None else torch.zeros_like(v)
     else:
         _needs(dev, ("out", out, (N, L, H, Dv), dt))
     if state_out is None:
@@ -173,13 +180,15 @@ def backward(q, k, v, alpha, beta, state_in, dout, dstate_out=None, *, dq=None, 
     for name, t in (("state_in", state_in), ("dstate_out", dstate_out)):
         if t is not None:
             _needs(dev, (name, t, (B, H, Dk, Dv), f32))
-    dq = _given("dq", dq, (B, T, H, Dk), dt, dev)
-    dk = _given("dk", dk, (B, T, H, Dk), dt, dev)
-    dv = _given("dv", dv, (B, T, H, Dv), dt, dev)
-    dalpha = _given("dalpha", dalpha, (B, T, H), f32, dev)
-    dbeta = _given("dbeta", dbeta, (B, T, H), f32, dev)
-    if want_dstate or dstate_in is not None:
-        dstate_in = _given("dstate_in", dstate_in, (B, H, Dk, Dv), f32, dev)
+    dq = _given("dq", dq, q)
+    dk = _given("dk", dk, k)
+    dv = _given("dv", dv, v)
+    dalpha = _given("dalpha", dalpha, alpha)
+    dbeta = _given("dbeta", dbeta, beta)
+    if dstate_in is not None:
+        _needs(dev, ("dstate_in", dstate_in, (B, H, Dk, Dv), f32))
+    elif want_dstate:
+        dstate_in = torch.empty((B, H, Dk, Dv), dtype=f32, device=dev)
     if ws is None:
         ws = backward_workspace(q, v, chunk)
     elif ws.device != dev or ws.dtype != torch.uint8 or not ws.is_contiguous():
@@ -212,10 +221,11 @@ def _block_inputs(x, y, gate, w_post, w_pre, gate_tokens):
     return dt, dev, B, T, C, gt
 
 
-def _given(name, t, shape, dtype, dev):
+def _given(name, t, like):
+    """An output: the one given, checked, or a new one like another tensor of the call."""
     if t is None:
-        return torch.empty(shape, dtype=dtype, device=dev)
-    _needs(dev, (name, t, shape, dtype))
+        return torch.empty_like(like)
+    _needs(like.device, (name, t, like.shape, like.dtype))
     return t
 
 
@@ -233,8 +243,8 @@ def block_norm(x, y, gate, w_post, w_pre, *, gate_tokens=1, res_scale=1.0, eps=1
         with _on(stream, x):
             return block_norm(x, y, gate, w_post, w_pre, gate_tokens=gate_tokens, res_scale=res_scale, eps=eps, r=r, u=u)
     dt, dev, B, T, C, gt = _block_inputs(x, y, gate, w_post, w_pre, gate_tokens)
-    r = _given("r", r, (B, T, C), dt, dev)
-    u = _given("u", u, (B, T, C), dt, dev)
+    r = _given("r", r, x)
+    u = _given("u", u, x)
     _call("gdn_block_norm_forward", dev, x.data_ptr(), y.data_ptr(), _ptr(gate), w_post.data_ptr(), w_pre.data_ptr(),
           r.data_ptr(), u.data_ptr(), B * T, C, gt, float(res_scale), float(eps), 1 if dt == torch.bfloat16 else 0)
     return r, u
@@ -254,14 +264,14 @@ def block_norm_backward(x, y, gate, w_post, w_pre, du, dr=None, *, gate_tokens=1
     _needs(dev, ("du", du, (B, T, C), dt))
     if dr is not None:
         _needs(dev, ("dr", dr, (B, T, C), dt))
-    dx = _given("dx", dx, (B, T, C), dt, dev)
-    dy = _given("dy", dy, (B, T, C), dt, dev)
+    dx = _given("dx", dx, x)
+    dy = _given("dy", dy, y)
     if gate is not None:
-        dgate = _given("dgate", dgate, (B, T // gt, C), dt, dev)
+        dgate = _given("dgate", dgate, gate)
     elif dgate is not None:
         raise ValueError("dgate without gate")
-    dw_post = _given("dw_post", dw_post, (C,), torch.float32, dev)
-    dw_pre = _given("dw_pre", dw_pre, (C,), torch.float32, dev)
+    dw_post = _given("dw_post", dw_post, w_post)
+    dw_pre = _given("dw_pre", dw_pre, w_pre)
     if ws is None:
         ws = block_norm_workspace(B * T, C, gt, dev)
     elif ws.device != dev or ws.dtype != torch.uint8 or not ws.is_contiguous():
