@@ -43,7 +43,8 @@ extern "C" {
  * that row is written.  A slot >= P, or one that an earlier row names already,
  * is refused on the device: the row's out (up to its length) becomes NaN and
  * no state is written for it; the first row that names a slot has it.
- * N, L, P, Hk, H >= 1; Dk, Dv in {64, 128}.  The call needs no workspace and may be captured.
+ * N, L, P, Hk, H >= 1, N H < 2^24; Dk, Dv in {64, 128}.  The call needs no workspace and may
+ * be captured.
  */
 int gdn_step_forward(const void *q, const void *k, const void *v, const float *alpha, const float *beta,
                      const float *state_in, const int *slots, const int *lengths, void *out,
@@ -66,7 +67,8 @@ int gdn_step_forward(const void *q, const void *k, const void *v, const float *a
  * and their gradients are fp32, and on the bf16 path too the operands of products
  * that lead to fp32 results keep fp32's mantissa.  Results are deterministic.
  *
- * Outputs may not overlap inputs or each other, except dstate_in == dstate_out.
+ * B H <= 65535, and B H chunks < 2^23.  Outputs may not overlap inputs or each other,
+ * except dstate_in == dstate_out.
  * `ws`: caller-owned device buffer, 256-byte aligned, of at least
  * gdn_chunk_backward_workspace_bytes(...) bytes (0 for arguments that the call
  * refuses; 338 KB a chunk and head at Dk = Dv = 128).  Calls that run at once need

@@ -163,9 +163,9 @@ BackWs back_layout(int B, int H, int T, int Dk, int Dv, size_t esz) {
 }
 
 bool back_shape_ok(int B, int H, int T) {
-    // the launches' grids: chunks x heads below 2^31
+    // a launch has fewer than 2^32 threads; prep has 512 a chunk and head, the scan 6144 a head
     return B >= 1 && H >= 1 && T >= 1 && (long long)B * H <= 65535 &&
-           (long long)B * H * ((T + (long long)gdn::kChunk - 1) / gdn::kChunk) < (1LL << 31);
+           (long long)B * H * ((T + (long long)gdn::kChunk - 1) / gdn::kChunk) < (1LL << 23);
 }
 
 template <class E, int DK, int DV> int launch_backward(const gdn::BackParams<E> &p, hipStream_t s) {
@@ -284,7 +284,7 @@ int gdn_step_forward(const void *q, const void *k, const void *v, const float *a
                      void *stream) {
     if (!q || !k || !v || !alpha || !beta || !state_in || !out || !state_out) return GDN_ERR_NULL;
     if (N < 1 || L < 1 || P < 1 || Hk < 1 || H < 1 || H % Hk || (!slots && N > P)) return GDN_ERR_SHAPE;
-    if ((long long)N * H > (1LL << 30)) return GDN_ERR_SHAPE;
+    if ((long long)N * H >= (1LL << 24)) return GDN_ERR_SHAPE;      // 256 threads each, below 2^32 a launch
     if (!dims_ok(Dk, Dv)) return GDN_ERR_UNSUPPORTED;
     for (const void *p : {q, k, v, (const void *)alpha, (const void *)beta, (const void *)state_in, (const void *)out,
                           (const void *)state_out})

@@ -214,6 +214,8 @@ def _block_inputs(x, y, gate, w_post, w_pre, gate_tokens):
     gt = int(gate_tokens)
     if gt < 1 or T % gt:
         raise ValueError("T must be a whole number of runs of gate_tokens tokens")
+    if max(B * T, C) >= 1 << 31:      # (the C call's sizes are 32-bit)
+        raise ValueError(f"B T and C must be below 2^31, got {B * T} and {C}")
     f32 = torch.float32
     _needs(dev, ("x", x, (B, T, C), dt), ("y", y, (B, T, C), dt), ("w_post", w_post, (C,), f32), ("w_pre", w_pre, (C,), f32))
     if gate is not None:

@@ -83,6 +83,17 @@ def test_norm_gradient_refusals(kw, want):
     assert ops._lib().gdn_block_norm_backward(*dict(GRAD, **kw).values(), None) == want
 
 
+@pytest.mark.parametrize("kw", [dict(N=1 << 13, H=1 << 11, P=1 << 13), dict(N=1 << 24, H=1, Hk=1, P=1 << 24)])
+def test_step_larger_than_a_launch(kw):
+    assert step(**dict(dict(out=1 << 60, state_out=addr(5)), **kw)) == SHAPE
+
+
+@pytest.mark.parametrize("B,H,T", [(1, 1, 1 << 30), (8, 64, 1 << 20), (1, 65535, 129 * 64)])
+def test_backward_larger_than_a_launch(B, H, T):
+    assert ops._lib().gdn_chunk_backward_workspace_bytes(B, H, T, 64, 64, 64, 1) == 0
+    assert ops._lib().gdn_chunk_backward(*dict(BACK, B=B, H=H, T=T).values(), None) == SHAPE
+
+
 def test_norm_workspace():
     f = ops._lib().gdn_block_norm_workspace_bytes
     assert f(12, 40, 5) == 0 and f(0, 40, 1) == 0 and f(12, 8193, 1) == 0
