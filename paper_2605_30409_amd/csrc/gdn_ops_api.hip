@@ -2,6 +2,7 @@
 // kernel variants, launches, and the extern "C" entry points.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 #include <initializer_list>
 #include <mutex>
@@ -82,13 +83,16 @@ int norm_team(int C) {
 }
 
 // How the gradient's rows are cut into strips (runs of consecutive rows whose
-// sums one team keeps).
+// sums one team keeps): as many as two workgroups of 256 threads a CU, and 512 of wider teams.
+// Twice as many have twice the partial sums to write and add up: 54 + 5.7 us (kernel + sums)
+// against 59.7 + 7.8 at 10560 x 2048 bf16, 335 + 14 against 370 + 35 at 200000 x 512; half
+// as many 65.5 + 4.6 at 10560 x 2048, and 512 strips of narrow rows 721 + 5 at 200000 x 512.
 struct Strips {
     int strips, strip_rows, per_unit, unit_rows;
 };
 
-Strips norm_strips(int R, int gate_tokens) {
-    const int rows = (R - 1) / 512 + 1;
+Strips norm_strips(int R, int C, int gate_tokens) {
+    const int rows = (R - 1) / std::max(512, (1 << 17) / norm_team(C)) + 1;
     Strips t;
     if (gate_tokens > rows) {             // a gate row spans strips: partial sums for dgate
         t.per_unit = (gate_tokens - 1) / rows + 1;
@@ -331,7 +335,11 @@ int gdn_block_norm_forward(const void *x, const void *y, const void *gate, const
         p.R = R;
         p.C = C;
         p.gate_tokens = gate_tokens;
-        p.strip_rows = (R - 1) / 2048 + 1;
+        // Up to 2048 teams a row each; then longer strips, for the next row's loads to be on their way, but
+        // short ones: a new team's loads run beside an old one's stores.  us at 10560 x 2048 bf16 with
+        // 1, 2, 3, 4 and 6 rows: 40, 33, 31, 30.5, 33; 100000 x 2048 with 3, 4, 6, 8 and 49: 364, 373, 386,
+        // 383, 428; 30000 x 8192 (teams of 1024) with 1, 2, 4, 6, 8 and 15: 566, 437, 381, 363, 366, 377.
+        p.strip_rows = std::min((R - 1) / 2048 + 1, norm_team(C) < 1024 ? 4 : 8);
         p.strips = (R - 1) / p.strip_rows + 1;
         p.res_scale = res_scale;
         p.eps = eps;
@@ -342,7 +350,7 @@ int gdn_block_norm_forward(const void *x, const void *y, const void *gate, const
 
 size_t gdn_block_norm_workspace_bytes(int R, int C, int gate_tokens) {
     if (!norm_shape_ok(R, C, gate_tokens) || C > kNormMaxC) return 0;
-    const Strips t = norm_strips(R, gate_tokens);
+    const Strips t = norm_strips(R, C, gate_tokens);
     return align256((size_t)t.strips * 2 * C * 4) + align256(t.per_unit > 1 ? (size_t)t.strips * C * 4 : 0);
 }
 
@@ -375,7 +383,7 @@ int gdn_block_norm_backward(const void *x, const void *y, const void *gate, cons
     }
     auto run = [&](auto *e) {
         using E = std::remove_pointer_t<decltype(e)>;
-        const Strips t = norm_strips(R, gate_tokens);
+        const Strips t = norm_strips(R, C, gate_tokens);
         gdn::NormParams<E> p{};
         p.x = (const E *)x;
         p.y = (const E *)y;

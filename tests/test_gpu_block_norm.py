@@ -126,12 +126,13 @@ def test_gradient(gdn, dtype, B, T, C, gt):
 
 
 @pytest.mark.parametrize("B,T,gt", [(1, 2000, 2000), (1, 2000, 1000), (2, 1500, 1), (1, 2000, 5), (1, 3000, 3), (3, 700, 7),
-                                    (1, 1153, 1153)])
+                                    (1, 1153, 1153), (1, 6000, 6000), (1, 6000, 3000), (2, 4500, 1), (1, 6000, 5),
+                                    (1, 9000, 3), (3, 2100, 7), (1, 4609, 4609), (1, 140000, 4)])
 def test_strips(gdn, B, T, gt):
     """Many rows: gate rows that span several strips, that fill strips and of one token,
     with a last strip that is short."""
     import torch
-    t = make(B, T, 72, gt, "f32", T + gt)
+    t = make(B, T, 72 if T < 10000 else 16, gt, "f32", T + gt)
     args = (t["x"], t["y"], t["gate"], t["w_post"], t["w_pre"])
     r, u = gdn.block_norm(*args, gate_tokens=gt)
     got = gdn.block_norm_backward(*args, t["du"], t["dr"], gate_tokens=gt)

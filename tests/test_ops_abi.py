@@ -99,7 +99,10 @@ def test_norm_workspace():
     assert f(12, 40, 5) == 0 and f(0, 40, 1) == 0 and f(12, 8193, 1) == 0
     for R, C, gt in ((1, 1, 1), (12, 40, 4), (10560, 2048, 3520), (100000, 8, 1), (99999, 16, 3), (700, 64, 700)):
         n = f(R, C, gt)
-        rows = -(-R // 512)
+        team = 64
+        while 8 * team < C:
+            team *= 2
+        rows = -(-R // max(512, (1 << 17) // team))
         assert 0 < n <= 12 * C * (R // max(1, min(rows, gt)) + R // gt + 1) + 1024
 
 
