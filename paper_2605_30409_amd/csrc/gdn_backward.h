@@ -28,10 +28,10 @@
 // backward side by side (gdn_back_scan_kernel); per chunk all that remains
 // (gdn_back_grad_kernel).  bf16, Dk = Dv = 128, us and MB between the L2 caches and memory:
 //                      prep         scan          grad
-//   T = 3520,  H = 16   39, 175     102, 338       79, 280
-//   T = 10560, H = 16  107, 523     323, 1011     245, 845
-// A large copy reaches 4.7 TB/s: prep is there, the last launch at 3.5, and the scan, at 3.2, waits for
-// its exchanges (its arithmetic alone, without loads and stores, takes 79 of the 102 us).
+//   T = 3520,  H = 16   39, 175     100, 338       80, 280
+//   T = 10560, H = 16  107, 523     319, 1011     245, 845
+// A large copy reaches 4.7 TB/s: prep is there, the last launch at 3.5, and the scan, at 3.3, waits for
+// its exchanges (its arithmetic alone, without loads and stores, takes 79 us of the 100).
 //
 // Precision: gate gradients and states are fp32 results, so what leads to them
 // keeps fp32's mantissa.  On the bf16 path an operand that is not itself an input
@@ -498,7 +498,7 @@ constexpr int kBackScanWaves = 4, kBackLoadWaves = 2;
 // place of 325 at T = 10560 (Q's rows, eight times over, and their products, in every workgroup).
 template <class E, int DK, bool DIRECT> struct BackScanLds {
     static constexpr int R = DK / 4, NK = R / 16;                             // state rows and row tiles per wave
-    static constexpr int LDC = lds_ld<E>(kChunk);
+    static constexpr int LDC = sizeof(E) == 2 ? kChunk : lds_ld<E>(kChunk);
     static constexpr int PT = 16 * kChunk, PC = 16 * LDC;                     // planes
     static constexpr int szK = (int)sizeof(E) * kChunk * DK, szF = DIRECT ? 0 : 4096, szA = DIRECT ? 0 : 4096 * NK;
     static constexpr int oF = szK, oA = oF + szF, oG = oA + szA;              // in a slot: K, first, add, gates
@@ -515,13 +515,50 @@ template <class E, int DK, bool DIRECT> struct BackScanLds {
     static_assert(SLOT % 16 == 0 && bytes <= 160 * 1024, "the ring fits the LDS");
 };
 
-// K rows in the ring: a row's 16-byte granules are permuted, granule g stored at g ^ kperm(r), so
-// that the 16 rows of an operand read (one granule each) and the 4 rows of a transposing
-// read (4 granules each) take different banks.
+// LDS layouts of the bf16 path.  A 16-byte read is served in 4 cycles, lanes 0-3, 12-15 and 20-27 in one
+// (the other lanes of the half in the next), if those 16 lanes take different 16-byte places of 256 bytes; an
+// 8-byte read, transposing or not, in 2, the lanes of each half in different 8-byte places; an
+// 8-byte store in 4, 16 lanes each, in different places of 128 bytes.  So the granules of a row are
+// permuted, granule g stored at g ^ perm(row); rows padded by 16 bytes cost twice that, and a
+// store of 32-byte rows four times (the scan: 102 -> 98.5 us at T = 3520, 16 heads of 128, 227 -> 220 at
+// 80 heads of 64).
+//
+// Rows of 128 bytes: 16-byte reads of 16 rows and transposing reads of 8 (r .. r + 3, r + 8 .. r + 11) at
+// full rate, 8-byte stores of one granule in 16 rows at half.
+__device__ __forceinline__ int perm128(int r) { return ((r >> 2) & 1) + (r & 2) + 4 * (((r >> 2) ^ (r >> 3)) & 1); }
+
+// K rows in the ring (of 256 bytes at Dk = 128: transposing reads at half rate, which they are in P32 order
+// in any case).
 template <class E, int DK> __device__ __forceinline__ int kperm(int r) {
     if constexpr (sizeof(E) == 4) return r & 15;
-    else if constexpr (DK == 128) return 4 * (r & 3) + ((r >> 2) & 3);
-    else return 2 * ((r >> 1) & 3);
+    else if constexpr (DK == 128) return 2 * (r & 3) + (r & 8);
+    else return perm128(r);
+}
+
+// T's operand, [token][16 columns]: 8-byte granule g of a token, and its planes with transposing reads.
+template <class E> __device__ __forceinline__ int xaddr(int row, int g) {
+    if constexpr (sizeof(E) == 2) return (row ^ ((row & 8) >> 1)) * 16 + ((g ^ (row >> 2)) & 3) * 4;
+    else return row * 16 + 4 * g;
+}
+template <class E> __device__ __forceinline__ typename Full<E>::frag xcols(const E *X, int plane, int row0, int li, int lg) {
+    if constexpr (sizeof(E) == 2) {
+        typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+        const int row = row0 + 8 * lg + (li >> 2);
+        const E *lo = X + xaddr<E>(row, li & 3), *hi = X + xaddr<E>(row + 4, li & 3);
+        typename Full<E>::frag f;
+#pragma unroll
+        for (int i = 0; i < Full<E>::planes; ++i)
+            f.pl[i] = Tr<E>::cat(__builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(lo + i * plane))),
+                                 __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4 *)(hi + i * plane))));
+        return f;
+    } else {
+        return Full<E>::tr(X, plane, 16, row0, 0, li, lg);
+    }
+}
+// after y, [column][token]: the place of token t's group of 4 or 8 (t a multiple of it)
+template <class E> __device__ __forceinline__ int yaddr(int col, int t) {
+    if constexpr (sizeof(E) == 2) return col * kChunk + (((t >> 3) ^ perm128(col)) << 3) + (t & 4);
+    else return col * lds_ld<E>(kChunk) + t;
 }
 template <class E, int DK> __device__ __forceinline__ const E *kaddr(const E *K, int row, int col) {
     constexpr int VE = 16 / (int)sizeof(E);
@@ -709,7 +746,7 @@ __device__ __forceinline__ void back_scan(const BackParams<E> &p, unsigned char 
 #pragma unroll
         for (int a = 0; a < NK; ++a) *(f32x4 *)(keep + 256 * a) = quad_transpose(st[a], li);
         const f32x4 x = (xs[0] + xs[1]) + (xs[2] + xs[3]);
-        WD::store4(sX + (16 * w + li) * 16 + 4 * lg, L::PT, first + before * x);
+        WD::store4(sX + xaddr<E>(16 * w + li, lg), L::PT, first + before * x);
         typename TR::frag kt[NK][2];
 #pragma unroll
         for (int a = 0; a < NK; ++a)
@@ -728,10 +765,10 @@ __device__ __forceinline__ void back_scan(const BackParams<E> &p, unsigned char 
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
             if (REV ? kb >= w / 2 : kb <= w / 2)                  // T is lower triangular
-                y[kb] = WD::ww(o.T[kb], WD::tr(sX, L::PT, 16, 32 * kb, 0, li, lg), y[kb]);
+                y[kb] = WD::ww(o.T[kb], xcols<E>(sX, L::PT, 32 * kb, li, lg), y[kb]);
         load(chunk(i + 1));
         y[0] += y[1];
-        WD::store4(sY + li * L::LDC + 16 * w + 4 * lg, L::PC, after * y[0]);
+        WD::store4(sY + yaddr<E>(li, 16 * w + 4 * lg), L::PC, after * y[0]);
         *(f32x4 *)((REV ? p.vT : p.eT) + cidx * (size_t)(kChunk * DV) + (unsigned)((16 * jt + li) * kChunk + 16 * w + 4 * lg)) = y[0];
         if constexpr (KAHEAD) {
             const E *Kn = (const E *)(smem + (i + 1) % L::DEPTH * L::SLOT);
@@ -741,7 +778,7 @@ __device__ __forceinline__ void back_scan(const BackParams<E> &p, unsigned char 
         lds_only_barrier();
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
-            const wfrag u = WD::load8(sY + li * L::LDC + 32 * kb + 8 * lg, L::PC);
+            const wfrag u = WD::load8(sY + yaddr<E>(li, 32 * kb + 8 * lg), L::PC);
 #pragma unroll
             for (int a = 0; a < NK; ++a) st[a] = WD::ew(kt[a][kb], u, st[a]);
         }

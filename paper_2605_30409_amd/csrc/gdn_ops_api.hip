@@ -176,8 +176,8 @@ template <class E, int DK, int DV> int launch_backward(const gdn::BackParams<E> 
     using P = gdn::PrepLds<E, DK, DV>;
     // bf16, Dk = 128: a workgroup of the scan that brings all its operands through LDS has a CU
     // to itself; with first and add loaded directly two share one.  us at T = 3520, the ring's
-    // first: 16 heads (one a CU) 102 and 110; 17 heads 172 and 155, 24 heads 193 and 192, 32 heads
-    // 216 and 208; 4 x 31 heads of T = 1320 334 and 325.
+    // first: 16 heads (one a CU) 103 and 109; 17 heads 175 and 152, 24 heads 196 and 194, 32 heads
+    // 221 and 210; 4 x 31 heads of T = 1320 332 and 326.
     constexpr bool SHARE = sizeof(E) == 2 && DK == 128;
     using S = gdn::BackScanLds<E, DK, false>;
     using D = gdn::BackScanLds<E, DK, SHARE>;
