@@ -13,6 +13,7 @@ from . import gdn as _gdn
 from .gdn import GDN_OK, GdnError
 
 _fns = None
+_Tensor, _BF16, _F32, _I32 = torch.Tensor, torch.bfloat16, torch.float32, torch.int32
 
 
 def _lib():
@@ -50,12 +51,13 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _raw_stream)
 
 def _call(name, dev, *args):
     """The C call with the current stream of `dev` behind its other arguments."""
-    fn = getattr(_lib(), name)
-    if torch.cuda.current_device() == dev.index:
-        rc = fn(*args, _raw_stream(dev.index))
+    fn = getattr(_fns or _lib(), name)
+    index = dev.index
+    if torch.cuda.current_device() == index:
+        rc = fn(*args, _raw_stream(index))
     else:
         with torch.cuda.device(dev):
-            rc = fn(*args, _raw_stream(dev.index))
+            rc = fn(*args, _raw_stream(index))
     if rc != GDN_OK:
         raise GdnError(name, rc)
 
@@ -65,10 +67,17 @@ def _needs(dev, *specs):
     a small call is as long as its checks."""
     index = dev.index
     for name, t, shape, dtype in specs:
-        if type(t) is torch.Tensor and t.dtype is dtype and t.get_device() == index and t.shape == shape \
-                and t.is_contiguous():
-            continue
-        _need(name, t, shape, dtype, dev)
+        if not _fit(index, dtype, shape, t):
+            _need(name, t, shape, dtype, dev)
+
+
+def _fit(index, dtype, shape, *tensors):
+    """Whether _need would pass all of these (it may pass others, a tensor's subclass)."""
+    for t in tensors:
+        if type(t) is not _Tensor or t.dtype is not dtype or t.get_device() != index or t.shape != shape \
+                or not t.is_contiguous():
+            return False
+    return True
 
 
 def _need(name, t, shape, dtype, dev):
@@ -76,7 +85,7 @@ def _need(name, t, shape, dtype, dev):
         raise TypeError(f"{name} must be a tensor, got {type(t).__name__}")
     if t.dtype != dtype:
         raise TypeError(f"{name} must have dtype {dtype}, got {t.dtype}")
-    if tuple(t.shape) != shape:
+    if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} must be {list(shape)}, got {list(t.shape)}")
     if t.device != dev:
         raise ValueError(f"{name} must be on {dev}, got {t.device}")
@@ -92,17 +101,18 @@ def _on(stream, t):
 
 
 def _element(name, t):
-    if not isinstance(t, torch.Tensor):
+    if not isinstance(t, _Tensor):
         raise TypeError(f"{name} must be a tensor, got {type(t).__name__}")
-    if t.dtype not in (torch.bfloat16, torch.float32):
-        raise TypeError(f"{name} must be bfloat16 or float32, got {t.dtype}")
-    if t.device.type != "cuda":
+    dt = t.dtype
+    if dt is not _BF16 and dt is not _F32:
+        raise TypeError(f"{name} must be bfloat16 or float32, got {dt}")
+    if not t.is_cuda:
         raise ValueError(f"{name} must be on a GPU, got {t.device}")
-    return t.dtype, t.device
+    return dt, t.device
 
 
 def _dims(name, t, dims, text):
-    shape = t.shape if isinstance(t, torch.Tensor) else ()
+    shape = t.shape if isinstance(t, _Tensor) else ()
     if len(shape) != dims:
         raise ValueError(f"{name} must be {text}, got {list(shape)}")
     return shape
@@ -125,28 +135,32 @@ def step(q, k, v, alpha, beta, state, *, slots=None, lengths=None, out=None, sta
         with _on(stream, q):
             return step(q, k, v, alpha, beta, state, slots=slots, lengths=lengths, out=out, state_out=state_out)
     dt, dev = _element("q", q)
-    N, L, Hk, Dk = _dims("q", q, 4, "[N, L, Hk, Dk]")
-    H, Dv = _dims("v", v, 4, "[N, L, H, Dv]")[2:]
-    P = _dims("state", state, 4, "[P, H, Dk, Dv]")[0]
-    f32, keys, gates = torch.float32, (N, L, Hk, Dk), (N, L, H)
-    _needs(dev, ("q", q, keys, dt), ("k", k, keys, dt), ("v", v, (N, L, H, Dv), dt), ("alpha", alpha, gates, f32),
-           ("beta", beta, gates, f32), ("state", state, (P, H, Dk, Dv), f32))
-    if slots is not None:
-        _needs(dev, ("slots", slots, (N,), torch.int32))
-    if lengths is not None:
-        _needs(dev, ("lengths", lengths, (N,), torch.int32))
+    N, L, Hk, Dk = keys = _dims("q", q, 4, "[N, L, Hk, Dk]")
+    Nv, Lv, H, Dv = values = _dims("v", v, 4, "[N, L, H, Dv]")
+    P, Hs, Dks, Dvs = pool = _dims("state", state, 4, "[P, H, Dk, Dv]")
+    f32, gates, index = _F32, (N, L, H), dev.index
+    if state_out is None:
+        state_out = state
+    # one condition where nothing is wrong: a token's step is as long as its checks
+    if not (N == Nv and L == Lv and H == Hs and Dk == Dks and Dv == Dvs and _fit(index, dt, keys, q, k)
+            and _fit(index, dt, values, v) and _fit(index, f32, gates, alpha, beta)
+            and _fit(index, f32, pool, state) and (state_out is state or _fit(index, f32, pool, state_out))
+            and (out is None or _fit(index, dt, values, out))
+            and (slots is None or _fit(index, _I32, (N,), slots))
+            and (lengths is None or _fit(index, _I32, (N,), lengths))):
+        values, pool = (N, L, H, Dv), (P, H, Dk, Dv)
+        _needs(dev, ("q", q, keys, dt), ("k", k, keys, dt), ("v", v, values, dt), ("alpha", alpha, gates, f32),
+               ("beta", beta, gates, f32), ("state", state, pool, f32), ("state_out", state_out, pool, f32))
+        for name, t, shape, dtype in (("slots", slots, (N,), _I32), ("lengths", lengths, (N,), _I32),
+                                      ("out", out, values, dt)):
+            if t is not None:
+                _needs(dev, (name, t, shape, dtype))
     if out is None:
         # every element is written unless a row may be short or padding
         out = torch.empty_like(v) if slots is None and lengths is None else torch.zeros_like(v)
-    else:
-        _needs(dev, ("out", out, (N, L, H, Dv), dt))
-    if state_out is None:
-        state_out = state
-    else:
-        _needs(dev, ("state_out", state_out, (P, H, Dk, Dv), f32))
     _call("gdn_step_forward", dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), alpha.data_ptr(), beta.data_ptr(),
           state.data_ptr(), _ptr(slots), _ptr(lengths), out.data_ptr(), state_out.data_ptr(), N, L, P, Hk, H, Dk, Dv,
-          1 if dt == torch.bfloat16 else 0)
+          1 if dt is _BF16 else 0)
     return out, state_out
 
 

@@ -209,3 +209,27 @@ def test_fresh_output_is_zero_where_nothing_is_written(gdn):
     torch.full((3, 2, 1, 64), float("nan"), dtype=torch.bfloat16, device="cuda")   # freed memory that is not zero
     out, _ = gdn.step(**t, slots=slots, lengths=torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda"))
     assert not out[0].any() and not out[1, 1].any() and not out[2].any() and out[1, 0].all()
+
+
+@pytest.mark.parametrize("name", ["q", "k", "v", "alpha", "beta", "state", "slots", "lengths", "out", "state_out"])
+def test_arguments(gdn, name):
+    """Each argument with a wrong size, a wrong type, on the host, or with gaps is refused by its name;
+    a parameter of a module passes, with the bits of its tensor."""
+    import torch
+    t, slots = make(3, 2, 4, 2, 4, 64, 128, "bf16", 41)
+    a = dict(t, slots=slots, lengths=torch.tensor([2, 0, 1], dtype=torch.int32, device="cuda"),
+             out=torch.zeros_like(t["v"]), state_out=t["state"].clone())
+    ref, after = (x.clone() for x in gdn.step(**a))
+    x = a[name]
+    wrong = [x.new_zeros([n + 1 for n in x.shape]), x.cpu(), x.new_zeros([2 * n for n in x.shape])[tuple(slice(None, None, 2) for _ in x.shape)]]
+    for bad in wrong:
+        with pytest.raises(ValueError):
+            gdn.step(**dict(a, **{name: bad}))
+    for bad in (x.double(), None if name in ("q", "k", "v", "alpha", "beta", "state") else 3):
+        with pytest.raises((TypeError, ValueError)):
+            gdn.step(**dict(a, **{name: bad}))
+    if x.is_floating_point():
+        a.update(out=torch.zeros_like(ref), state_out=t["state"].clone())
+        a[name] = torch.nn.Parameter(a[name], requires_grad=False)
+        out, state = gdn.step(**a)
+        assert torch.equal(out, ref) and torch.equal(state, after)
