@@ -189,8 +189,10 @@ def backward(q, k, v, alpha, beta, state_in, dout, dstate_out=None, *, dq=None, 
     Dv = _dims("v", v, 4, "[B, T, H, Dv]")[3]
     f32 = torch.float32
     keys, values, gates = (B, T, H, Dk), (B, T, H, Dv), (B, T, H)
-    _needs(dev, ("q", q, keys, dt), ("k", k, keys, dt), ("v", v, values, dt), ("dout", dout, values, dt),
-           ("alpha", alpha, gates, f32), ("beta", beta, gates, f32))
+    if not (_fit(dev.index, dt, keys, q, k) and _fit(dev.index, dt, values, v, dout)
+            and _fit(dev.index, f32, gates, alpha, beta)):
+        _needs(dev, ("q", q, keys, dt), ("k", k, keys, dt), ("v", v, values, dt), ("dout", dout, values, dt),
+               ("alpha", alpha, gates, f32), ("beta", beta, gates, f32))
     for name, t in (("state_in", state_in), ("dstate_out", dstate_out)):
         if t is not None:
             _needs(dev, (name, t, (B, H, Dk, Dv), f32))
@@ -231,7 +233,9 @@ def _block_inputs(x, y, gate, w_post, w_pre, gate_tokens):
     if max(B * T, C) >= 1 << 31:      # (the C call's sizes are 32-bit)
         raise ValueError(f"B T and C must be below 2^31, got {B * T} and {C}")
     f32 = torch.float32
-    _needs(dev, ("x", x, (B, T, C), dt), ("y", y, (B, T, C), dt), ("w_post", w_post, (C,), f32), ("w_pre", w_pre, (C,), f32))
+    if not (_fit(dev.index, dt, (B, T, C), x, y) and _fit(dev.index, f32, (C,), w_post, w_pre)):
+        _needs(dev, ("x", x, (B, T, C), dt), ("y", y, (B, T, C), dt), ("w_post", w_post, (C,), f32),
+               ("w_pre", w_pre, (C,), f32))
     if gate is not None:
         _needs(dev, ("gate", gate, (B, T // gt, C), dt))
     return dt, dev, B, T, C, gt
