@@ -822,12 +822,11 @@ void gdn_back_scan_kernel(BackParams<E> p) {
 
 // --------------------------------------------------------------------------
 // Stage 3, per chunk and head: dQ, dK, dV, dalpha and dbeta.  Four waves, two
-// workgroups to a CU.  Wave w has the Dk / 4 key channels from (Dk / 4) w on in the
+// workgroups to a CU (or eight, see NH).  Wave w has the Dk / 4 key channels from (Dk / 4) w on in the
 // products over Dk; the 64 x 64 products are dealt out as lower tiles.  The value
 // channels go through LDS 64 at a time; once they are done, G1, G2 and X take their
 // place there.
 // --------------------------------------------------------------------------
-constexpr int kGradWaves = 4;
 
 template <class E> struct GradLds {
     static constexpr int LDC = lds_ld<E>(kChunk), PC = kChunk * LDC;
@@ -847,8 +846,10 @@ template <class E> struct GradLds {
     static constexpr size_t bytes = oRed + 4 * (48 * 64 + 64 + 4);
 };
 
-template <class E, int DK, int DV>
-__global__ __launch_bounds__(64 * kGradWaves) __attribute__((amdgpu_waves_per_eu(2, 2)))
+// NH = 2: eight waves, four for each half of the tokens in the products over Dk, for launches that
+// leave every workgroup a CU of its own.
+template <class E, int DK, int DV, int NH>
+__global__ __launch_bounds__(256 * NH) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void gdn_back_grad_kernel(BackParams<E> p) {
     using L = GradLds<E>;
     using TR = Tr<E>;
@@ -856,7 +857,8 @@ void gdn_back_grad_kernel(BackParams<E> p) {
     using WH = Half<E>;
     using frag = typename TR::frag;
     using wfrag = typename WD::frag;
-    constexpr int NW = kGradWaves, NT = 64 * NW, NK = DK / 64;     // NK: channel tiles per wave
+    constexpr int NW = 4 * NH, NT = 64 * NW;
+    constexpr int NK = DK / 64, RT = 4 / NH;                       // channel and token tiles per wave
     constexpr int VE = 16 / (int)sizeof(E);
     constexpr int NST = kChunk * 64 / 4 / NT, NSO = kChunk * 64 / VE / NT;   // staged quads / vectors per thread
     extern __shared__ __align__(16) unsigned char smem[];
@@ -867,7 +869,8 @@ void gdn_back_grad_kernel(BackParams<E> p) {
     float *rX = (float *)(smem + L::oRed), *rE = rX + 16 * 64, *cb = rE + 16 * 64, *xm = cb + 16 * 64, *gh = xm + 64;
     const int c = blockIdx.x / (p.B * p.H), bh = blockIdx.x - c * (p.B * p.H);
     const int b = bh / p.H, h = bh - b * p.H;
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63;
+    const int w = wave & 3, rt0 = wave / 4 * RT;                   // its channels, its first token tile
     int tid = threadIdx.x, li = l & 15, lg = l >> 4;
     // What follows computes its addresses anew: kept from the front on, they would take the
     // registers of the products between.
@@ -884,14 +887,14 @@ void gdn_back_grad_kernel(BackParams<E> p) {
     for (int i = tid; i < kBackGateRec; i += NT) ((float *)(smem + L::oGate))[i] = p.gates[cidx * kBackGateRec + i];
 
     // PQ, PV, PE transposed, tiles [16 key channels][16 tokens]; Z and F
-    constexpr int NTI = 3;                                         // lower tiles w, w + 4, w + 8 of ten
-    f32x4 pq[NK][4], pv[NK][4], pe[NK][4], z[NTI], f[NTI], dot = {0.f, 0.f, 0.f, 0.f};
+    constexpr int NTI = (9 + NW) / NW;                             // lower tiles wave, wave + NW, .. of ten
+    f32x4 pq[NK][RT], pv[NK][RT], pe[NK][RT], z[NTI], f[NTI], dot = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int n = 0; n < NTI; ++n) z[n] = f[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int n = 0; n < NK; ++n)
 #pragma unroll
-        for (int rt = 0; rt < 4; ++rt) pq[n][rt] = pv[n][rt] = pe[n][rt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int rt = 0; rt < RT; ++rt) pq[n][rt] = pv[n][rt] = pe[n][rt] = f32x4{0.f, 0.f, 0.f, 0.f};
     // row li of tile n stands for channel 32 w + p32_row(n, li) (Dk = 64: 16 w + li): a lane gets
     // 4 NK consecutive channels in its NK results
     auto channel = [&](int n) { return NK == 2 ? 32 * w + p32_row(n, li) : 16 * w + li; };
@@ -949,24 +952,25 @@ void gdn_back_grad_kernel(BackParams<E> p) {
 #pragma unroll
             for (int n = 0; n < NK; ++n) S[n] = WD::split(hs[n][0], hs[n][1]);
 #pragma unroll
-            for (int rt = 0; rt < 4; ++rt) {
-                const frag o = load_frag<E>(sO + (16 * rt + li) * L::LDC + 32 * kb, lg);
-                const wfrag dv = WD::tr(sV, L::PC, L::LDC, 32 * kb, 16 * rt, li, lg);
+            for (int rt = 0; rt < RT; ++rt) {
+                const int tt = rt0 + rt;
+                const frag o = load_frag<E>(sO + (16 * tt + li) * L::LDC + 32 * kb, lg);
+                const wfrag dv = WD::tr(sV, L::PC, L::LDC, 32 * kb, 16 * tt, li, lg);
 #pragma unroll
                 for (int n = 0; n < NK; ++n) {
                     pq[n][rt] = WD::we(S[n], o, pq[n][rt]);
                     pv[n][rt] = WD::ww(S[n], dv, pv[n][rt]);
                 }
-                // dV: wave rt stores the rows it has at hand
-                if (w == rt && 16 * rt + li < nvalid)
-                    TR::store8(p.dv + (row0 + (size_t)(16 * rt + li) * p.H) * DV + dv0 + 32 * kb + 8 * lg, WD::rounded(dv));
+                // dV: one wave stores the rows it has at hand
+                if (w == tt && 16 * tt + li < nvalid)
+                    TR::store8(p.dv + (row0 + (size_t)(16 * tt + li) * p.H) * DV + dv0 + 32 * kb + 8 * lg, WD::rounded(dv));
                 if (rt & 1) __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
             for (int n = 0; n < NTI; ++n) {
-                if (w + 4 * n >= 10) continue;
+                if (wave + NW * n >= 10) continue;
                 int bi, bj;
-                lower_tile(w + 4 * n, bi, bj);
+                lower_tile(wave + NW * n, bi, bj);
                 const wfrag ej = WD::tr(sE, L::PC, L::LDC, 32 * kb, 16 * bj, li, lg);
                 z[n] = WD::ew(load_frag<E>(sO + (16 * bi + li) * L::LDC + 32 * kb, lg), ej, z[n]);
                 f[n] = WD::ww(WD::tr(sV, L::PC, L::LDC, 32 * kb, 16 * bi, li, lg), ej, f[n]);
@@ -980,8 +984,8 @@ void gdn_back_grad_kernel(BackParams<E> p) {
             quads(p.Hs, min(j0 + 32, DV - 32), hs);
             __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int rt = 0; rt < 4; ++rt) {
-                const wfrag e = WD::tr(sE, L::PC, L::LDC, 32 * kb, 16 * rt, li, lg);
+            for (int rt = 0; rt < RT; ++rt) {
+                const wfrag e = WD::tr(sE, L::PC, L::LDC, 32 * kb, 16 * (rt0 + rt), li, lg);
 #pragma unroll
                 for (int n = 0; n < NK; ++n) pe[n][rt] = WD::ww(S[n], e, pe[n][rt]);
                 if (rt & 1) __builtin_amdgcn_sched_barrier(0);
@@ -998,7 +1002,7 @@ void gdn_back_grad_kernel(BackParams<E> p) {
     } ra, rb;
     auto tile_rows = [&](int n, Rows &x) {
         int bi, bj;
-        lower_tile(min(w + 4 * n, 9), bi, bj);
+        lower_tile(min(wave + NW * n, 9), bi, bj);
 #pragma unroll
         for (int kb = 0; kb < DK / 32; ++kb) {
             x.q[kb] = rows(p.q, 16 * bi + li, kb);
@@ -1007,10 +1011,10 @@ void gdn_back_grad_kernel(BackParams<E> p) {
         }
     };
     using own = std::conditional_t<NK == 2, frag, typename TR::quad>;
-    own qo[4], ko[4];
+    own qo[RT], ko[RT];
 #pragma unroll
-    for (int rt = 0; rt < 4; ++rt) {
-        const size_t at = (row0 + (size_t)min(16 * rt + li, nvalid - 1) * p.H) * DK + ch0();
+    for (int rt = 0; rt < RT; ++rt) {
+        const size_t at = (row0 + (size_t)min(16 * (rt0 + rt) + li, nvalid - 1) * p.H) * DK + ch0();
         if constexpr (NK == 2) qo[rt] = TR::load8(p.q + at), ko[rt] = TR::load8(p.k + at);
         else qo[rt] = TR::load(p.q + at), ko[rt] = TR::load(p.k + at);
     }
@@ -1020,13 +1024,13 @@ void gdn_back_grad_kernel(BackParams<E> p) {
         float s = dot[0] + dot[1] + dot[2] + dot[3];
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) s += __shfl_xor(s, d);
-        if (l == 0) gh[w] = s;
+        if (l == 0 && rt0 == 0) gh[w] = s;
     }
     // q.PQ - k.PV and k.PE of this wave's channels; then the parts of dQ and dK that
     // come from the states
 #pragma unroll
-    for (int rt = 0; rt < 4; ++rt) {
-        const int t = 16 * rt + li;
+    for (int rt = 0; rt < RT; ++rt) {
+        const int t = 16 * (rt0 + rt) + li;
         float x = 0.f, y = 0.f;
 #pragma unroll
         for (int n = 0; n < NK; ++n) {
@@ -1049,14 +1053,14 @@ void gdn_back_grad_kernel(BackParams<E> p) {
         rX[(w * 4 + lg) * 64 + t] = x;
         rE[(w * 4 + lg) * 64 + t] = y;
     }
-    if (AHEAD) tile_rows(1, rb);
+    if (AHEAD && wave + NW < 10) tile_rows(1, rb);
     lds_barrier();
     // The 64 x 64 matrices: element (i, j) with i = 16 bi + 4 lg + q, j = 16 bj + li.  The six
     // tiles above the diagonal of G1 and X are zero.
     auto matrices = [&](int n, const Rows &r) {
-        if (w + 4 * n >= 10) return;
+        if (wave + NW * n >= 10) return;
         int bi, bj;
-        lower_tile(w + 4 * n, bi, bj);
+        lower_tile(wave + NW * n, bi, bj);
         const int j = 16 * bj + li, i0 = 16 * bi + 4 * lg;
         const float bj_ = beta[j];
         f32x4 sqk = {0.f, 0.f, 0.f, 0.f}, skk = sqk, g1, g2, xx;
@@ -1095,8 +1099,8 @@ void gdn_back_grad_kernel(BackParams<E> p) {
     if (!AHEAD) tile_rows(0, ra);
     matrices(0, ra);
     __builtin_amdgcn_sched_barrier(0);
-    if (AHEAD) tile_rows(2, ra);
-    else tile_rows(1, rb);
+    if (!AHEAD) tile_rows(1, rb);
+    else if (NTI == 3) tile_rows(2, ra);
     __builtin_amdgcn_sched_barrier(0);
     matrices(1, rb);
     __builtin_amdgcn_sched_barrier(0);
@@ -1114,11 +1118,11 @@ void gdn_back_grad_kernel(BackParams<E> p) {
     if (AHEAD) {
         columns(p.k, kt_);
         columns(p.q, qt_);
-    } else {
+    } else if (NTI == 3) {
         tile_rows(2, ra);
     }
     __builtin_amdgcn_sched_barrier(0);
-    matrices(2, ra);
+    if (NTI == 3) matrices(2, ra);
     __builtin_amdgcn_sched_barrier(0);
     if (!AHEAD) {
         columns(p.k, kt_);
@@ -1128,12 +1132,12 @@ void gdn_back_grad_kernel(BackParams<E> p) {
     forget();
 
     // Sums over the waves: X's border row and column, dbeta
-    if (w == 0) {
+    if (wave == 0) {
         float x = 0.f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) x += rX[i * 64 + l];
         xm[l] = x;
-    } else if (w == 1) {
+    } else if (wave == 1) {
         float y = 0.f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) y += rE[i * 64 + l];
@@ -1153,28 +1157,29 @@ void gdn_back_grad_kernel(BackParams<E> p) {
                 qt[n][kb] = __builtin_bit_cast(frag, qt_[n][kb]);
             }
 #pragma unroll
-        for (int rt = 0; rt < 4; ++rt) {
+        for (int rt = 0; rt < RT; ++rt) {
+            const int tt = rt0 + rt;
             f32x4 gk[NK];
 #pragma unroll
             for (int n = 0; n < NK; ++n) gk[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
-                const int at = (16 * rt + li) * L::LDC + 32 * kb + 8 * lg;
+                const int at = (16 * tt + li) * L::LDC + 32 * kb + 8 * lg;
                 const typename WH::frag g2 = WH::load8(sG2 + at, L::PC);
 #pragma unroll
                 for (int n = 0; n < NK; ++n) gk[n] = WH::ew(kt[n][kb], g2, gk[n]);
-                if (kb <= rt / 2) {
-                    const typename WH::frag g1 = WH::tr(sG1, L::PC, L::LDC, 32 * kb, 16 * rt, li, lg);
+                if (kb <= tt / 2) {
+                    const typename WH::frag g1 = WH::tr(sG1, L::PC, L::LDC, 32 * kb, 16 * tt, li, lg);
 #pragma unroll
                     for (int n = 0; n < NK; ++n) pq[n][rt] = WH::ew(kt[n][kb], g1, pq[n][rt]);
                 }
-                if (kb >= rt / 2) {
+                if (kb >= tt / 2) {
                     const typename WH::frag g1 = WH::load8(sG1 + at, L::PC);
 #pragma unroll
                     for (int n = 0; n < NK; ++n) pe[n][rt] = WH::ew(qt[n][kb], g1, pe[n][rt]);
                 }
             }
-            const int t = 16 * rt + li;
+            const int t = 16 * tt + li;
             if (t < nvalid) {
                 const size_t at = (row0 + (size_t)t * p.H) * DK + ch0();
                 if constexpr (NK == 2) {
@@ -1188,6 +1193,7 @@ void gdn_back_grad_kernel(BackParams<E> p) {
         }
     }
     lds_barrier();
+    if (wave >= 4) return;
     // dalpha: M_it = sum_j X_ij D_{t-1,j}, then D_it M_it summed over rows; row 0 of X is the
     // exit state's (its own has no j < 0), so row tile 0 is needed for every t.  Wave w has the
     // tokens t of tile w.
