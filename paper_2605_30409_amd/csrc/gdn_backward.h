@@ -28,7 +28,7 @@
 // backward side by side (gdn_back_scan_kernel); per chunk all that remains
 // (gdn_back_grad_kernel).  bf16, Dk = Dv = 128, us and MB between the L2 caches and memory:
 //                      prep         scan          grad
-//   T = 3520,  H = 16   39, 175     100, 338       80, 280
+//   T = 3520,  H = 16   40, 175     100, 338       82, 280
 //   T = 10560, H = 16  107, 523     319, 1011     245, 845
 // A large copy reaches 4.7 TB/s: prep is there, the last launch at 3.5, and the scan, at 3.3, waits for
 // its exchanges (its arithmetic alone, without loads and stores, takes 79 us of the 100).
