@@ -65,7 +65,7 @@ int gdn_step_forward(const void *q, const void *k, const void *v, const float *a
  * gradients are those of the recurrence itself: alpha and beta of 0 have theirs
  * too (alpha below 1.2e-38 acts as that value, as in the forward).  Sums, states
  * and their gradients are fp32, and on the bf16 path too the operands of products
- * that lead to fp32 results keep fp32's mantissa.  Results are deterministic.
+ * that are not inputs keep fp32's mantissa.  Results are deterministic.
  *
  * B H <= 65535, and B H chunks < 2^23.  Outputs may not overlap inputs or each other,
  * except dstate_in == dstate_out.

@@ -33,14 +33,14 @@
 // A large copy reaches 4.7 TB/s: prep is there, the last launch at 3.5, and the scan, at 3.3, waits for
 // its exchanges (its arithmetic alone, without loads and stores, takes 79 us of the 100).
 //
-// Precision: gate gradients and states are fp32 results, so what leads to them
+// Precision: gate gradients and states are fp32 results, and dQ and dK sums whose terms
+// may cancel, so what leads to them
 // keeps fp32's mantissa.  On the bf16 path an operand that is not itself an input
 // is cut into three bf16 planes, x = hi + mid + lo exactly (8 bits of mantissa
 // each, denormals aside); a product with an input takes three bf16 MFMAs and one of two
 // such operands six (the terms left out are below 2^-25).  That is 48 and 96 cycles where
 // fp32 MFMAs take 256.  Two planes, tried first, left 2e-6 to 4e-6 of error in
-// the fp32 results; fp32 evaluation has 2e-7 to 3e-7.  Only the last products of dQ and dK,
-// whose results are rounded to bf16, take G1 and G2 in two planes (2^-17).  On the fp32 path
+// the fp32 results; fp32 evaluation has 2e-7 to 3e-7.  On the fp32 path
 // operands are fp32 and all products fp32 MFMAs.
 #pragma once
 
@@ -210,7 +210,6 @@ __device__ __forceinline__ f32x4 quad_transpose(f32x4 x, int l) {
 }
 
 template <class E> using Full = Wide<E, 3>;    // fp32's mantissa
-template <class E> using Half = Wide<E, 2>;    // 16 bits of it
 
 __device__ __forceinline__ float elem_f32(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
 __device__ __forceinline__ float elem_f32(float x) { return x; }
@@ -824,21 +823,23 @@ void gdn_back_scan_kernel(BackParams<E> p) {
 // Stage 3, per chunk and head: dQ, dK, dV, dalpha and dbeta.  Four waves, two
 // workgroups to a CU (or eight, see NH).  Wave w has the Dk / 4 key channels from (Dk / 4) w on in the
 // products over Dk; the 64 x 64 products are dealt out as lower tiles.  The value
-// channels go through LDS 64 at a time; once they are done, G1, G2 and X take their
-// place there.
+// channels go through LDS 64 at a time; once they are done, X and G1, then G2, take their
+// place there (all three at once are more than two workgroups a CU leave room for;
+// G1 and G2 side by side in two planes of bf16 took 1 % less of the whole call at heads of 128, 2 % at
+// 64, and lost what their sums cancel down to).
 // --------------------------------------------------------------------------
 
 template <class E> struct GradLds {
     static constexpr int LDC = lds_ld<E>(kChunk), PC = kChunk * LDC;
-    static constexpr size_t szF = sizeof(E) * Full<E>::planes * PC, szH = sizeof(E) * Half<E>::planes * PC;
+    static constexpr size_t szF = sizeof(E) * Full<E>::planes * PC;
     static constexpr size_t oE = 0;                     // e^T, 64 value channels
     static constexpr size_t oV = oE + szF;              // dV^T
     static constexpr size_t oO = oV + szF;              // dO, [token][value channel]
     static constexpr size_t endA = oO + sizeof(E) * PC;
     static constexpr size_t oX = 0;                     // X^T, its column 0 the exit state's
-    static constexpr size_t oG1 = oX + szF;             // G1^T
-    static constexpr size_t oG2 = oG1 + szH;            // G2 + G2^T
-    static constexpr size_t endB = oG2 + szH;
+    static constexpr size_t oG1 = oX + szF;             // G1^T, then G2 + G2^T
+    static constexpr size_t oG2 = oG1 + szF;            // G2's ten lower tiles, fp32, as their lanes have them
+    static constexpr size_t endB = oG2 + 10 * 1024;
     static constexpr size_t oGate = endA > endB ? endA : endB;
     static constexpr size_t oRed = oGate + 4 * kBackGateRec;
     // floats behind oRed: [4 wave][4 lg][64] parts of X_i,-1, the same of k.PE, [4 row tile][4 lg][64] of
@@ -854,7 +855,6 @@ void gdn_back_grad_kernel(BackParams<E> p) {
     using L = GradLds<E>;
     using TR = Tr<E>;
     using WD = Full<E>;
-    using WH = Half<E>;
     using frag = typename TR::frag;
     using wfrag = typename WD::frag;
     constexpr int NW = 4 * NH, NT = 64 * NW;
@@ -863,7 +863,8 @@ void gdn_back_grad_kernel(BackParams<E> p) {
     constexpr int NST = kChunk * 64 / 4 / NT, NSO = kChunk * 64 / VE / NT;   // staged quads / vectors per thread
     extern __shared__ __align__(16) unsigned char smem[];
     E *sE = (E *)(smem + L::oE), *sV = (E *)(smem + L::oV), *sO = (E *)(smem + L::oO), *sX = (E *)(smem + L::oX),
-      *sG1 = (E *)(smem + L::oG1), *sG2 = (E *)(smem + L::oG2);
+      *sG = (E *)(smem + L::oG1);
+    float *sG2 = (float *)(smem + L::oG2);
     const float *gate = (const float *)(smem + L::oGate);
     const float *gam = gate + kBackGam, *tail = gate + kBackTail, *beta = gate + kBackBeta;
     float *rX = (float *)(smem + L::oRed), *rE = rX + 16 * 64, *cb = rE + 16 * 64, *xm = cb + 16 * 64, *gh = xm + 64;
@@ -1056,7 +1057,7 @@ void gdn_back_grad_kernel(BackParams<E> p) {
     if (AHEAD && wave + NW < 10) tile_rows(1, rb);
     lds_barrier();
     // The 64 x 64 matrices: element (i, j) with i = 16 bi + 4 lg + q, j = 16 bj + li.  The six
-    // tiles above the diagonal of G1 and X are zero.
+    // tiles above the diagonal of G1 and X are zero.  G2 waits as it is until G1 has been read.
     auto matrices = [&](int n, const Rows &r) {
         if (wave + NW * n >= 10) return;
         int bi, bj;
@@ -1080,21 +1081,29 @@ void gdn_back_grad_kernel(BackParams<E> p) {
             xx[q] = i > j ? bj_ * (sqk[q] * z[n][q] - skk[q] * f[n][q]) : 0.f;
             cs += sqk[q] * dz - skk[q] * df;
         }
-        WH::store4(sG1 + j * L::LDC + i0, L::PC, g1);
+        *(f32x4 *)(sG2 + (wave + NW * n) * 256 + l * 4) = g2;
+        WD::store4(sG + j * L::LDC + i0, L::PC, g1);
         WD::store4(sX + j * L::LDC + i0, L::PC, xx);
         if (bi != bj) {
-            WH::store4(sG2 + j * L::LDC + i0, L::PC, g2);
             const f32x4 none = {0.f, 0.f, 0.f, 0.f};
-            WH::store4(sG1 + (16 * bi + li) * L::LDC + 16 * bj + 4 * lg, L::PC, none);
+            WD::store4(sG + (16 * bi + li) * L::LDC + 16 * bj + 4 * lg, L::PC, none);
             WD::store4(sX + (16 * bi + li) * L::LDC + 16 * bj + 4 * lg, L::PC, none);
         }
+        cb[(bi * 4 + lg) * 64 + j] = cs;
+    };
+    auto symmetric = [&](int n) {                                  // G2 + G2^T
+        if (wave + NW * n >= 10) return;
+        int bi, bj;
+        lower_tile(wave + NW * n, bi, bj);
+        const int j = 16 * bj + li, i0 = 16 * bi + 4 * lg;
+        const f32x4 g2 = *(const f32x4 *)(sG2 + (wave + NW * n) * 256 + l * 4);
+        if (bi != bj) WD::store4(sG + j * L::LDC + i0, L::PC, g2);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             if (i0 + q < j) continue;                              // written from below the diagonal
-            WH::store1(sG2 + (i0 + q) * L::LDC + j, L::PC, g2[q]);
-            if (bi == bj && i0 + q > j) WH::store1(sG2 + j * L::LDC + i0 + q, L::PC, g2[q]);
+            WD::store1(sG + (i0 + q) * L::LDC + j, L::PC, g2[q]);
+            if (bi == bj && i0 + q > j) WD::store1(sG + j * L::LDC + i0 + q, L::PC, g2[q]);
         }
-        cb[(bi * 4 + lg) * 64 + j] = cs;
     };
     if (!AHEAD) tile_rows(0, ra);
     matrices(0, ra);
@@ -1146,7 +1155,7 @@ void gdn_back_grad_kernel(BackParams<E> p) {
         for (int i = l >> 4 << 2; i < 16; ++i) d += cb[i * 64 + l];
         if (l < nvalid) p.dbeta[row0 + (size_t)l * p.H] = d;
     }
-    // dQ += G1 K;  dK += G1^T Q - (G2 + G2^T) K
+    // dQ += G1 K;  dK += G1^T Q, then, with G2 in the place of G1, dK -= (G2 + G2^T) K
     {
         frag kt[NK][2], qt[NK][2];
 #pragma unroll
@@ -1156,43 +1165,55 @@ void gdn_back_grad_kernel(BackParams<E> p) {
                 kt[n][kb] = __builtin_bit_cast(frag, kt_[n][kb]);
                 qt[n][kb] = __builtin_bit_cast(frag, qt_[n][kb]);
             }
+        auto put = [&](E *dst, int tt, const f32x4 (&x)[NK]) {
+            const int t = 16 * tt + li;
+            if (t >= nvalid) return;
+            dst += (row0 + (size_t)t * p.H) * DK + ch0();
+            if constexpr (NK == 2) TR::store8(dst, TR::cat(TR::from_f32(x[0]), TR::from_f32(x[1])));
+            else TR::store(dst, TR::from_f32(x[0]));
+        };
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             const int tt = rt0 + rt;
-            f32x4 gk[NK];
-#pragma unroll
-            for (int n = 0; n < NK; ++n) gk[n] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int kb = 0; kb < 2; ++kb) {
-                const int at = (16 * tt + li) * L::LDC + 32 * kb + 8 * lg;
-                const typename WH::frag g2 = WH::load8(sG2 + at, L::PC);
-#pragma unroll
-                for (int n = 0; n < NK; ++n) gk[n] = WH::ew(kt[n][kb], g2, gk[n]);
                 if (kb <= tt / 2) {
-                    const typename WH::frag g1 = WH::tr(sG1, L::PC, L::LDC, 32 * kb, 16 * tt, li, lg);
+                    const wfrag g1 = WD::tr(sG, L::PC, L::LDC, 32 * kb, 16 * tt, li, lg);
 #pragma unroll
-                    for (int n = 0; n < NK; ++n) pq[n][rt] = WH::ew(kt[n][kb], g1, pq[n][rt]);
+                    for (int n = 0; n < NK; ++n) pq[n][rt] = WD::ew(kt[n][kb], g1, pq[n][rt]);
                 }
                 if (kb >= tt / 2) {
-                    const typename WH::frag g1 = WH::load8(sG1 + at, L::PC);
+                    const wfrag g1 = WD::load8(sG + (16 * tt + li) * L::LDC + 32 * kb + 8 * lg, L::PC);
 #pragma unroll
-                    for (int n = 0; n < NK; ++n) pe[n][rt] = WH::ew(qt[n][kb], g1, pe[n][rt]);
+                    for (int n = 0; n < NK; ++n) pe[n][rt] = WD::ew(qt[n][kb], g1, pe[n][rt]);
                 }
             }
-            const int t = 16 * tt + li;
-            if (t < nvalid) {
-                const size_t at = (row0 + (size_t)t * p.H) * DK + ch0();
-                if constexpr (NK == 2) {
-                    TR::store8(p.dq + at, TR::cat(TR::from_f32(pq[0][rt]), TR::from_f32(pq[1][rt])));
-                    TR::store8(p.dk + at, TR::cat(TR::from_f32(pe[0][rt] - gk[0]), TR::from_f32(pe[1][rt] - gk[1])));
-                } else {
-                    TR::store(p.dq + at, TR::from_f32(pq[0][rt]));
-                    TR::store(p.dk + at, TR::from_f32(pe[0][rt] - gk[0]));
-                }
+            f32x4 x[NK];
+#pragma unroll
+            for (int n = 0; n < NK; ++n) x[n] = pq[n][rt];
+            put(p.dq, tt, x);
+        }
+        lds_barrier();
+#pragma unroll
+        for (int n = 0; n < NTI; ++n) symmetric(n);
+        lds_barrier();
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            const int tt = rt0 + rt;
+            f32x4 x[NK];
+#pragma unroll
+            for (int n = 0; n < NK; ++n) x[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int kb = 0; kb < 2; ++kb) {
+                const wfrag g2 = WD::load8(sG + (16 * tt + li) * L::LDC + 32 * kb + 8 * lg, L::PC);
+#pragma unroll
+                for (int n = 0; n < NK; ++n) x[n] = WD::ew(kt[n][kb], g2, x[n]);
             }
+#pragma unroll
+            for (int n = 0; n < NK; ++n) x[n] = pe[n][rt] - x[n];
+            put(p.dk, tt, x);
         }
     }
-    lds_barrier();
     if (wave >= 4) return;
     // dalpha: M_it = sum_j X_ij D_{t-1,j}, then D_it M_it summed over rows; row 0 of X is the
     // exit state's (its own has no j < 0), so row tile 0 is needed for every t.  Wave w has the
