@@ -346,7 +346,10 @@ int gdn_block_norm_forward(const void *x, const void *y, const void *gate, const
         // short ones: a new team's loads run beside an old one's stores.  us at 10560 x 2048 bf16 with
         // 1, 2, 3, 4 and 6 rows: 40, 33, 31, 30.5, 33; 100000 x 2048 with 3, 4, 6, 8 and 49: 364, 373, 386,
         // 383, 428; 30000 x 8192 (teams of 1024) with 1, 2, 4, 6, 8 and 15: 566, 437, 381, 363, 366, 377.
+        // Past 2^31 threads (rows of up to 512 channels from 2^27 on) strips grow with the rows: a launch
+        // has fewer than 2^32.
         p.strip_rows = std::min((R - 1) / 2048 + 1, norm_team(C) < 1024 ? 4 : 8);
+        p.strip_rows = std::max(p.strip_rows, (R - 1) / (INT32_MAX / norm_team(C)) + 1);
         p.strips = (R - 1) / p.strip_rows + 1;
         p.res_scale = res_scale;
         p.eps = eps;
