@@ -3,7 +3,10 @@ recurrent step of a decoding batch, the gradient of the token-wise chunk forward
 and the norms, gate and scaled residual between two blocks with their gradient.
 
 Thin binding like :mod:`.gdn`: argument checks and marshalling only.  Outputs and
-workspaces that are not given are allocated on the stream the call runs on.
+workspaces that are not given are allocated on the stream the call runs on.  No call
+records an autograd graph: results of inputs that require a gradient do not.  Tensors that
+a call is given to write count as modified in place, and while gradients are recorded may not require
+one.
 """
 import ctypes
 
@@ -49,8 +52,15 @@ def _raw_stream(index):
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _raw_stream)
 
 
-def _call(name, dev, *args):
-    """The C call with the current stream of `dev` behind its other arguments."""
+_modified = torch.autograd.graph.increment_version
+
+
+def _call(name, dev, *args, written=()):
+    """The C call with the current stream of `dev` behind its other arguments.  written: the
+    caller's own tensors among the outputs, whose saved uses autograd is told of."""
+    for t in written:
+        if t.requires_grad and torch.is_grad_enabled():
+            raise ValueError("a tensor that requires a gradient cannot be written while gradients are recorded")
     fn = getattr(_fns or _lib(), name)
     index = dev.index
     if torch.cuda.current_device() == index:
@@ -60,6 +70,8 @@ def _call(name, dev, *args):
             rc = fn(*args, _raw_stream(index))
     if rc != GDN_OK:
         raise GdnError(name, rc)
+    if written:
+        _modified(written)
 
 
 def _needs(dev, *specs):
@@ -155,12 +167,14 @@ def step(q, k, v, alpha, beta, state, *, slots=None, lengths=None, out=None, sta
                                       ("out", out, values, dt)):
             if t is not None:
                 _needs(dev, (name, t, shape, dtype))
+    written = (state_out, out)
     if out is None:
+        written = (state_out,)
         # every element is written unless a row may be short or padding
         out = torch.empty_like(v) if slots is None and lengths is None else torch.zeros_like(v)
     _call("gdn_step_forward", dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), alpha.data_ptr(), beta.data_ptr(),
           state.data_ptr(), _ptr(slots), _ptr(lengths), out.data_ptr(), state_out.data_ptr(), N, L, P, Hk, H, Dk, Dv,
-          1 if dt is _BF16 else 0)
+          1 if dt is _BF16 else 0, written=written)
     return out, state_out
 
 
@@ -196,6 +210,7 @@ def backward(q, k, v, alpha, beta, state_in, dout, dstate_out=None, *, dq=None, 
     for name, t in (("state_in", state_in), ("dstate_out", dstate_out)):
         if t is not None:
             _needs(dev, (name, t, (B, H, Dk, Dv), f32))
+    written = [t for t in (dq, dk, dv, dalpha, dbeta, dstate_in) if t is not None]
     dq = _given("dq", dq, q)
     dk = _given("dk", dk, k)
     dv = _given("dv", dv, v)
@@ -212,7 +227,7 @@ def backward(q, k, v, alpha, beta, state_in, dout, dstate_out=None, *, dq=None, 
     _call("gdn_chunk_backward", dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), alpha.data_ptr(), beta.data_ptr(),
           _ptr(state_in), dout.data_ptr(), _ptr(dstate_out), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
           dalpha.data_ptr(), dbeta.data_ptr(), _ptr(dstate_in), B, H, T, Dk, Dv, int(chunk),
-          1 if dt == torch.bfloat16 else 0, ws.data_ptr(), ws.numel())
+          1 if dt == torch.bfloat16 else 0, ws.data_ptr(), ws.numel(), written=written)
     return dq, dk, dv, dalpha, dbeta, dstate_in
 
 
@@ -263,10 +278,12 @@ def block_norm(x, y, gate, w_post, w_pre, *, gate_tokens=1, res_scale=1.0, eps=1
         with _on(stream, x):
             return block_norm(x, y, gate, w_post, w_pre, gate_tokens=gate_tokens, res_scale=res_scale, eps=eps, r=r, u=u)
     dt, dev, B, T, C, gt = _block_inputs(x, y, gate, w_post, w_pre, gate_tokens)
+    written = [t for t in (r, u) if t is not None]
     r = _given("r", r, x)
     u = _given("u", u, x)
     _call("gdn_block_norm_forward", dev, x.data_ptr(), y.data_ptr(), _ptr(gate), w_post.data_ptr(), w_pre.data_ptr(),
-          r.data_ptr(), u.data_ptr(), B * T, C, gt, float(res_scale), float(eps), 1 if dt == torch.bfloat16 else 0)
+          r.data_ptr(), u.data_ptr(), B * T, C, gt, float(res_scale), float(eps), 1 if dt == torch.bfloat16 else 0,
+          written=written)
     return r, u
 
 
@@ -284,6 +301,7 @@ def block_norm_backward(x, y, gate, w_post, w_pre, du, dr=None, *, gate_tokens=1
     _needs(dev, ("du", du, (B, T, C), dt))
     if dr is not None:
         _needs(dev, ("dr", dr, (B, T, C), dt))
+    written = [t for t in (dx, dy, dgate, dw_post, dw_pre) if t is not None]
     dx = _given("dx", dx, x)
     dy = _given("dy", dy, y)
     if gate is not None:
@@ -298,5 +316,6 @@ def block_norm_backward(x, y, gate, w_post, w_pre, du, dr=None, *, gate_tokens=1
         raise ValueError(f"ws must be a contiguous uint8 tensor on {dev}")
     _call("gdn_block_norm_backward", dev, x.data_ptr(), y.data_ptr(), _ptr(gate), w_post.data_ptr(), w_pre.data_ptr(),
           du.data_ptr(), _ptr(dr), dx.data_ptr(), dy.data_ptr(), _ptr(dgate), dw_post.data_ptr(), dw_pre.data_ptr(),
-          B * T, C, gt, float(res_scale), float(eps), 1 if dt == torch.bfloat16 else 0, ws.data_ptr(), ws.numel())
+          B * T, C, gt, float(res_scale), float(eps), 1 if dt == torch.bfloat16 else 0, ws.data_ptr(), ws.numel(),
+          written=written)
     return dx, dy, dgate, dw_post, dw_pre
