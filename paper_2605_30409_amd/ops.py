@@ -123,6 +123,14 @@ def _element(name, t):
     return dt, t.device
 
 
+def _int(name, n):
+    """A whole number of the caller's that the C call takes in 32 bits (and ctypes would cut)."""
+    i = int(n)
+    if i != n or not 0 <= i < 1 << 31:
+        raise ValueError(f"{name} must be a whole number below 2^31, got {n}")
+    return i
+
+
 def _dims(name, t, dims, text):
     shape = t.shape if isinstance(t, _Tensor) else ()
     if len(shape) != dims:
@@ -181,7 +189,10 @@ def step(q, k, v, alpha, beta, state, *, slots=None, lengths=None, out=None, sta
 def backward_workspace(q, v, chunk=_gdn.CHUNK):
     """Workspace tensor for backward on inputs shaped like q [B, T, H, Dk] and v [.., Dv]."""
     B, T, H, Dk = q.shape
-    n = _lib().gdn_chunk_backward_workspace_bytes(B, H, T, Dk, v.shape[-1], chunk, 1 if q.dtype == torch.bfloat16 else 0)
+    if max(B, T, H) >= 1 << 31:
+        raise ValueError(f"B, T and H must be below 2^31, got {list(q.shape)}")
+    n = _lib().gdn_chunk_backward_workspace_bytes(B, H, T, Dk, v.shape[-1], _int("chunk", chunk),
+                                                  1 if q.dtype == torch.bfloat16 else 0)
     if n == 0:
         raise ValueError("unsupported shape for the GDN chunk backward")
     return torch.empty(n, dtype=torch.uint8, device=q.device)
@@ -226,13 +237,17 @@ def backward(q, k, v, alpha, beta, state_in, dout, dstate_out=None, *, dq=None, 
         raise ValueError(f"ws must be a contiguous uint8 tensor on {dev}")
     _call("gdn_chunk_backward", dev, q.data_ptr(), k.data_ptr(), v.data_ptr(), alpha.data_ptr(), beta.data_ptr(),
           _ptr(state_in), dout.data_ptr(), _ptr(dstate_out), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
-          dalpha.data_ptr(), dbeta.data_ptr(), _ptr(dstate_in), B, H, T, Dk, Dv, int(chunk),
+          dalpha.data_ptr(), dbeta.data_ptr(), _ptr(dstate_in), B, H, T, Dk, Dv, _int("chunk", chunk),
           1 if dt == torch.bfloat16 else 0, ws.data_ptr(), ws.numel(), written=written)
     return dq, dk, dv, dalpha, dbeta, dstate_in
 
 
 def block_norm_workspace(rows, channels, gate_tokens, device):
     """Workspace tensor for block_norm_backward on `rows` tokens of `channels`."""
+    return _block_norm_ws(_int("rows", rows), _int("channels", channels), _int("gate_tokens", gate_tokens), device)
+
+
+def _block_norm_ws(rows, channels, gate_tokens, device):
     n = _lib().gdn_block_norm_workspace_bytes(rows, channels, gate_tokens)
     if n == 0:
         raise ValueError("unsupported shape for the block norm")
@@ -242,7 +257,7 @@ def block_norm_workspace(rows, channels, gate_tokens, device):
 def _block_inputs(x, y, gate, w_post, w_pre, gate_tokens):
     dt, dev = _element("x", x)
     B, T, C = _dims("x", x, 3, "[B, T, C]")
-    gt = int(gate_tokens)
+    gt = gate_tokens if type(gate_tokens) is int else _int("gate_tokens", gate_tokens)   # (one that divides T fits)
     if gt < 1 or T % gt:
         raise ValueError("T must be a whole number of runs of gate_tokens tokens")
     if max(B * T, C) >= 1 << 31:      # (the C call's sizes are 32-bit)
@@ -311,7 +326,7 @@ def block_norm_backward(x, y, gate, w_post, w_pre, du, dr=None, *, gate_tokens=1
     dw_post = _given("dw_post", dw_post, w_post)
     dw_pre = _given("dw_pre", dw_pre, w_pre)
     if ws is None:
-        ws = block_norm_workspace(B * T, C, gt, dev)
+        ws = _block_norm_ws(B * T, C, gt, dev)
     elif ws.device != dev or ws.dtype != torch.uint8 or not ws.is_contiguous():
         raise ValueError(f"ws must be a contiguous uint8 tensor on {dev}")
     _call("gdn_block_norm_backward", dev, x.data_ptr(), y.data_ptr(), _ptr(gate), w_post.data_ptr(), w_pre.data_ptr(),

@@ -22,3 +22,15 @@ def test_more_rows_than_a_launch_has_threads(gdn, C):
     for x, y in zip(got, ref):
         whole = R // n * n
         assert (x[:, :whole].view(-1, n, C) == y).all() and torch.equal(x[:, whole:], y[:, :R - whole])
+
+
+def test_gate_tokens_is_a_whole_number(gdn):
+    """1.5 is refused, not cut to 1."""
+    t = make(1, 6, 16, 1, "f32", 4)
+    args = (t["x"], t["y"], t["gate"], t["w_post"], t["w_pre"])
+    for bad in (1.5, (1 << 32) + 1, -1, 0):
+        with pytest.raises(ValueError):
+            gdn.block_norm(*args, gate_tokens=bad)
+        with pytest.raises(ValueError):
+            gdn.block_norm_backward(*args, t["du"], gate_tokens=bad)
+    check_forward(t, *gdn.block_norm(*args, gate_tokens=1.0), 1, 1.0)

@@ -151,3 +151,23 @@ def test_backward_workspace():
         assert want <= f(1, 16, 3520, 128, 128, 64, bf16) < want + 12 * 256
     with pytest.raises(ValueError, match="unsupported"):
         gdn.backward_workspace(torch.zeros(1, 3, 2, 32), torch.zeros(1, 3, 2, 64))
+
+
+@pytest.mark.parametrize("rows,channels,gate_tokens", [((1 << 32) + 12, 40, 4), (12, (1 << 32) + 40, 4), (12, 40, (1 << 32) + 4),
+                                                       (12, 40, 4.5), (12.5, 40, 1), (-12, 40, 4)])
+def test_norm_workspace_of_sizes_past_32_bits(rows, channels, gate_tokens):
+    """Sizes that 32 bits or whole numbers do not hold are refused, not cut to others."""
+    with pytest.raises(ValueError):
+        gdn.block_norm_workspace(rows, channels, gate_tokens, "cpu")
+    assert gdn.block_norm_workspace(12.0, 40, 4, "cpu").numel() == gdn.block_norm_workspace(12, 40, 4, "cpu").numel()
+
+
+def test_backward_workspace_of_sizes_past_32_bits():
+    one = torch.zeros(1, 1, 1, 64)
+    for shape in ((1, (1 << 32) + 100, 2), ((1 << 32) + 1, 100, 2), (1, 100, (1 << 32) + 2)):
+        q = one.expand(*shape, 64)
+        with pytest.raises(ValueError):
+            gdn.backward_workspace(q, q)
+    for chunk in ((1 << 32) + 64, 64.5):
+        with pytest.raises(ValueError):
+            gdn.backward_workspace(torch.zeros(1, 100, 2, 64), torch.zeros(1, 100, 2, 64), chunk)
