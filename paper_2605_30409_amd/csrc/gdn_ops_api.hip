@@ -174,11 +174,14 @@ bool back_shape_ok(int B, int H, int T) {
 
 template <class E, int DK, int DV> int launch_backward(const gdn::BackParams<E> &p, hipStream_t s) {
     using P = gdn::PrepLds<E, DK, DV>;
-    // bf16, Dk = 128: a workgroup of the scan that brings all its operands through LDS has a CU
+    // bf16, Dk = Dv = 128: a workgroup of the scan that brings all its operands through LDS has a CU
     // to itself; with first and add loaded directly two share one.  us at T = 3520, the ring's
     // first: 16 heads (one a CU) 103 and 109; 17 heads 175 and 152, 24 heads 196 and 194, 32 heads
-    // 221 and 210; 4 x 31 heads of T = 1320 332 and 326.
-    constexpr bool SHARE = sizeof(E) == 2 && DK == 128;
+    // 221 and 210; 4 x 31 heads of T = 1320 332 and 326.  Whole call: T = 1320, 17 heads 118 and 108, 24
+    // 131 and 131, 32 169 and 172, 48 252 and 247, 64 333 and 345; T = 3520, 17 heads 293 and 276, 32 432
+    // and 426.  Dv = 64 keeps the ring: T = 1320, 32 heads 118 and 120, 33 140 and 136, 40 153 and 154;
+    // T = 3520, 32 heads 274 and 279, 33 334 and 338, 48 433 and 436.
+    constexpr bool SHARE = sizeof(E) == 2 && DK == 128 && DV == 128;
     using S = gdn::BackScanLds<E, DK, false>;
     using D = gdn::BackScanLds<E, DK, SHARE>;
     using G = gdn::GradLds<E>;
@@ -205,9 +208,11 @@ template <class E, int DK, int DV> int launch_backward(const gdn::BackParams<E> 
         st = launch(gdn::gdn_back_scan_kernel<E, DK, DV, SHARE>, tiles, dim3(D::threads), D::bytes, s, p);
     else if (st == GDN_OK)
         st = launch(gdn::gdn_back_scan_kernel<E, DK, DV, false>, tiles, dim3(S::threads), S::bytes, s, p);
-    // Up to a workgroup a CU they have eight waves; from two on four. us with 8 and 4: 256 workgroups
+    // Up to a workgroup a CU they have eight waves; where CUs get a second one, four.  us with 8 and
+    // 4: 256 workgroups
     // of bf16, D = 64 16.2, 18.4; D = 128 27.1, 30.8; fp32, D = 64 25.1, 27.8; 512 of them
-    // 31.8, 26.1; 55.7, 46.9; 48.3, 40.8.
+    // 31.8, 26.1; 55.7, 46.9; 48.3, 40.8.  Whole call at 192, 256, 264, 320, 384 workgroups, bf16, D = 128: 72, 83,
+    // 107, 116, 129 and 75, 86, 98, 108, 121; fp32, D = 64: 78, 93, 117, 129, 142 and 81, 95, 109, 121, 135.
     if (st == GDN_OK)
         st = n <= 256 ? launch(gdn::gdn_back_grad_kernel<E, DK, DV, 2>, dim3(n), dim3(512), G::bytes, s, p)
                       : launch(gdn::gdn_back_grad_kernel<E, DK, DV, 1>, dim3(n), dim3(256), G::bytes, s, p);

@@ -3,7 +3,7 @@ shape, each head with values of its own, against the recurrence's adjoint in fp6
 reference and tolerances of test_gpu_backward).
 
 The last launch has four waves from 257 chunks and heads on and eight below; the scan of bf16 heads of
-Dk = 128 loads its operands directly from 17 heads of Dv = 128 or 33 of 64 on."""
+Dk = Dv = 128 loads its operands directly from 17 heads on (at Dv = 64 it has as many workgroups from 33 on)."""
 import pytest
 
 from test_gpu_backward import NAMES, TOL, adjoint, compare, host, make
