@@ -42,7 +42,10 @@ extern "C" {
  * takes its state over unchanged.  A negative slot marks padding: nothing of
  * that row is written.  A slot >= P, or one that an earlier row names already,
  * is refused on the device: the row's out (up to its length) becomes NaN and
- * no state is written for it; the first row that names a slot has it.
+ * no state is written for it; the first row that names a slot has it.  Finding
+ * that row takes time that grows with N^2: with slots in place of NULL, 4096 rows of 16 heads of 128
+ * take no longer, 16384 rows 11.3 in place of 6.8 ms; one head of 64: 1024 rows no
+ * longer, 4096 rows 29 in place of 21 us, 65536 rows 1.4 in place of 0.43 ms.
  * N, L, P, Hk, H >= 1, N H < 2^24; Dk, Dv in {64, 128}.  The call needs no workspace and may
  * be captured.
  */
@@ -65,7 +68,10 @@ int gdn_step_forward(const void *q, const void *k, const void *v, const float *a
  * gradients are those of the recurrence itself: alpha and beta of 0 have theirs
  * too (alpha below 1.2e-38 acts as that value, as in the forward).  Sums, states
  * and their gradients are fp32, and on the bf16 path too the operands of products
- * that are not inputs keep fp32's mantissa.  Results are deterministic.
+ * that are not inputs keep fp32's mantissa.  Results are deterministic.  A NaN
+ * or an infinity, given or where a sum leaves fp32's range, may make any gradient
+ * of its batch and head NaN, also those of earlier tokens and where fp32
+ * arithmetic would keep the infinity; other heads' are as without it.
  *
  * B H <= 65535, and B H chunks < 2^23.  Outputs may not overlap inputs or each other,
  * except dstate_in == dstate_out.
@@ -94,7 +100,8 @@ int gdn_chunk_backward(const void *q, const void *k, const void *v, const float 
  *   x, y, r, u  [R][C] E        gate [R / gate_tokens][C] E or NULL (all ones)
  *   w_post, w_pre [C] fp32      1 <= C <= 8192, any value; gate_tokens divides R
  *
- * u is formed from r before its rounding.  Sums and norms are fp32.  r may be x
+ * u is formed from r before its rounding.  Sums and norms are fp32 (a row whose
+ * squares sum to 2^128 or more has an infinite norm).  r may be x
  * or y itself and u may be y (whole buffers); outputs overlap nothing else.
  */
 int gdn_block_norm_forward(const void *x, const void *y, const void *gate, const float *w_post,

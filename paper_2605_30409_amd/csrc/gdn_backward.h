@@ -28,9 +28,9 @@
 // backward side by side (gdn_back_scan_kernel); per chunk all that remains
 // (gdn_back_grad_kernel).  bf16, Dk = Dv = 128, us and MB between the L2 caches and memory:
 //                      prep         scan          grad
-//   T = 3520,  H = 16   40, 175     100, 338       82, 280
-//   T = 10560, H = 16  107, 523     319, 1011     245, 845
-// A large copy reaches 4.7 TB/s: prep is there, the last launch at 3.5, and the scan, at 3.3, waits for
+//   T = 3520,  H = 16   42, 175     103, 338       90, 278
+//   T = 10560, H = 16  108, 523     319, 1011     255, 833
+// A large copy reaches 4.7 TB/s: prep is there, the last launch and the scan, at 3.2, are not: the scan waits for
 // its exchanges (its arithmetic alone, without loads and stores, takes 79 us of the 100).
 //
 // Precision: gate gradients and states are fp32 results, and dQ and dK sums whose terms
@@ -268,6 +268,7 @@ template <class E, int DK, int DV> struct PrepLds {
     static constexpr int waves_per_simd = bytes * 2 <= 160 * 1024 ? 4 : 2;
 };
 
+// (Four waves a SIMD have 128 registers; on the bf16 path one or two more are spilled.)
 constexpr int kPrepWaves = 8;
 
 // Lower tile t = 0..9 of a 4 x 4 grid of tiles: row and column tile.
@@ -849,6 +850,8 @@ template <class E> struct GradLds {
 
 // NH = 2: eight waves, four for each half of the tokens in the products over Dk, for launches that
 // leave every workgroup a CU of its own.
+// Registers: all 256 of two waves a SIMD at Dk = 128 and NH = 1, in bf16 five more than that (spilled to
+// scratch memory, 24 bytes a lane).
 template <class E, int DK, int DV, int NH>
 __global__ __launch_bounds__(256 * NH) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void gdn_back_grad_kernel(BackParams<E> p) {

@@ -16,6 +16,16 @@
 // read again only where it changes, and the sums over rows are kept in registers
 // until the strip ends.  10560 rows of 2048 channels, bf16: forward 31 to 35 us (173 MB at 4.9 to
 // 5.6 TB/s), gradient 54 to 57 us (272 MB at 4.7 to 5.0) and 5 us for its sums.
+// Whole calls at other widths, TB/s of what must move (172 MB forward, 258 MB gradient in bf16, twice that
+// in fp32):
+//   channels             32     64    128    256    512   1024   4096   5120   8192
+//   bf16 forward       0.78   1.47   2.72   4.75   5.18   4.85   4.95   3.42   3.82
+//        gradient      0.51   0.97   1.77   3.07   3.80   4.11   4.10   2.23   2.58
+//   fp32 forward       1.45   2.51   4.15   4.85   4.62   4.85   5.03   4.04   4.08
+//        gradient      1.04   1.90   3.25   4.34   4.26   4.46   4.44   2.64   2.84
+// Rows under 512 channels leave lanes of their wave without any (8 channels each).  Rows over 4096 take 1024
+// threads: at 5120 channels 3 in 8 of them have none, and in the gradient 128 registers a thread are too
+// few (16 spilled in bf16, 30 in fp32).
 #pragma once
 
 #include <type_traits>

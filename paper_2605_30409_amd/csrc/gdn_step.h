@@ -71,7 +71,8 @@ __global__ __launch_bounds__(64 * kStepWaves) void gdn_step_kernel(StepParams<E>
 #pragma unroll
         for (int i = 0; i < RPL; ++i) s[i] = *(const f32x4 *)(p.state_in + at + (size_t)i * DV);
     }
-    // a slot belongs to the first row that names it
+    // A slot belongs to the first row that names it: a row looks at those before it, 64 at a time (N^2 / 128
+    // loads a head and column tile; hidden behind the state's load up to some thousand rows, see gdn_ops.h).
     if (p.slots) {
         bool taken = false;
         for (int m = l; m < n; m += 64) taken |= p.slots[m] == slot;

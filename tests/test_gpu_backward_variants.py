@@ -48,6 +48,23 @@ def test_short_sequences_of_many_heads(gdn, dtype, Dk, Dv, H):
         compare(result(got, 0, h), adjoint(host(head(t, 0, h))), dtype, f"{H} heads {Dk}x{Dv} {dtype} head {h}")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("name", ["q", "k", "v", "dout", "state_in", "dstate_out"])
+def test_infinities_stay_in_their_head(gdn, dtype, name):
+    import torch
+    t = make(2, 150, 3, 64, 64, dtype, 60, mu=-1.0)
+    ref = gdn.backward(**t)
+    t[name][(1, 2, 3, 4) if "state" in name else (1, 70, 2, 7)] = float("inf")
+    got = gdn.backward(**t)
+    for n, a, b in zip(NAMES, ref, got):
+        for i in range(2):
+            for h in range(3):
+                if (i, h) != (1, 2):
+                    x, y = (z[i, h] if n == "dstate_in" else z[i, :, h] for z in (a, b))
+                    assert torch.equal(x, y), (n, i, h)
+    assert not all(x.isfinite().all() for x in got)
+
+
 def test_many_chunks_of_different_heads(gdn):
     """The last of 64 heads lies behind element 2^31 of the kept states and byte 2^32 of the workspace.
     Each head has one head's inputs with v and state_in times 2^i and dout and dstate_out times 2^j, (i, j)
