@@ -94,3 +94,22 @@ def test_many_chunks_of_different_heads(gdn):
             step = 2.0 ** -7 if r.dtype == torch.bfloat16 else 0.0
             over = ((y - r64).abs() - step * r64.abs()).clamp_min(0.0)
             assert y.isfinite().all() and float(over.norm()) <= 2 * TOL["bf16"] * float(r64.norm()), (name, h)
+
+
+@pytest.mark.parametrize("dtype,D", [("bf16", 64), ("f32", 64), ("bf16", 128)])
+def test_as_many_heads_as_are_allowed(gdn, dtype, D):
+    """65535 heads, a chunk and two tokens."""
+    import torch
+    room(100)
+    T, H = 66, 65535
+    g = torch.Generator(device="cuda").manual_seed(70 + D)
+    dt = torch.bfloat16 if dtype == "bf16" else torch.float32
+
+    def rn(*s):
+        return torch.randn(s, generator=g, device="cuda")
+    t = dict(q=torch.nn.functional.normalize(rn(1, T, H, D), dim=-1).to(dt), k=torch.nn.functional.normalize(rn(1, T, H, D), dim=-1).to(dt),
+             v=rn(1, T, H, D).to(dt), alpha=torch.sigmoid(rn(1, T, H) + 2.0), beta=torch.sigmoid(rn(1, T, H)), state_in=0.3 * rn(1, H, D, D),
+             dout=rn(1, T, H, D).to(dt), dstate_out=0.3 * rn(1, H, D, D))
+    got = gdn.backward(**t)
+    for h in (0, 32768, H - 1):
+        compare(result(got, 0, h), adjoint(host(head(t, 0, h))), dtype, f"{H} heads of {D} {dtype} head {h}")
