@@ -268,7 +268,7 @@ template <class E, int DK, int DV> struct PrepLds {
     static constexpr int waves_per_simd = bytes * 2 <= 160 * 1024 ? 4 : 2;
 };
 
-// (Four waves a SIMD have 128 registers; on the bf16 path one or two more are spilled.)
+// (Four waves a SIMD have 128 registers; one or two more are spilled in bf16 and at fp32 heads of 64.)
 constexpr int kPrepWaves = 8;
 
 // Lower tile t = 0..9 of a 4 x 4 grid of tiles: row and column tile.
