@@ -11,7 +11,14 @@ operator with its prologue and epilogue (``frame_forward_fused``).
 Around it (``include/gdn_ops.h``, :mod:`.ops`): the recurrent step of a decoding
 batch (``step``), the gradient of ``forward`` (``backward``), and the norms, gate and scaled residual between two blocks
 (``block_norm``, ``block_norm_backward``).
+
+The rest of a block and of a training step (``include/gdn_block.h``, :mod:`.block`): the gated linear map of a
+feed-forward block (``gated_linear``, ``gated_linear_backward``), the short causal convolution in front of the
+recurrence (``short_conv``, ``short_conv_backward``, ``short_conv_step``), and the norm and clipping of all gradients
+(``grad_norm``, ``clip_grads``).
 """
+from .block import (clip_grads, gated_linear, gated_linear_backward, gated_linear_workspace, grad_norm,  # noqa: F401
+                    grad_workspace, short_conv, short_conv_backward, short_conv_step, short_conv_workspace)
 from .gdn import (CHUNK, FRAME_STAGE_NAMES, STAGE_NAMES, GdnError, LIB_PATH,  # noqa: F401
                   default_key_scale, forward, frame_forward, frame_forward_bidir, frame_forward_fused,
                   frame_forward_norm, frame_workspace, fused_workspace, gdn_chunk_forward, gdn_frame_profile_stages_bidir,

@@ -8,10 +8,11 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libgdn.so")
-SOURCES = [os.path.join(CSRC, f) for f in ("gdn_api.hip", "gdn_ops_api.hip")]
-HEADERS = [os.path.join(CSRC, f) for f in ("gdn_backward.h", "gdn_device.h", "gdn_frame.h",
+SOURCES = [os.path.join(CSRC, f) for f in ("gdn_api.hip", "gdn_ops_api.hip", "gdn_block_api.hip")]
+HEADERS = [os.path.join(CSRC, f) for f in ("gdn_act.h", "gdn_backward.h", "gdn_clip.h", "gdn_conv.h",
+                                           "gdn_device.h", "gdn_frame.h", "gdn_gated.h", "gdn_host.h",
                                            "gdn_kernels.h", "gdn_norm.h", "gdn_step.h")] + \
-          [os.path.join(INCLUDE, f) for f in ("gdn.h", "gdn_ops.h")]
+          [os.path.join(INCLUDE, f) for f in ("gdn.h", "gdn_block.h", "gdn_ops.h")]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -9,33 +9,14 @@
 #include <type_traits>
 
 #include "gdn_backward.h"
+#include "gdn_host.h"
 #include "gdn_norm.h"
 #include "gdn_ops.h"
 #include "gdn_step.h"
 
 namespace {
 
-bool misaligned(const void *p, uintptr_t to = 16) { return ((uintptr_t)p & (to - 1)) != 0; }
-
-struct Range {
-    uintptr_t lo, hi;
-    Range(const void *p, size_t bytes) : lo((uintptr_t)p), hi((uintptr_t)p + (p ? bytes : 0)) {}
-    bool overlaps(const Range &o) const { return lo < o.hi && o.lo < hi; }
-    bool same(const Range &o) const { return lo == o.lo && hi == o.hi; }
-};
-
-// Launch one kernel whose only argument is a parameter struct; returns the
-// launch's own status (the thread's pending HIP error is neither read nor cleared).
-template <class P>
-int launch(void (*fn)(P), dim3 grid, dim3 block, size_t lds, hipStream_t s, const P &p) {
-    P copy = p;
-    void *args[] = {&copy};
-    return hipLaunchKernel((const void *)fn, grid, block, args, lds, s) == hipSuccess ? GDN_OK : GDN_ERR_HIP;
-}
-
 bool dims_ok(int Dk, int Dv) { return (Dk == 64 || Dk == 128) && (Dv == 64 || Dv == 128); }
-
-size_t align256(size_t x) { return (x + 255) & ~size_t(255); }
 
 // ---------------------------------------------------------------------------
 // Recurrent step.
