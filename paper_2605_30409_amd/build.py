@@ -18,11 +18,14 @@ HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
     # no packed fp32 VALU instructions in device code
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-    # MFMA accumulators in ordinary VGPRs: avoids AGPR<->VGPR copies whenever
-    # VALU code touches an accumulator (state scaling, bf16 conversion)
-    "-mllvm", "-amdgpu-mfma-vgpr-form=1",
     "-Wall", "-Wno-unused-function",
 ]
+
+
+# MFMA accumulators in ordinary VGPRs: avoids AGPR<->VGPR copies whenever
+# VALU code touches an accumulator (state scaling, bf16 conversion).  The tiled products of
+# gdn_block_api.hip only accumulate, and choose for themselves.
+VGPR_FORM = ["-mllvm", "-amdgpu-mfma-vgpr-form=1"]
 
 
 def build(verbose: bool = False, extra_flags=()) -> str:
@@ -37,7 +40,7 @@ def build(verbose: bool = False, extra_flags=()) -> str:
         subprocess.run(cmd, check=True)
 
     with ThreadPoolExecutor(len(jobs)) as pool:
-        list(pool.map(lambda j: run([hipcc, *flags, "-I", INCLUDE, "-I", CSRC, "-c", "-o", j[1], j[0]]), jobs))
+        list(pool.map(lambda j: run([hipcc, *flags, *([] if "gdn_block_api" in j[0] else VGPR_FORM), "-I", INCLUDE, "-I", CSRC, "-c", "-o", j[1], j[0]]), jobs))
     run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB + ".tmp", *(o for _, o in jobs)])
     os.replace(LIB + ".tmp", LIB)
     return LIB

@@ -11,8 +11,8 @@ namespace gdn {
 
 enum Act { kActNone = 0, kActSilu = 1, kActGelu = 2, kActGeluTanh = 3 };
 
-// 1 / (1 + e^-z); an e^-z past fp32's range gives 0.
-__device__ __forceinline__ float logistic(float z) { return 1.f / (1.f + __expf(-z)); }
+// 1 / (1 + e^-z) by the hardware's reciprocal (within 1 ulp); an e^-z past fp32's range gives 0.
+__device__ __forceinline__ float logistic(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
 
 __device__ __forceinline__ float normal_cdf(float z) { return 0.5f * erfcf(-0.70710678f * z); }
 

@@ -34,18 +34,63 @@ bool gated_shape_ok(int M, int C, int F) {
            (M / 64 + 1LL) * (F / 64 + 1LL) < (1LL << 23) && (M / 64 + 1LL) * (C / 64 + 1LL) < (1LL << 23);
 }
 
+// How one of the products is cut: tiles of BM x BN and parts of the contraction.
+struct GatedCut {
+    int BM, BN, splits;
+    int rows, pitch;             // of a part's sums
+    long long tiles;
+};
+
+GatedCut gated_cut(int kind, int M, int C, int F, bool bf16) {
+    const bool fwd = kind == gdn::kGatedFwd || kind == gdn::kGatedD;
+    const int Fp = (F + 63) / 64 * 64, KB = bf16 ? 64 : 32;
+    const long long cols = fwd ? 2LL * F : C;
+    GatedCut g;
+    g.rows = kind == gdn::kGatedDw ? 2 * Fp : M;
+    g.pitch = fwd ? 2 * Fp : (C + 7) / 8 * 8;
+    const int stages = fwd ? (C - 1) / KB + 1 : kind == gdn::kGatedDx ? 2 * ((F - 1) / KB + 1) : (M - 1) / KB + 1;
+    // The cheapest by what stages were measured to take, us: of a tile that has its CU to itself, and of the one or two that a
+    // CU holds on a full chip.
+    const struct {
+        int BM, BN, slots;
+        float one, full;
+    } size[] = {{256, 256, 1, bf16 ? 1.45f : 4.3f, bf16 ? 1.45f : 4.3f},
+                {128, 128, 2, bf16 ? .62f : 1.9f, bf16 ? 1.2f : 3.05f},
+                {64, 128, 2, bf16 ? .45f : 1.25f, bf16 ? .8f : 1.95f}};
+    float best = INFINITY;
+    for (const auto &t : size) {
+        const long long tiles = ((long long)g.rows + t.BM - 1) / t.BM * ((cols + t.BN - 1) / t.BN);
+        for (int splits = 1; splits <= 16 && splits * 4 <= stages + 3; ++splits) {
+            const long long n = tiles * splits, rounds = n / (256 * t.slots), left = n % (256 * t.slots);
+            if (splits > 1 && n > 256 * t.slots) break;
+            float us = (rounds * t.full + (left == 0 ? 0 : left <= 256 ? t.one : t.full)) * ((stages + splits - 1) / splits + 3);
+            if (splits > 1) us += 4 + 2e-6f * splits * g.rows * g.pitch;        // a launch, and the sums out and in at 4 TB/s
+            if (us < best) {
+                best = us;
+                g.BM = t.BM;
+                g.BN = t.BN;
+                g.tiles = tiles;
+                g.splits = splits;
+            }
+        }
+    }
+    return g;
+}
+
 // Where the parts of the workspace begin.
 struct GatedLayout {
-    size_t x, wg, wu, d, total;
+    size_t x, wg, wu, d, part, total;
     bool pack;
     int ld, Fp;
 };
 GatedLayout gated_layout(int M, int C, int F, bool bf16, bool backward) {
     GatedLayout L{};
     const size_t esz = bf16 ? 2 : 4;
-    L.pack = C * esz % 16 != 0 && (backward || M > kSkinnyRows);
-    L.ld = L.pack ? (C + 63) / 64 * 64 : C;
     L.Fp = (F + 63) / 64 * 64;
+    L.ld = C;
+    if (!backward && M <= kSkinnyRows) return L;
+    L.pack = C * esz % 16 != 0;
+    if (L.pack) L.ld = (C + 63) / 64 * 64;
     size_t off = 0;
     auto take = [&](size_t n) {
         const size_t at = off;
@@ -58,32 +103,44 @@ GatedLayout gated_layout(int M, int C, int F, bool bf16, bool backward) {
         L.wu = take((size_t)F * L.ld * esz);
     }
     if (backward) L.d = take((size_t)M * 2 * L.Fp * esz);
+    size_t part = 0;
+    for (int kind = backward ? gdn::kGatedD : gdn::kGatedFwd; kind <= (backward ? gdn::kGatedDw : gdn::kGatedFwd); ++kind) {
+        const GatedCut g = gated_cut(kind, M, C, F, bf16);
+        if (g.splits > 1) part = std::max(part, (size_t)g.splits * g.rows * g.pitch * 4);
+    }
+    L.part = take(part);
     L.total = off;
     return L;
 }
 
-template <class E, int KIND, int BM, int BN, int WM, int WN> int launch_tiles(gdn::GatedParams<E> p, hipStream_t s) {
-    constexpr bool FWD = KIND == gdn::kGatedFwd || KIND == gdn::kGatedD;
-    constexpr size_t lds = 2 * (BM + BN) * 128;
-    const auto fn = gdn::gdn_gated_tile_kernel<E, KIND, BM, BN, WM, WN>;
+template <class E, int KIND, int BM, int BN, int WM, int WN, int DEPTH> int launch_tiles(const gdn::GatedParams<E> &p, hipStream_t s) {
+    constexpr size_t lds = DEPTH * (BM + BN) * 128;
+    const auto fn = gdn::gdn_gated_tile_kernel<E, KIND, BM, BN, WM, WN, DEPTH>;
     static std::once_flag once;
     static hipError_t attr = hipSuccess;
     std::call_once(once, [&] {
         attr = hipFuncSetAttribute((const void *)fn, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     });
     if (attr != hipSuccess) return GDN_ERR_HIP;
-    const int rows = KIND == gdn::kGatedDw ? 2 * p.Fp : p.M, cols = FWD ? p.F : p.C;
-    p.tiles_m = (rows + BM - 1) / BM;
-    p.tiles_n = (cols + (FWD ? BN / 2 : BN) - 1) / (FWD ? BN / 2 : BN);
-    return launch(fn, dim3((unsigned)(p.tiles_m * p.tiles_n)), dim3(64 * WM * WN), lds, s, p);
+    return launch(fn, dim3((unsigned)(p.tiles_m * p.tiles_n * p.splits)), dim3(64 * WM * WN), lds, s, p);
 }
 
-template <class E, int KIND> int run_tiles(const gdn::GatedParams<E> &p, hipStream_t s) {
+template <class E, int KIND> int run_tiles(gdn::GatedParams<E> p, hipStream_t s) {
     constexpr bool FWD = KIND == gdn::kGatedFwd || KIND == gdn::kGatedD;
-    const long long rows = KIND == gdn::kGatedDw ? 2 * p.Fp : p.M, cols = FWD ? 2LL * p.F : p.C;
-    const long long large = ((rows + 255) / 256) * ((cols + 255) / 256);
-    if (large >= 192) return launch_tiles<E, KIND, 256, 256, 2, 4>(p, s);
-    return launch_tiles<E, KIND, 128, 128, 2, 2>(p, s);
+    const GatedCut g = gated_cut(KIND, p.M, p.C, p.F, sizeof(E) == 2);
+    const int cols = FWD ? p.F : p.C, wide = FWD ? g.BN / 2 : g.BN;
+    p.rows = g.rows;
+    p.pitch = g.pitch;
+    p.splits = g.splits;
+    p.tiles_m = (g.rows + g.BM - 1) / g.BM;
+    p.tiles_n = (cols + wide - 1) / wide;
+    const bool alone = g.tiles * g.splits <= 256;      // a CU each
+    const int st = g.BM == 256   ? launch_tiles<E, KIND, 256, 256, 2, 4, 2>(p, s)
+                   : g.BM == 128 ? (alone ? launch_tiles<E, KIND, 128, 128, 2, 2, 4>(p, s) : launch_tiles<E, KIND, 128, 128, 2, 2, 2>(p, s))
+                                 : (alone ? launch_tiles<E, KIND, 64, 128, 2, 2, 6>(p, s) : launch_tiles<E, KIND, 64, 128, 2, 2, 3>(p, s));
+    if (st != GDN_OK || g.splits == 1) return st;
+    const long long units = (long long)g.rows * ((FWD ? p.Fp : g.pitch) / 8);
+    return launch(gdn::gdn_gated_join_kernel<E, KIND>, dim3((unsigned)((units + 255) / 256)), dim3(256), 0, s, p);
 }
 
 template <class E> int pack(const void *src, void *dst, long long rows, int C, int ld, hipStream_t s) {
@@ -110,6 +167,7 @@ template <class E> int run_gated(gdn::GatedParams<E> p, const GatedLayout &L, un
         p.wu = (const E *)(ws + L.wu);
     }
     if (st != GDN_OK) return st;
+    p.part = (float *)(ws + L.part);
     if (!backward) return run_tiles<E, gdn::kGatedFwd>(p, s);
     p.d = (E *)(ws + L.d);
     st = run_tiles<E, gdn::kGatedD>(p, s);

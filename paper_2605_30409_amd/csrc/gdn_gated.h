@@ -28,9 +28,38 @@ template <class E> struct GatedParams {
     E *h, *d, *dx, *dwg, *dwu;
     long long ldx, ldw;          // elements from row to row of x and the weights
     int M, C, F, Fp;
+    float *part;                 // sums of `splits` parts of the contraction: [split][rows][pitch]
     int act;
-    int tiles_m, tiles_n;
+    int tiles_m, tiles_n, splits;
+    int rows, pitch;             // of a part: pitch a multiple of 8; kGatedFwd, kGatedD: g at column n, u at Fp + n
 };
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+// 32 x 32 x 16 products: lane l = 32 h + i has k = 8 h .. 8 h + 7 of the operands' row i, and of the result D[8 b + 4 h + q][i] at
+// 4 b + q.
+__device__ __forceinline__ f32x16 mma_32(u32x4 a, u32x4 b, f32x16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// The column of 32 that the N side's tile row r stands for: a lane then has 16 consecutive ones, 16 h + e at e.
+__device__ __forceinline__ int n_order(int r) { return 16 * ((r >> 2) & 1) + 4 * (r >> 3) + (r & 3); }
+
+// 8 fp32 values (two granules) as the sum of three bf16 planes, exactly: 8 bits of the mantissa each, cut off, not
+// rounded, so that no plane overflows.  (What is infinite becomes NaN; planes of values below 2^-110 may be lost.)
+__device__ __forceinline__ void planes(u32x4 lo, u32x4 hi, u32x4 *p) {
+    uint32_t x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            p[k][i] = __builtin_amdgcn_perm(x[2 * i + 1], x[2 * i], 0x07060302);     // the high halves of both
+            if (k < 2) {
+#pragma unroll
+                for (int e = 2 * i; e < 2 * i + 2; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) - __uint_as_float(x[e] & 0xffff0000u));
+            }
+        }
+}
 
 enum GatedKind { kGatedFwd, kGatedD, kGatedDx, kGatedDw };
 
@@ -123,12 +152,16 @@ template <class E, int MT> __global__ __launch_bounds__(64 * kSkinnyWaves) void 
 // Tiles.
 
 // One asynchronous copy: lane l's 16 bytes to LDS at `lds` + 16 l.  (As assembly, so that the compiler does
-// not wait for it before every read of LDS; it has no output register.  M0 holds the LDS address.)
+// not wait for it before every read of LDS; it has no output register, and M0 holds the LDS address.  What orders it is the
+// wait and barrier in front of the reads, and the barrier behind the last reads of what it overwrites: both are
+// volatile, too, and memory accesses do not cross them.)
 __device__ __forceinline__ void copy_tile(const void *base, uint32_t off, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(lds), "v"(off), "s"(base) : "memory");
+    const uint64_t at = (uint64_t)base;
+    const uint64_t s = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(off), "s"(s));
 }
 __device__ __forceinline__ void copy_lane(const void *src, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(lds), "v"(src) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(src));
 }
 
 __device__ const u32x4 kZeroGranule = {0u, 0u, 0u, 0u};
@@ -146,8 +179,7 @@ template <class E, bool COLS, int R, int NW> struct Operand {
     // COLS: place of granule g of row k.  Four rows that a transposed read takes at once, 16 bytes apart, lie 64
     // bytes apart after it (bf16); fp32 reads 4 rows k, k + 4, .. of 64 bytes each.
     static __device__ __forceinline__ int place(int k, int g) {
-        if (sizeof(E) == 2) return g ^ ((k & 3) << 2) ;
-        return g ^ (((k >> 2) & 3) << 2);
+        return g ^ (((sizeof(E) == 2 ? k : k >> 2) & 3) << 2 & (GR - 1));
     }
     // row(r): memory row of the tile's row r, or for COLS granule(g): first column of granule g
     template <class Row> __device__ __forceinline__ void init(int wave, int lane, long long ld, Row row) {
@@ -159,44 +191,42 @@ template <class E, bool COLS, int R, int NW> struct Operand {
                 const int k = at / GR, g = place(k, at % GR);
                 off[i] = (uint32_t)(((long long)k * ld + row(g)) * (long long)sizeof(E));
             } else {
-                const int r = at / 8, g = (at & 7) ^ (r & 7);
+                const int r = at / 8, g = (at & 7) ^ ((r >> 1) & 7);
                 off[i] = (uint32_t)((row(r) * ld + g * EG) * (long long)sizeof(E));
             }
         }
     }
-    __device__ __forceinline__ void stage(const E *base, uint32_t lds) const {
-#pragma unroll
-        for (int i = 0; i < COPIES; ++i) copy_tile(base, off[i], lds + (w + i * NW) * 1024);
-    }
-    // A stage with `k` < KB valid elements of the contraction: zeros behind them.
-    __device__ __forceinline__ void stage_tail(const E *base, uint32_t lds, int k) const {
-#pragma unroll
-        for (int i = 0; i < COPIES; ++i) {
+    // Copy i of a stage; TAIL: of one with `k` < KB valid elements of the contraction, zeros behind them.
+    template <bool TAIL> __device__ __forceinline__ void copy(int i, const E *base, uint32_t lds, int k) const {
+        const uint32_t to = lds + (w + i * NW) * 1024;
+        if constexpr (TAIL) {
             const int at = (w + i * NW) * 64 + l;
-            const int e = COLS ? at / GR : ((at & 7) ^ ((at / 8) & 7)) * EG;
-            copy_lane(e < k ? (const char *)base + off[i] : (const char *)&kZeroGranule, lds + (w + i * NW) * 1024);
+            const int e = COLS ? at / GR : ((at & 7) ^ ((at / 16) & 7)) * EG;
+            copy_lane(e < k ? (const char *)base + off[i] : (const char *)&kZeroGranule, to);
+        } else {
+            copy_tile(base, off[i], to);
         }
     }
-    // Granule kk (of two 64-byte halves) of tile t's 16 rows; P32: tiles 2 j, 2 j + 1 stand for 32 columns in
-    // P32 order (for ROWS the order is in the staged rows).
-    template <bool P32> static __device__ __forceinline__ u32x4 frag(const unsigned char *tile, int r0, int t, int kk, int li, int lg) {
+    // k = 8 (2 kk + h) .. + 7 (bf16: granules 2 kk + h; fp32: 4 kk + 2 h + part) of row i of tile t; N: in n_order (for ROWS the
+    // order is in the staged rows).
+    template <bool N> static __device__ __forceinline__ u32x4 frag(const unsigned char *tile, int r0, int t, int kk, int part, int i, int h) {
         if constexpr (!COLS) {
-            const int r = r0 + 16 * t + li;
-            return *(const u32x4 *)(tile + r * 128 + (((lg + 4 * kk) ^ (li & 7)) << 4));
+            const int r = r0 + 32 * t + i, g = sizeof(E) == 2 ? 2 * kk + h : 4 * kk + 2 * h + part;
+            return *(const u32x4 *)(tile + r * 128 + ((g ^ ((i >> 1) & 7)) << 4));
         } else if constexpr (sizeof(E) == 2) {
             typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-            const int k = 32 * kk + 8 * lg + (li >> 2);
-            const int c = P32 ? r0 + 32 * (t >> 1) + 8 * (li & 3) + 4 * (t & 1) : r0 + 16 * t + 4 * (li & 3);
+            const int k = 16 * kk + 8 * h + ((i >> 2) & 3), block = 4 * (i >> 4) + (i & 3);
+            const int c = r0 + 32 * t + (N ? 16 * (block & 1) + 4 * (block >> 1) : 4 * block);
             auto at = [&](int kr) { return (lds_i16x4 *)(tile + kr * (2 * R) + place(kr, c >> 3) * 16 + (c & 7) * 2); };
             const i16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at(k));
             const i16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16(at(k + 4));
             return Tr<uint16_t>::cat(__builtin_bit_cast(u32x2, lo), __builtin_bit_cast(u32x2, hi));
         } else {
-            const int c = P32 ? r0 + 32 * (t >> 1) + p32_row(t & 1, li) : r0 + 16 * t + li;
+            const int c = r0 + 32 * t + (N ? n_order(i) : i);
             u32x4 f;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int k = 16 * kk + 4 * lg + j;
+                const int k = 16 * kk + 8 * h + 4 * part + j;
                 f[j] = *(const uint32_t *)(tile + k * (4 * R) + place(k, c >> 2) * 16 + (c & 3) * 4);
             }
             return f;
@@ -215,24 +245,66 @@ template <class E> __device__ __forceinline__ void store_row(E *row, int n, int 
     }
 }
 
-template <class E, int KIND, int BM, int BN, int WM, int WN>
+// dh of row m, columns n .. n + 7, as far as they are there.
+template <class E> __device__ __forceinline__ Vec8<E> gated_dh(const GatedParams<E> &p, int m, int n) {
+    Vec8<E> e{};
+    const E *row = p.dh + (size_t)m * p.F;
+    if (n + 8 <= p.F) e.load(row + n);
+    else if (n < p.F) e.load_some(row + n, p.F - n);
+    return e;
+}
+
+// What becomes of 8 sums of row m, columns n .. n + 7 (kGatedFwd, kGatedD: v of g and u of u).
+template <class E, int KIND>
+__device__ __forceinline__ void gated_result(const GatedParams<E> &p, int m, int n, float *v, float *u, const Vec8<E> &e) {
+    if constexpr (KIND == kGatedFwd) {
+        act_all<8>(v, p.act);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] *= u[q];
+        store_row(p.h + (size_t)m * p.F, n, p.F, v);
+    } else if constexpr (KIND == kGatedD) {
+        if (n >= p.Fp) return;
+        float dh[8];
+        e.values(dh);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            float a, s;
+            act_and_slope(v[q], p.act, a, s);
+            const bool on = n + q < p.F;
+            v[q] = on ? dh[q] * u[q] * s : 0.f;
+            u[q] = on ? dh[q] * a : 0.f;
+        }
+        E *d = p.d + (size_t)m * 2 * p.Fp + n;
+        Vec8<E>::store(d, v);
+        Vec8<E>::store(d + p.Fp, u);
+    } else if constexpr (KIND == kGatedDx) {
+        store_row(p.dx + (size_t)m * p.C, n, p.C, v);
+    } else {
+        const int f = m < p.Fp ? m : m - p.Fp;
+        if (f < p.F) store_row((m < p.Fp ? p.dwg : p.dwu) + (size_t)f * p.C, n, p.C, v);
+    }
+}
+
+template <class E, int KIND, int BM, int BN, int WM, int WN, int DEPTH>
 __global__ __launch_bounds__(64 * WM * WN, 2) void gdn_gated_tile_kernel(GatedParams<E> p) {
     constexpr bool FWD = KIND == kGatedFwd || KIND == kGatedD;
-    constexpr int NW = WM * WN, MT = BM / WM / 16, NT = BN / WN / 16;
+    constexpr int NW = WM * WN, MT = BM / WM / 32, NT = BN / WN / 32;
     using OpN = Operand<E, !FWD, BN, NW>;
     using OpM = Operand<E, KIND == kGatedDw, BM, NW>;
     constexpr int KB = OpN::KB, EG = OpN::EG, STAGE = (BM + BN) * 128;
     extern __shared__ __align__(1024) unsigned char smem[];
-    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, li = l & 15, lg = l >> 4;
+    const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, li = l & 31, lh = l >> 5;
     const int wm = w / WN, wn = w % WN;
 
     // Tiles of an XCD (workgroups go to the 8 of them in turn) are neighbours: runs of 8 rows of tiles, column by
     // column, so that what its CUs read together fits its L2.
-    int tm, tn;
+    int tm, tn, split;
     {
-        const int total = p.tiles_m * p.tiles_n, per = total / 8, more = total % 8;
+        const int tiles = p.tiles_m * p.tiles_n, total = tiles * p.splits, per = total / 8, more = total % 8;
         const int xcd = blockIdx.x % 8;
-        const int id = xcd * per + min(xcd, more) + blockIdx.x / 8;
+        int id = xcd * per + min(xcd, more) + blockIdx.x / 8;
+        split = id / tiles;
+        id -= split * tiles;
         constexpr int RUN = 8;
         const int run = id / (RUN * p.tiles_n), in = id - run * RUN * p.tiles_n;
         const int height = min(RUN, p.tiles_m - run * RUN);
@@ -245,163 +317,250 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gdn_gated_tile_kernel(GatedPa
     OpM om;
     const E *bn, *bn2 = nullptr, *bm;
     long long step_n = KB, step_m = KB;        // elements from stage to stage
-    int stages, half = 0, tail;                // kGatedDx: stages of Wg
+    int whole, tails, tail;                    // stages that are whole; behind them those that are not, and how long those are
     if constexpr (FWD) {
-        // rows 64 j + 32 s + 16 a + i of the tile: hidden unit 32 j + p32_row(a, i) of Wg (s = 0) or Wu (s = 1); the
-        // two weights' distance goes into the offset of the second half of the copies
         bn = p.wg;
         bm = p.x + (long long)m0 * p.ldx;
         om.init(w, l, p.ldx, [&](int r) { return (long long)min(r, p.M - 1 - m0); });
-        stages = (p.C + KB - 1) / KB;
-        tail = p.C - (stages - 1) * KB;
+        whole = p.C / KB;
+        tail = p.C % KB;
+        tails = tail ? 1 : 0;
     } else if constexpr (KIND == kGatedDx) {
         bn = p.wg;
         bn2 = p.wu;
         bm = p.d + (long long)m0 * 2 * p.Fp;
         on.init(w, l, p.ldw, [&](int g) { return (long long)min(n0 + g * EG, (p.C - 1) / EG * EG); });
         om.init(w, l, 2 * p.Fp, [&](int r) { return (long long)min(r, p.M - 1 - m0); });
-        half = p.Fp / KB;
-        stages = 2 * half;
-        tail = 0;
+        whole = 2 * (p.F / KB);
+        tail = p.F % KB;
+        tails = tail ? 2 : 0;
         step_n = (long long)KB * p.ldw;
     } else {
         bn = p.x;
         bm = p.d;
         on.init(w, l, p.ldx, [&](int g) { return (long long)min(n0 + g * EG, (p.C - 1) / EG * EG); });
         om.init(w, l, 2 * p.Fp, [&](int g) { return (long long)min(m0 + g * EG, 2 * p.Fp - EG); });
-        stages = (p.M + KB - 1) / KB;
-        tail = p.M - (stages - 1) * KB;
+        whole = p.M / KB;
+        tail = p.M % KB;
+        tails = tail ? 1 : 0;
         step_n = (long long)KB * p.ldx;
         step_m = (long long)KB * 2 * p.Fp;
     }
-    // FWD: Wg's rows and Wu's through bases of their own
+    // FWD: row 64 j + 32 s + i of the tile is hidden unit 32 j + n_order(i) of Wg (s = 0) or Wu (s = 1)
     const E *wrow[2];
     if constexpr (FWD) {
         wrow[0] = p.wg + (long long)n0 * p.ldw;
         wrow[1] = p.wu + (long long)n0 * p.ldw;
         on.init(w, l, p.ldw, [&](int r) {
-            return (long long)min(32 * (r >> 6) + p32_row((r >> 4) & 1, r & 15), p.F - 1 - n0);
+            return (long long)min(32 * (r >> 6) + n_order(r & 31), p.F - 1 - n0);
         });
     }
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)smem;
 
-    auto stage = [&](int s) {
-        const uint32_t lds = lds0 + (s & 1) * STAGE;
-        if constexpr (FWD) {
-            const bool end = s == stages - 1 && tail < KB;
-            // a copy holds 8 rows: all of Wg or all of Wu
-#pragma unroll
-            for (int i = 0; i < OpN::COPIES; ++i) {
-                const int c = w + i * NW;
-                const E *base = wrow[(c >> 2) & 1] + (long long)s * KB;
-                const uint32_t to = lds + BM * 128 + c * 1024;
-                if (!end) copy_tile(base, on.off[i], to);
-                else copy_lane(((l & 7) ^ ((l >> 3) & 7)) * EG < tail ? (const char *)base + on.off[i] : (const char *)&kZeroGranule, to);
-            }
-            const E *xb = bm + (long long)s * KB;
-            if (!end) om.stage(xb, lds);
-            else om.stage_tail(xb, lds, tail);
-        } else if constexpr (KIND == kGatedDx) {
-            const int f = (s < half ? s : s - half) * KB;
-            const E *base = (s < half ? bn : bn2) + (long long)f * p.ldw;
-            if (f + KB <= p.F) on.stage(base, lds + BM * 128);
-            else on.stage_tail(base, lds + BM * 128, p.F - f);
-            om.stage(bm + (long long)s * KB, lds);
+    // Copy c of stage s to the buffer at `to`.
+    auto copy = [&](int c, int s, uint32_t to, auto is_tail) {
+        constexpr bool TAIL = decltype(is_tail)::value;
+        const uint32_t lds = lds0 + to;
+        // kGatedDx: Wg's stages, Wu's, and what is left of both
+        int part = 0, at = s;
+        if constexpr (KIND == kGatedDx) {
+            const int half = whole / 2;
+            part = TAIL ? s - whole : s >= half;
+            at = TAIL ? half : s - part * half;
+        }
+        if (c < OpN::COPIES) {
+            const E *base;
+            // FWD: a copy holds 8 rows, all of Wg or all of Wu
+            if constexpr (FWD) base = wrow[((w + c * NW) >> 2) & 1];
+            else base = KIND == kGatedDx && part ? bn2 : bn;
+            on.template copy<TAIL>(c, base + at * step_n, lds + BM * 128, tail);
         } else {
-            const bool end = s == stages - 1 && tail < KB;
-            if (!end) {
-                on.stage(bn + s * step_n, lds + BM * 128);
-                om.stage(bm + s * step_m, lds);
-            } else {
-                on.stage_tail(bn + s * step_n, lds + BM * 128, tail);
-                om.stage_tail(bm + s * step_m, lds, tail);
-            }
+            om.template copy<TAIL && KIND != kGatedDx>(c - OpN::COPIES, bm + (long long)part * p.Fp + at * step_m, lds, tail);
         }
     };
 
-    f32x4 acc[MT][NT];
+    f32x16 acc[MT][NT];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NT; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
 
-    stage(0);
-    for (int s = 0; s < stages; ++s) {
-        asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
-        if (s + 1 < stages) stage(s + 1);
-        const unsigned char *tm_ = smem + (s & 1) * STAGE, *tn_ = tm_ + BM * 128;
+    const int stages = whole + tails;
+    const int first = (int)((long long)stages * split / p.splits), end = (int)((long long)stages * (split + 1) / p.splits);
+    // DEPTH buffers, as many stages on their way.
+    constexpr int COPIES = OpN::COPIES + OpM::COPIES;
+    uint32_t ahead = 0, here = 0;
+    auto turn = [](uint32_t &at) { at = at == (DEPTH - 1) * STAGE ? 0 : at + STAGE; };
+    auto stage = [&](int s) {
+        if (s >= end) return;
 #pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            u32x4 a[NT], b[MT];
+        for (int c = 0; c < COPIES; ++c) {
+            if (s < whole) copy(c, s, ahead, std::false_type{});
+            else copy(c, s, ahead, std::true_type{});
+        }
+        turn(ahead);
+    };
+    // stage s is there, for all waves, and what this wave asked of LDS too
+    auto arrived = [&](int s) {
+        if (DEPTH > 2 && s + DEPTH - 2 < end) asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"((DEPTH - 2) * COPIES) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    };
+    auto rows_n = [&](uint32_t at, int j, int kk, int part) {
+        return OpN::template frag<true>(smem + at + BM * 128, wn * (BN / WN), j, kk, part, li, lh);
+    };
+    auto rows_m = [&](uint32_t at, int i, int kk, int part) {
+        return OpM::template frag<false>(smem + at, wm * (BM / WM), i, kk, part, li, lh);
+    };
 #pragma unroll
-            for (int j = 0; j < NT; ++j) a[j] = OpN::template frag<true>(tn_, wn * (BN / WN), j, kk, li, lg);
+    for (int i = 0; i < DEPTH - 1; ++i) stage(first + i);
+    arrived(first);
+    stage(first + DEPTH - 1);
+    if constexpr (sizeof(E) == 2) {
+        // Operands are read a step of 16 ahead of their products, also across stages: a stage's last ones are in
+        // registers when all waves meet, so its buffer is free for the stage DEPTH on, and products to
+        // do are left for the time until the next stage's first operands are there.  Products, reads and
+        // copies are dealt out evenly, a row of products at a time.
+        constexpr int ROW = (NT + MT + MT - 1) / MT, COPY = (COPIES + MT - 1) / MT;
+        u32x4 a[2][NT], b[2][MT];
+        // the r-th operand of step kk
+        auto read = [&](uint32_t at, int kk, int r) {
+            if (r < NT) a[kk & 1][r] = rows_n(at, r, kk, 0);
+            else if (r < NT + MT) b[kk & 1][r - NT] = rows_m(at, r - NT, kk, 0);
+        };
+        auto products = [&](int kk, int i) {
 #pragma unroll
-            for (int i = 0; i < MT; ++i) b[i] = OpM::template frag<false>(tm_, wm * (BM / WM), i, kk, li, lg);
+            for (int j = 0; j < NT; ++j) acc[i][j] = mma_32(a[kk & 1][j], b[kk & 1][i], acc[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        // Stage s, with the copies of stage s + DEPTH, if that is a whole one, between the last products.
+        auto step = [&](int s, auto copies) {
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+                if (kk == 3) {
+                    arrived(s + 1);
+                    turn(here);
+                    if (!decltype(copies)::value) stage(s + DEPTH);
+                }
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+#pragma unroll
+                    for (int r = ROW * i; r < ROW * i + ROW; ++r) read(here, (kk + 1) & 3, r);
+                    if (kk == 3 && decltype(copies)::value) {
+#pragma unroll
+                        for (int c = COPY * i; c < COPY * i + COPY; ++c)
+                            if (c < COPIES) copy(c, s + DEPTH, ahead, std::false_type{});
+                    }
+                    products(kk, i);
+                }
+            }
+            if (decltype(copies)::value) turn(ahead);
+        };
+#pragma unroll
+        for (int r = 0; r < NT + MT; ++r) read(here, 0, r);
+        int s = first;
+        for (const int to = min(end, whole) - DEPTH; s < to; ++s) step(s, std::true_type{});
+        for (; s < end - 1; ++s) step(s, std::false_type{});
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+            for (int i = 0; i < MT; ++i) {
+                if (kk < 3) {
+#pragma unroll
+                    for (int r = ROW * i; r < ROW * i + ROW; ++r) read(here, kk + 1, r);
+                }
+                products(kk, i);
+            }
+    } else {
+        for (int s = first; s < end; ++s) {
+#pragma unroll
+            for (int kk = 0; kk < 2; ++kk) {
+                u32x4 a[NT][3];
+#pragma unroll
+                for (int j = 0; j < NT; ++j) planes(rows_n(here, j, kk, 0), rows_n(here, j, kk, 1), a[j]);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) {
+                    u32x4 b[3];
+                    planes(rows_m(here, i, kk, 0), rows_m(here, i, kk, 1), b);
+                    constexpr int PA[6] = {2, 0, 1, 1, 0, 0}, PB[6] = {0, 2, 1, 0, 1, 0};     // small products first
+#pragma unroll
+                    for (int q = 0; q < 6; ++q)
+#pragma unroll
+                        for (int j = 0; j < NT; ++j) acc[i][j] = mma_32(a[j][PA[q]], b[PB[q]], acc[i][j]);
+                }
+            }
+            if (s + 1 < end) {
+                arrived(s + 1);
+                turn(here);
+                stage(s + DEPTH);
+            }
+        }
+    }
+
+    // Results.  Lane 32 h + i: row 32 t + i, columns 16 h .. 16 h + 15 of a tile.
+    constexpr int STEP = FWD ? 2 : 1, ROWS = FWD ? NT : 1;
+    Vec8<E> dh[MT][ROWS]{};
+    if constexpr (KIND == kGatedD)
+        if (p.splits == 1)
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = mma_granule((E *)nullptr, a[j], b[i], acc[i][j]);
-        }
-    }
-
-    // Results.  Lane (li, lg): row 16 i + li, columns 8 lg .. 8 lg + 7 of a pair of tiles.
+                for (int j = 0; j < NT; ++j) {
+                    const int m = min(m0 + wm * (BM / WM) + 32 * i + li, p.M - 1);
+                    dh[i][j] = gated_dh(p, m, n0 + (wn * (BN / WN) + 32 * (j & ~1)) / 2 + 16 * lh + 8 * (j & 1));
+                }
 #pragma unroll
     for (int i = 0; i < MT; ++i) {
-        const int m = m0 + wm * (BM / WM) + 16 * i + li;
-        if constexpr (FWD) {
-            if (m >= p.M) continue;
+        const int m = m0 + wm * (BM / WM) + 32 * i + li;
+        if (m >= p.rows) continue;
+        float *part = p.part + ((size_t)split * p.rows + m) * p.pitch;
 #pragma unroll
-            for (int j = 0; j < NT; j += 4) {
-                const int n = n0 + (wn * (BN / WN) + 16 * j) / 2 + 8 * lg;
-                float g[8], u[8];
+        for (int j = 0; j < NT; j += STEP)
 #pragma unroll
-                for (int q = 0; q < 8; ++q) g[q] = acc[i][j + (q >> 2)][q & 3], u[q] = acc[i][j + 2 + (q >> 2)][q & 3];
-                if constexpr (KIND == kGatedFwd) {
-                    act_all<8>(g, p.act);
+            for (int e = 0; e < 16; e += 8) {
+                const int n = n0 + (wn * (BN / WN) + 32 * j) / (FWD ? 2 : 1) + 16 * lh + e;
+                float v[8], u[8];
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) g[q] *= u[q];
-                    store_row(p.h + (size_t)m * p.F, n, p.F, g);
-                } else {
-                    float dh[8];
-                    Vec8<E> v;
-                    const E *row = p.dh + (size_t)m * p.F;
-                    if (n >= p.Fp) continue;
-                    if (n + 8 <= p.F) v.load(row + n);
-                    else v.load_some(row + n, max(p.F - n, 0));
-                    v.values(dh);
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        float a, s;
-                        act_and_slope(g[q], p.act, a, s);
-                        const bool on = n + q < p.F;
-                        g[q] = on ? dh[q] * u[q] * s : 0.f;
-                        u[q] = on ? dh[q] * a : 0.f;
-                    }
-                    E *d = p.d + (size_t)m * 2 * p.Fp + n;
-                    Vec8<E>::store(d, g);
-                    Vec8<E>::store(d + p.Fp, u);
+                for (int q = 0; q < 8; ++q) {
+                    v[q] = acc[i][j][e + q];
+                    if constexpr (FWD) u[q] = acc[i][j + 1][e + q];
                 }
+                if (p.splits == 1) {
+                    gated_result<E, KIND>(p, m, n, v, u, dh[i][FWD ? j + e / 8 : 0]);
+                } else if (n < (FWD ? p.Fp : p.pitch)) {
+                    Vec8<float>::store(part + n, v);
+                    if constexpr (FWD) Vec8<float>::store(part + p.Fp + n, u);
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
-        } else {
-            E *row;
-            if constexpr (KIND == kGatedDx) {
-                if (m >= p.M) continue;
-                row = p.dx + (size_t)m * p.C;
-            } else {
-                const int f = m < p.Fp ? m : m - p.Fp;
-                if (f >= p.F) continue;
-                row = (m < p.Fp ? p.dwg : p.dwu) + (size_t)f * p.C;
-            }
+    }
+}
+
+// The parts of a contraction that was split, added up in a fixed order.
+template <class E, int KIND> __global__ __launch_bounds__(256) void gdn_gated_join_kernel(GatedParams<E> p) {
+    constexpr bool FWD = KIND == kGatedFwd || KIND == kGatedD;
+    const int G = (FWD ? p.Fp : p.pitch) / 8;
+    const long long unit = (long long)blockIdx.x * 256 + threadIdx.x;
+    const int m = (int)min(unit / G, (long long)p.rows), n = (int)(unit % G) * 8;
+    if (m >= p.rows) return;
+    float v[8] = {}, u[8] = {};
+    const size_t step = (size_t)p.rows * p.pitch;
+    const float *at = p.part + (size_t)m * p.pitch + n;
+#pragma unroll 4
+    for (int s = 0; s < p.splits; ++s) {
+        const f32x4 a = *(const f32x4 *)(at + s * step), b = *(const f32x4 *)(at + s * step + 4);
 #pragma unroll
-            for (int j = 0; j < NT; j += 2) {
-                const int n = n0 + wn * (BN / WN) + 16 * j + 8 * lg;
-                float v[8];
+        for (int q = 0; q < 4; ++q) v[q] += a[q], v[4 + q] += b[q];
+        if constexpr (FWD) {
+            const f32x4 c = *(const f32x4 *)(at + p.Fp + s * step), d = *(const f32x4 *)(at + p.Fp + s * step + 4);
 #pragma unroll
-                for (int q = 0; q < 8; ++q) v[q] = acc[i][j + (q >> 2)][q & 3];
-                store_row(row, n, p.C, v);
-            }
+            for (int q = 0; q < 4; ++q) u[q] += c[q], u[4 + q] += d[q];
         }
     }
+    Vec8<E> e{};
+    if constexpr (KIND == kGatedD) e = gated_dh(p, m, n);
+    gated_result<E, KIND>(p, m, n, v, u, e);
 }
 
 // Rows copied to a pitch that is a multiple of 64 elements, zeros behind them: operands whose rows do not start
