@@ -38,8 +38,8 @@ enum {
  *
  * with fp32 sums; h is rounded once.  M, C, F >= 1, C < 2^21, F < 2^20.  h overlaps nothing else.
  * `ws`: caller-owned device buffer, 256-byte aligned, of at least
- * gdn_gated_linear_workspace_bytes(..., 0) bytes.  That is 0 (and ws may be NULL) for up to 64 rows and for rows
- * of x that are whole multiples of 16 bytes, and for arguments that the call refuses.
+ * gdn_gated_linear_workspace_bytes(..., 0) bytes.  That may be 0 (and ws NULL; it is for most sizes, and for arguments that
+ * the call refuses); room is needed where rows of x are not whole multiples of 16 bytes, or few and long.
  */
 size_t gdn_gated_linear_workspace_bytes(int M, int C, int F, int is_bf16, int backward);
 

@@ -109,8 +109,8 @@ def gated_linear(x, w_gate, w_up, *, activation="silu", out=None, ws=None, strea
         h = act(x w_gate^T) o (x w_up^T)
 
     x [..., C], w_gate and w_up [F, C] (two halves of one [2 F, C] weight, say), all bf16 or all fp32;
-    activation "silu", "gelu", "gelu_tanh" or None.  Any number of rows: up to 64 (a decoding batch) take a
-    kernel that streams the weights.  Returns h [..., F] like x."""
+    activation "silu", "gelu", "gelu_tanh" or None.  Any number of rows; a decoding batch takes a kernel that
+    streams the weights.  Returns h [..., F] like x."""
     if stream is not None:
         with _on(stream, x):
             return gated_linear(x, w_gate, w_up, activation=activation, out=out, ws=ws)

@@ -27,7 +27,7 @@ bool ws_ok(const void *ws, size_t have, size_t need) { return need == 0 || (ws &
 // ---------------------------------------------------------------------------
 // Gated linear map.
 
-constexpr int kSkinnyRows = 64;      // rows up to which the weights are streamed
+constexpr int kSkinnyRows = 64;      // rows up to which the weights may be streamed
 
 bool gated_shape_ok(int M, int C, int F) {
     return M >= 1 && C >= 1 && F >= 1 && C < (1 << 21) && F < (1 << 20) &&
@@ -39,6 +39,7 @@ struct GatedCut {
     int BM, BN, splits;
     int rows, pitch;             // of a part's sums
     long long tiles;
+    float us;
 };
 
 GatedCut gated_cut(int kind, int M, int C, int F, bool bf16) {
@@ -56,17 +57,20 @@ GatedCut gated_cut(int kind, int M, int C, int F, bool bf16) {
         float one, full;
     } size[] = {{256, 256, 1, bf16 ? 1.45f : 4.3f, bf16 ? 1.45f : 4.3f},
                 {128, 128, 2, bf16 ? .62f : 1.9f, bf16 ? 1.2f : 3.05f},
-                {64, 128, 2, bf16 ? .45f : 1.25f, bf16 ? .8f : 1.95f}};
-    float best = INFINITY;
+                {64, 128, 2, bf16 ? .45f : 1.25f, bf16 ? .8f : 1.95f},
+                {64, 64, 2, .36f, .6f}};
+    g.us = INFINITY;
     for (const auto &t : size) {
+        // (decoding batches in bf16: 64 rows of 2048 x 8192 19.0 us, with 64 x 128 tiles 21.1; nothing gained elsewhere)
+        if (t.BN == 64 && !(bf16 && kind == gdn::kGatedFwd && M <= kSkinnyRows)) continue;
         const long long tiles = ((long long)g.rows + t.BM - 1) / t.BM * ((cols + t.BN - 1) / t.BN);
         for (int splits = 1; splits <= 16 && splits * 4 <= stages + 3; ++splits) {
             const long long n = tiles * splits, rounds = n / (256 * t.slots), left = n % (256 * t.slots);
             if (splits > 1 && n > 256 * t.slots) break;
             float us = (rounds * t.full + (left == 0 ? 0 : left <= 256 ? t.one : t.full)) * ((stages + splits - 1) / splits + 3);
             if (splits > 1) us += 4 + 2e-6f * splits * g.rows * g.pitch;        // a launch, and the sums out and in at 4 TB/s
-            if (us < best) {
-                best = us;
+            if (us < g.us) {
+                g.us = us;
                 g.BM = t.BM;
                 g.BN = t.BN;
                 g.tiles = tiles;
@@ -77,10 +81,24 @@ GatedCut gated_cut(int kind, int M, int C, int F, bool bf16) {
     return g;
 }
 
+// Whether a decoding batch streams the weights (every workgroup of 16 hidden units reads all rows of x) or goes through
+// tiles.  Streams reach 6 TB/s (fp32 5) of what they read, x from the caches, and 39 (24) GB/s a workgroup where there are few.
+// us, streams and tiles, bf16, 2048 x 8192: 1 row 16.3, 17.3; 16 rows 20.2, 18.3; 32 23.4, 19.0; 64 32.1, 19.0 (floor 14.2);
+// 4096 x 1024: 1 row 10.4, 15.8; 32 17.0, 17.8; 64 24.4, 14.8; fp32, 2048 x 8192: 1 row 32, 42; 16 38, 43; 64 82, 47.
+bool gated_streams(int M, int C, int F, bool bf16) {
+    if (M > kSkinnyRows) return false;
+    const size_t esz = bf16 ? 2 : 4;
+    if (C * esz % 16) return true;                 // tiles would have the weights copied first
+    const float row = (2 + M / 16.f) * (float)(C * esz), groups = (F + 15) / 16, turns = (F + 4095) / 4096;
+    const float weights = 2e-6f * C * F * esz / 4.7f;
+    const float stream = std::max({weights, row * 16 * groups / (bf16 ? 6e6f : 5e6f), row * 16 * turns / (bf16 ? 39e3f : 24e3f)});
+    return 3 + stream <= 5 + std::max(weights, gated_cut(gdn::kGatedFwd, M, C, F, bf16).us);
+}
+
 // Where the parts of the workspace begin.
 struct GatedLayout {
     size_t x, wg, wu, d, part, total;
-    bool pack;
+    bool streams, pack;
     int ld, Fp;
 };
 GatedLayout gated_layout(int M, int C, int F, bool bf16, bool backward) {
@@ -88,7 +106,8 @@ GatedLayout gated_layout(int M, int C, int F, bool bf16, bool backward) {
     const size_t esz = bf16 ? 2 : 4;
     L.Fp = (F + 63) / 64 * 64;
     L.ld = C;
-    if (!backward && M <= kSkinnyRows) return L;
+    L.streams = !backward && gated_streams(M, C, F, bf16);
+    if (L.streams) return L;
     L.pack = C * esz % 16 != 0;
     if (L.pack) L.ld = (C + 63) / 64 * 64;
     size_t off = 0;
@@ -135,9 +154,13 @@ template <class E, int KIND> int run_tiles(gdn::GatedParams<E> p, hipStream_t s)
     p.tiles_m = (g.rows + g.BM - 1) / g.BM;
     p.tiles_n = (cols + wide - 1) / wide;
     const bool alone = g.tiles * g.splits <= 256;      // a CU each
-    const int st = g.BM == 256   ? launch_tiles<E, KIND, 256, 256, 2, 4, 2>(p, s)
-                   : g.BM == 128 ? (alone ? launch_tiles<E, KIND, 128, 128, 2, 2, 4>(p, s) : launch_tiles<E, KIND, 128, 128, 2, 2, 2>(p, s))
-                                 : (alone ? launch_tiles<E, KIND, 64, 128, 2, 2, 6>(p, s) : launch_tiles<E, KIND, 64, 128, 2, 2, 3>(p, s));
+    int st = GDN_ERR_UNSUPPORTED;
+    if constexpr (KIND == gdn::kGatedFwd && sizeof(E) == 2)
+        if (g.BN == 64) st = alone ? launch_tiles<E, KIND, 64, 64, 2, 1, 8>(p, s) : launch_tiles<E, KIND, 64, 64, 2, 1, 4>(p, s);
+    if (g.BN > 64)
+        st = g.BM == 256   ? launch_tiles<E, KIND, 256, 256, 2, 4, 2>(p, s)
+             : g.BM == 128 ? (alone ? launch_tiles<E, KIND, 128, 128, 2, 2, 4>(p, s) : launch_tiles<E, KIND, 128, 128, 2, 2, 2>(p, s))
+                           : (alone ? launch_tiles<E, KIND, 64, 128, 2, 2, 6>(p, s) : launch_tiles<E, KIND, 64, 128, 2, 2, 3>(p, s));
     if (st != GDN_OK || g.splits == 1) return st;
     const long long units = (long long)g.rows * ((FWD ? p.Fp : g.pitch) / 8);
     return launch(gdn::gdn_gated_join_kernel<E, KIND>, dim3((unsigned)((units + 255) / 256)), dim3(256), 0, s, p);
@@ -151,7 +174,7 @@ template <class E> int pack(const void *src, void *dst, long long rows, int C, i
 template <class E> int run_gated(gdn::GatedParams<E> p, const GatedLayout &L, unsigned char *ws, bool backward, hipStream_t s) {
     p.Fp = L.Fp;
     p.ldx = p.ldw = L.ld;
-    if (!backward && p.M <= kSkinnyRows) {
+    if (L.streams) {
         const dim3 grid((unsigned)((p.F + 15) / 16)), block(64 * gdn::kSkinnyWaves);
         if (p.M <= 16) return launch(gdn::gdn_gated_skinny_kernel<E, 1>, grid, block, 0, s, p);
         if (p.M <= 32) return launch(gdn::gdn_gated_skinny_kernel<E, 2>, grid, block, 0, s, p);
