@@ -236,10 +236,11 @@ struct ConvGrad {
 };
 ConvGrad conv_grad(int B, int T, int C, int W) {
     ConvGrad g;
-    const int G = (C + 7) / 8;
+    const int G = (C + 3) / 4;
     g.TX = 1;
     while (g.TX < G && g.TX < 64) g.TX *= 2;
-    g.strip = 16;
+    const long long turns = (long long)B * T * G / 65536;
+    g.strip = (int)std::max(4LL, std::min(16LL, turns / 4 * 4));
     g.strips = (T - 1) / g.strip + 1;
     const int TY = gdn::kConvGradThreads / g.TX;
     g.blocks = (g.strips - 1) / TY + 1;
@@ -485,9 +486,14 @@ int gdn_short_conv_backward(const void *x, int64_t x_batch, int64_t x_token, con
         return with_taps(W, p, [&](const auto &q, auto taps) {
             constexpr int N = decltype(taps)::value;
             auto grad = [&](gdn::ConvParams<E> a, int tx) {
+                const void *fn[] = {(const void *)gdn::gdn_short_conv_grad_kernel<E, N, GDN_ACT_NONE>,
+                                    (const void *)gdn::gdn_short_conv_grad_kernel<E, N, GDN_ACT_SILU>,
+                                    (const void *)gdn::gdn_short_conv_grad_kernel<E, N, GDN_ACT_GELU>,
+                                    (const void *)gdn::gdn_short_conv_grad_kernel<E, N, GDN_ACT_GELU_TANH>,
+                                    (const void *)gdn::gdn_short_conv_grad_kernel<E, N, -1>};
                 void *args[] = {&a, &tx};
-                return hipLaunchKernel((const void *)gdn::gdn_short_conv_grad_kernel<E, N>, dim3((unsigned)(g.gx * rows)),
-                                       dim3(gdn::kConvGradThreads), args, 0, (hipStream_t)stream);
+                return hipLaunchKernel(fn[C < 4 ? 4 : act], dim3((unsigned)(g.gx * rows)), dim3(gdn::kConvGradThreads), args, 0,
+                                       (hipStream_t)stream);
             };
             auto sums = [&](gdn::ConvParams<E> a, int taps_, int n) {
                 void *args[] = {&a, &taps_, &n};

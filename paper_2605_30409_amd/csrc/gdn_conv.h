@@ -147,97 +147,195 @@ template <class E, int W> __global__ __launch_bounds__(256) void gdn_short_conv_
     }
 }
 
-// The gradient.  A thread forms dz for its strip and the W - 1 tokens behind it; with the last W of them it has
-// dxe of its own tokens (the first strip: of the state too).  The sums of its strip go through LDS to
-// those of the workgroup (TY strips of one sequence) and from there to the second launch, in a fixed order.
+// 4 consecutive elements at any element alignment.
+template <class E> struct Vec4;
+template <> struct Vec4<uint16_t> {
+    typedef u32x2 loose __attribute__((aligned(2)));
+    u32x2 v;
+    __device__ __forceinline__ void load(const uint16_t *p) { v = *(const loose *)p; }
+    __device__ __forceinline__ void load_some(const uint16_t *p, int n) {
+        v = u32x2{p[0] | (n > 1 ? (uint32_t)p[1] << 16 : 0u), n > 2 ? (uint32_t)p[2] : 0u};
+    }
+    __device__ __forceinline__ void values(float *x) const {
+        const f32x4 f = Tr<uint16_t>::to_f32(v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = f[i];
+    }
+    static __device__ __forceinline__ void store(uint16_t *p, const float *x) {
+        *(loose *)p = Tr<uint16_t>::from_f32(f32x4{x[0], x[1], x[2], x[3]});
+    }
+};
+template <> struct Vec4<float> {
+    typedef f32x4 loose __attribute__((aligned(4)));
+    f32x4 v;
+    __device__ __forceinline__ void load(const float *p) { v = *(const loose *)p; }
+    __device__ __forceinline__ void load_some(const float *p, int n) { v = f32x4{p[0], n > 1 ? p[1] : 0.f, n > 2 ? p[2] : 0.f, 0.f}; }
+    __device__ __forceinline__ void values(float *x) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = v[i];
+    }
+    static __device__ __forceinline__ void store(float *p, const float *x) { *(loose *)p = f32x4{x[0], x[1], x[2], x[3]}; }
+};
+
+// The gradient.  A thread has 4 channels (8 leave registers for two waves a SIMD only) and forms dz for its strip and the
+// W - 1 tokens behind it; with the last W of them it has dxe of its own tokens (the first strip: of the state too).  A
+// row's last thread takes its last 4 channels, what another has too among them: those are written twice, with the
+// same bits, and left out of the sums.  The sums of a strip go through LDS to those of the workgroup (TY strips of one
+// sequence) and from there to the second launch, in a fixed order.  ACT: the activation, or -1: p.act, rows of fewer than
+// 4 channels.
 constexpr int kConvGradThreads = 256;
 
-template <class E, int W> __global__ __launch_bounds__(kConvGradThreads) void gdn_short_conv_grad_kernel(ConvParams<E> p, int TX) {
-    __shared__ float sm[2][kConvGradThreads][9];
-    const int G = (p.C + 7) / 8, TY = kConvGradThreads / TX;
+template <class E, int W, int ACT> __global__ __launch_bounds__(kConvGradThreads) void gdn_short_conv_grad_kernel(ConvParams<E> p, int TX) {
+    constexpr bool SHORT = ACT < 0;
+    __shared__ float sm[2][kConvGradThreads][5];
+    const int G = (p.C + 3) / 4, TY = kConvGradThreads / TX;
     const int tx = threadIdx.x % TX, ty = threadIdx.x / TX;
     const int gx = (G + TX - 1) / TX;
     const int bx = blockIdx.x % gx, by = blockIdx.x / gx;
     const int g = bx * TX + tx;
     const int blocks = (p.strips + TY - 1) / TY;               // of a sequence
     const int b = by / blocks, s = (by % blocks) * TY + ty;
-    float sw[W][8], sb[8];
+    float sw[W][4], sb[4];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < 4; ++e) {
         sb[e] = 0.f;
 #pragma unroll
         for (int i = 0; i < W; ++i) sw[i][e] = 0.f;
     }
-    const Chan ch{8 * min(g, G - 1), min(8, p.C - 8 * min(g, G - 1))};
     if (g < G && s < p.strips) {
+        const int c0 = SHORT ? 0 : min(4 * g, p.C - 4);
+        auto fetch = [&](const E *row) {
+            Vec4<E> v;
+            if constexpr (SHORT) v.load_some(row, p.C);
+            else v.load(row + c0);
+            return v;
+        };
+        auto store = [&](E *row, const float *x) {
+            if constexpr (SHORT) {
+#pragma unroll
+                for (int e = 0; e < 3; ++e)
+                    if (e < p.C) row[e] = Vec8<E>::cvt(x[e]);
+            } else {
+                Vec4<E>::store(row + c0, x);
+            }
+        };
         const int t0 = s * p.strip, t1 = min(t0 + p.strip, p.T);
-        float wt[W][8], bias[8], win[W][8], dz[W][8];
+        float wt[W][4], bias[4], win[W][4], dz[W][4];
         constexpr int AHEAD = 4;
-        Vec8<E> nx[AHEAD], nd[AHEAD];
+        Vec4<E> nx[AHEAD], nd[AHEAD];
+        const E *x = p.x + b * p.xb, *dy = p.dy + b * p.yb;
+        E *dx = p.dx + b * p.ob - (W - 1) * p.ot;
         auto ask = [&](int t) {
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) {
                 const int r = min(t + j, p.T - 1);
-                nx[j] = ch.fetch(p.x + b * p.xb + (long long)r * p.xt);
-                nd[j] = ch.fetch(p.dy + b * p.yb + (long long)r * p.yt);
+                nx[j] = fetch(x + (long long)r * p.xt);
+                nd[j] = fetch(dy + (long long)r * p.yt);
             }
         };
         ask(t0);
 #pragma unroll
         for (int i = 0; i < W; ++i)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) dz[i][e] = 0.f;
+            for (int e = 0; e < 4; ++e) dz[i][e] = 0.f;
 #pragma unroll
-        for (int i = 1; i < W; ++i) conv_row<E, W>(p, ch, b, t0 + i - 1).values(win[i]);
-        conv_weights<W>(p.w, p.bias, ch, wt, bias);
-        const int end = t1 + W - 1;
-        for (int t = t0; t < end; t += AHEAD) {
-            Vec8<E> cx[AHEAD], cd[AHEAD];
+        for (int i = 1; i < W; ++i) {
+            const int at = t0 + i - 1;
+            Vec4<E> v{};
+            if (at >= W - 1) v = fetch(x + (long long)(at - (W - 1)) * p.xt);
+            else if (p.state) v = fetch(p.state + ((size_t)b * (W - 1) + at) * p.C);
+            v.values(win[i]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int c = SHORT ? min(e, p.C - 1) : c0 + e;
+#pragma unroll
+            for (int i = 0; i < W; ++i) wt[i][e] = p.w[(size_t)c * W + i];
+            bias[e] = p.bias ? p.bias[c] : 0.f;
+        }
+        // the next token: its inputs into the window, its dz (zero behind the end) in front of the others, and dxe_tt
+        auto shift = [&] {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+#pragma unroll
+                for (int i = 0; i + 1 < W; ++i) win[i][e] = win[i + 1][e];
+#pragma unroll
+                for (int i = W - 1; i > 0; --i) dz[i][e] = dz[i - 1][e];
+            }
+        };
+        auto token = [&](const Vec4<E> &vx, const Vec4<E> &vd) {
+            float z[4], d[4];
+            vx.values(win[W - 1]);
+            vd.values(d);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                z[e] = bias[e];
+#pragma unroll
+                for (int i = 0; i < W; ++i) z[e] += wt[i][e] * win[i][e];
+            }
+            slope_all<4>(z, SHORT ? p.act : ACT);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) dz[0][e] = d[e] * z[e];
+        };
+        auto result = [&](float *o) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                o[e] = 0.f;
+#pragma unroll
+                for (int i = 0; i < W; ++i) o[e] += wt[i][e] * dz[i][e];
+            }
+        };
+        auto sums = [&] {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                sb[e] += dz[0][e];
+#pragma unroll
+                for (int i = 0; i < W; ++i) sw[i][e] += dz[0][e] * win[i][e];
+            }
+        };
+        // the strip's whole runs of AHEAD tokens; of the first run, some results belong elsewhere
+        int t = t0;
+        for (; t + AHEAD <= t1; t += AHEAD) {
+            Vec4<E> cx[AHEAD], cd[AHEAD];
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) cx[j] = nx[j], cd[j] = nd[j];
-            if (t + AHEAD < end) ask(t + AHEAD);
+            ask(t + AHEAD);
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) {
-                const int tt = t + j;
-                if (tt >= end) break;
-                float d[8], z[8], o[8];
+                float o[4];
+                shift();
+                token(cx[j], cd[j]);
+                sums();
+                result(o);
+                if (j >= W - 1 || t > t0) store(dx + (long long)(t + j) * p.ot, o);
+                else if (s == 0 && p.dstate) store(p.dstate + ((size_t)b * (W - 1) + t + j) * p.C, o);
+            }
+        }
+        // what is left of it, and the tokens behind it
+        const int end = t1 + W - 1;
+        for (; t < end; ++t) {
+            float o[4];
+            shift();
+            token(nx[0], nd[0]);
+            const bool in = t < p.T;
 #pragma unroll
-                for (int i = 0; i + 1 < W; ++i)
+            for (int e = 0; e < 4; ++e) dz[0][e] = in ? dz[0][e] : 0.f;
+            if (t < t1) sums();
+            result(o);
+            if (!in && p.dstate_out) {
+                float d[4];
+                fetch(p.dstate_out + ((size_t)b * (W - 1) + t - p.T) * p.C).values(d);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) win[i][e] = win[i + 1][e];
+                for (int e = 0; e < 4; ++e) o[e] += d[e];
+            }
+            if (t >= t0 + W - 1) store(dx + (long long)t * p.ot, o);
+            else if (s == 0 && p.dstate) store(p.dstate + ((size_t)b * (W - 1) + t) * p.C, o);
 #pragma unroll
-                for (int i = W - 1; i > 0; --i)
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) dz[i][e] = dz[i - 1][e];       // dz[i]: of token tt - i
-                cx[j].values(win[W - 1]);
-                cd[j].values(d);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    z[e] = bias[e];
-#pragma unroll
-                    for (int i = 0; i < W; ++i) z[e] += wt[i][e] * win[i][e];
-                }
-                slope_all<8>(z, p.act);
-                const bool in = tt < p.T, mine = tt < t1;
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    dz[0][e] = in ? d[e] * z[e] : 0.f;
-                    if (mine) {
-                        sb[e] += dz[0][e];
-#pragma unroll
-                        for (int i = 0; i < W; ++i) sw[i][e] += dz[0][e] * win[i][e];
-                    }
-                    o[e] = 0.f;
-#pragma unroll
-                    for (int i = 0; i < W; ++i) o[e] += wt[i][e] * dz[i][e];
-                }
-                if (!in && p.dstate_out) {
-                    ch.load(p.dstate_out + ((size_t)b * (W - 1) + tt - p.T) * p.C, d);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) o[e] += d[e];
-                }
-                if (tt >= t0 + W - 1) ch.store(p.dx + b * p.ob + (long long)(tt - (W - 1)) * p.ot, o);
-                else if (s == 0 && p.dstate) ch.store(p.dstate + ((size_t)b * (W - 1) + tt) * p.C, o);
+            for (int j = 0; j + 1 < AHEAD; ++j) nx[j] = nx[j + 1], nd[j] = nd[j + 1];
+            if (t + AHEAD < end) {
+                const int r = min(t + AHEAD, p.T - 1);
+                nx[AHEAD - 1] = fetch(x + (long long)r * p.xt);
+                nd[AHEAD - 1] = fetch(dy + (long long)r * p.yt);
             }
         }
     }
@@ -245,16 +343,16 @@ template <class E, int W> __global__ __launch_bounds__(kConvGradThreads) void gd
     float *part = p.part + (size_t)by * (W + 1) * p.C;
 #pragma unroll
     for (int i = 0; i <= W; ++i) {
-        float (*buf)[9] = sm[i & 1];
+        float (*buf)[5] = sm[i & 1];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) buf[threadIdx.x][e] = i < W ? sw[i < W ? i : 0][e] : sb[e];
+        for (int e = 0; e < 4; ++e) buf[threadIdx.x][e] = i < W ? sw[i < W ? i : 0][e] : sb[e];
         lds_barrier();
-        // 8 TX columns, a thread each (or several)
-        for (int c = threadIdx.x; c < 8 * TX; c += kConvGradThreads) {
-            const int col = 8 * TX * bx + c;
+        const int c = threadIdx.x, col = 4 * TX * bx + c;
+        if (c < 4 * TX && col < p.C) {
+            const int e = SHORT ? col : col - min(col / 4 * 4, p.C - 4);
             float a = 0.f;
-            for (int y = 0; y < TY; ++y) a += buf[y * TX + c / 8][c % 8];
-            if (col < p.C) part[(size_t)i * p.C + col] = a;
+            for (int y = 0; y < TY; ++y) a += buf[y * TX + c / 4][e];
+            part[(size_t)i * p.C + col] = a;
         }
     }
 }
