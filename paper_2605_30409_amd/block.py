@@ -325,11 +325,10 @@ def _dense(t):
     return True
 
 
-def _grads(tensors, name="grads"):
-    """The list, checked, and the C call's arrays of it."""
-    if isinstance(tensors, _Tensor):
-        raise TypeError(f"{name} must be a sequence of tensors, got one tensor")
-    tensors = list(tensors)
+_KINDS = {_BF16, _F32}
+
+
+def _check_grads(tensors, name):
     dev = None
     for i, t in enumerate(tensors):
         if not isinstance(t, _Tensor):
@@ -346,9 +345,27 @@ def _grads(tensors, name="grads"):
             raise ValueError(f"{name}[{i}] must fill a run of memory, got strides {list(t.stride())}")
     if dev is None:
         raise ValueError(f"{name} holds no tensor")
+
+
+def _pointers(tensors, n):
+    return (ctypes.c_void_p * n)(*[t.data_ptr() for t in tensors])
+
+
+def _grads(tensors, name="grads"):
+    """The list, checked, its device, length, and the C call's arrays of it."""
+    if isinstance(tensors, _Tensor):
+        raise TypeError(f"{name} must be a sequence of tensors, got one tensor")
+    tensors = list(tensors)
     n = len(tensors)
-    return (tensors, dev, n, (ctypes.c_void_p * n)(*[t.data_ptr() for t in tensors]),
-            (ctypes.c_int64 * n)(*[t.numel() for t in tensors]), (ctypes.c_int * n)(*[t.dtype is _BF16 for t in tensors]))
+    # (a call is as long as its checks: all of them in one expression where nothing is wrong)
+    index = tensors[0].get_device() if n and isinstance(tensors[0], _Tensor) else -1
+    if index < 0 or not all([type(t) is _Tensor and t.get_device() == index and t.is_contiguous() for t in tensors]):
+        _check_grads(tensors, name)
+    dtypes = [t.dtype for t in tensors]
+    if not _KINDS.issuperset(dtypes):
+        _check_grads(tensors, name)
+    return (tensors, tensors[0].device, n, _pointers(tensors, n), (ctypes.c_int64 * n)(*[t.numel() for t in tensors]),
+            (ctypes.c_int * n)(*[d is _BF16 for d in dtypes]), dtypes)
 
 
 def grad_workspace(grads):
@@ -366,7 +383,7 @@ def grad_norm(grads, *, out=None, ws=None, stream=None):
         grads = list(grads)
         with _on(stream, grads[0] if grads else None):
             return grad_norm(grads, out=out, ws=ws)
-    grads, dev, n, ptrs, sizes, kinds = _grads(grads)
+    grads, dev, n, ptrs, sizes, kinds, _ = _grads(grads)
     written = ()
     if out is None:
         out = torch.empty((), dtype=_F32, device=dev)
@@ -387,16 +404,23 @@ def clip_grads(grads, max_norm, *, norm=None, eps=1e-6, out=None, ws=None, strea
         grads = list(grads)
         with _on(stream, grads[0] if grads else None):
             return clip_grads(grads, max_norm, norm=norm, eps=eps, out=out, ws=ws)
-    grads, dev, n, ptrs, sizes, kinds = _grads(grads)
+    grads, dev, n, ptrs, sizes, kinds, dtypes = _grads(grads)
     if out is None:
         out, outs = grads, ptrs
     else:
-        out, odev, m, outs, osizes, _ = _grads(out, "out")
-        if odev != dev or m != n:
-            raise ValueError(f"out must hold {n} tensors on {dev}, got {m} on {odev}")
-        for i, (g, o) in enumerate(zip(grads, out)):
-            if g.shape != o.shape or g.dtype != o.dtype or (g.stride() != o.stride() and not (g.is_contiguous() and o.is_contiguous())):
-                raise ValueError(f"out[{i}] must be like grads[{i}]")
+        if isinstance(out, _Tensor):
+            raise TypeError("out must be a sequence of tensors, got one tensor")
+        out, index = list(out), dev.index
+        if len(out) != n:
+            raise ValueError(f"out must hold {n} tensors, got {len(out)}")
+        if not all([type(o) is _Tensor and o.get_device() == index and o.shape == g.shape and o.is_contiguous() and g.is_contiguous()
+                    for g, o in zip(grads, out)]) or [o.dtype for o in out] != dtypes:
+            _check_grads(out, "out")
+            for i, (g, o) in enumerate(zip(grads, out)):
+                if g.device != o.device or g.shape != o.shape or g.dtype != o.dtype or not (
+                        g.stride() == o.stride() or (g.is_contiguous() and o.is_contiguous())):
+                    raise ValueError(f"out[{i}] must be like grads[{i}]")
+        outs = _pointers(out, n)
     max_norm, eps = float(max_norm), float(eps)
     if not max_norm >= 0 or not eps >= 0:
         raise ValueError(f"max_norm and eps must not be negative, got {max_norm} and {eps}")

@@ -151,7 +151,8 @@ __global__ __launch_bounds__(kClipThreads) void gdn_grad_scale_kernel(ClipTable 
     const double want = (double)t.max_norm / ((double)norm + (double)t.eps);
     const float scale = want >= 1.0 ? 1.f : (float)want;           // (a NaN stays one)
     const long long chunks = t.count ? t.end[t.count - 1] >> 1 : 0;
-    for (long long c = blockIdx.x; c < chunks; c += t.groups) {
+    // (from the end: what was read last for the norm may still be in the caches)
+    for (long long c = chunks - 1 - blockIdx.x; c >= 0; c -= t.groups) {
         const ClipPiece p = clip_piece(t, c);
         const void *x = t.in[p.i];
         void *y = t.out[p.i];
