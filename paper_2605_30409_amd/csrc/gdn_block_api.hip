@@ -55,8 +55,8 @@ GatedCut gated_cut(int kind, int M, int C, int F, bool bf16) {
     const struct {
         int BM, BN, slots;
         float one, full;
-    } size[] = {{256, 256, 1, bf16 ? 1.45f : 4.3f, bf16 ? 1.45f : 4.3f},
-                {128, 128, 2, bf16 ? .62f : 1.9f, bf16 ? 1.2f : 3.05f},
+    } size[] = {{256, 256, 1, bf16 ? 1.35f : 4.2f, bf16 ? 1.6f : 4.6f},
+                {128, 128, 2, bf16 ? .62f : 1.65f, bf16 ? 1.2f : 3.f},
                 {64, 128, 2, bf16 ? .45f : 1.25f, bf16 ? .8f : 1.95f},
                 {64, 64, 2, .36f, .6f}};
     g.us = INFINITY;
@@ -68,7 +68,7 @@ GatedCut gated_cut(int kind, int M, int C, int F, bool bf16) {
             const long long n = tiles * splits, rounds = n / (256 * t.slots), left = n % (256 * t.slots);
             if (splits > 1 && n > 256 * t.slots) break;
             float us = (rounds * t.full + (left == 0 ? 0 : left <= 256 ? t.one : t.full)) * ((stages + splits - 1) / splits + 3);
-            if (splits > 1) us += 4 + 2e-6f * splits * g.rows * g.pitch;        // a launch, and the sums out and in at 4 TB/s
+            if (splits > 1) us += 4 + 1.5e-6f * splits * g.rows * g.pitch;        // a launch, and the sums out and in at 5 TB/s
             if (us < g.us) {
                 g.us = us;
                 g.BM = t.BM;
@@ -97,7 +97,7 @@ bool gated_streams(int M, int C, int F, bool bf16) {
 
 // Where the parts of the workspace begin.
 struct GatedLayout {
-    size_t x, wg, wu, d, part, total;
+    size_t x, d, part, total;     // x: x, Wg and Wu at whole rows' pitch
     bool streams, pack;
     int ld, Fp;
 };
@@ -117,9 +117,7 @@ GatedLayout gated_layout(int M, int C, int F, bool bf16, bool backward) {
         return at;
     };
     if (L.pack) {
-        L.x = take((size_t)M * L.ld * esz);
-        L.wg = take((size_t)F * L.ld * esz);
-        L.wu = take((size_t)F * L.ld * esz);
+        L.x = take(((size_t)M + 2 * (size_t)F) * L.ld * esz);
     }
     if (backward) L.d = take((size_t)M * 2 * L.Fp * esz);
     size_t part = 0;
@@ -166,11 +164,6 @@ template <class E, int KIND> int run_tiles(gdn::GatedParams<E> p, hipStream_t s)
     return launch(gdn::gdn_gated_join_kernel<E, KIND>, dim3((unsigned)((units + 255) / 256)), dim3(256), 0, s, p);
 }
 
-template <class E> int pack(const void *src, void *dst, long long rows, int C, int ld, hipStream_t s) {
-    const gdn::PackParams<E> p{(const E *)src, (E *)dst, rows, C, ld};
-    return launch(gdn::gdn_gated_pack_kernel<E>, dim3((unsigned)((rows * (ld / 8) + 255) / 256)), dim3(256), 0, s, p);
-}
-
 template <class E> int run_gated(gdn::GatedParams<E> p, const GatedLayout &L, unsigned char *ws, bool backward, hipStream_t s) {
     p.Fp = L.Fp;
     p.ldx = p.ldw = L.ld;
@@ -182,12 +175,12 @@ template <class E> int run_gated(gdn::GatedParams<E> p, const GatedLayout &L, un
     }
     int st = GDN_OK;
     if (L.pack) {
-        st = pack<E>(p.x, ws + L.x, p.M, p.C, L.ld, s);
-        if (st == GDN_OK) st = pack<E>(p.wg, ws + L.wg, p.F, p.C, L.ld, s);
-        if (st == GDN_OK) st = pack<E>(p.wu, ws + L.wu, p.F, p.C, L.ld, s);
+        const gdn::PackParams<E> q{{p.x, p.wg, p.wu}, (E *)(ws + L.x), p.M, p.F, p.C, L.ld};
+        const long long units = (p.M + 2LL * p.F) * (L.ld / 8);
+        st = launch(gdn::gdn_gated_pack_kernel<E>, dim3((unsigned)((units + 255) / 256)), dim3(256), 0, s, q);
         p.x = (const E *)(ws + L.x);
-        p.wg = (const E *)(ws + L.wg);
-        p.wu = (const E *)(ws + L.wu);
+        p.wg = p.x + (size_t)p.M * L.ld;
+        p.wu = p.wg + (size_t)p.F * L.ld;
     }
     if (st != GDN_OK) return st;
     p.part = (float *)(ws + L.part);

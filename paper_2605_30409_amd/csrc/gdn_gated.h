@@ -61,6 +61,9 @@ __device__ __forceinline__ void planes(u32x4 lo, u32x4 hi, u32x4 *p) {
         }
 }
 
+// The six products of planes that fp32 asks for, small ones first.
+constexpr int kPlaneN[6] = {2, 0, 1, 1, 0, 0}, kPlaneM[6] = {0, 2, 1, 0, 1, 0};
+
 enum GatedKind { kGatedFwd, kGatedD, kGatedDx, kGatedDw };
 
 // Products of a 16-byte granule of each operand: k = 8 (bf16) or 4 (fp32) a lane.
@@ -472,23 +475,18 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gdn_gated_tile_kernel(GatedPa
                 }
                 products(kk, i);
             }
-    } else {
+    } else if constexpr (MT == 1) {
         for (int s = first; s < end; ++s) {
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk) {
-                u32x4 a[NT][3];
+                u32x4 a[NT][3], b[3];
 #pragma unroll
                 for (int j = 0; j < NT; ++j) planes(rows_n(here, j, kk, 0), rows_n(here, j, kk, 1), a[j]);
+                planes(rows_m(here, 0, kk, 0), rows_m(here, 0, kk, 1), b);
 #pragma unroll
-                for (int i = 0; i < MT; ++i) {
-                    u32x4 b[3];
-                    planes(rows_m(here, i, kk, 0), rows_m(here, i, kk, 1), b);
-                    constexpr int PA[6] = {2, 0, 1, 1, 0, 0}, PB[6] = {0, 2, 1, 0, 1, 0};     // small products first
+                for (int q = 0; q < 6; ++q)
 #pragma unroll
-                    for (int q = 0; q < 6; ++q)
-#pragma unroll
-                        for (int j = 0; j < NT; ++j) acc[i][j] = mma_32(a[j][PA[q]], b[PB[q]], acc[i][j]);
-                }
+                    for (int j = 0; j < NT; ++j) acc[0][j] = mma_32(a[j][kPlaneN[q]], b[kPlaneM[q]], acc[0][j]);
             }
             if (s + 1 < end) {
                 arrived(s + 1);
@@ -496,6 +494,57 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gdn_gated_tile_kernel(GatedPa
                 stage(s + DEPTH);
             }
         }
+    } else {
+        // Regions of a row of products each, two times MT in a stage.  In one, the rows two regions on are read, those of the
+        // next are cut into planes, and the N side's of the next step of 16 in a step's last two regions, between
+        // the products: a wave's vector instructions run beside its matrix instructions only where they alternate.
+        constexpr int R = 2 * MT;
+        u32x4 a[2][NT][3], b[2][3], ra[NT][2], rb[2][2];
+        auto read_b = [&](int t) {
+            rb[t & 1][0] = rows_m(here, t % MT, t / MT, 0);
+            rb[t & 1][1] = rows_m(here, t % MT, t / MT, 1);
+        };
+        auto read_a = [&](int kk) {
+#pragma unroll
+            for (int j = 0; j < NT; ++j) ra[j][0] = rows_n(here, j, kk, 0), ra[j][1] = rows_n(here, j, kk, 1);
+        };
+        auto cut_a = [&](int kk) {
+#pragma unroll
+            for (int j = 0; j < NT; ++j) planes(ra[j][0], ra[j][1], a[kk & 1][j]);
+        };
+        auto step = [&](int s, auto more) {
+            constexpr bool MORE = decltype(more)::value;
+#pragma unroll
+            for (int t = 0; t < R; ++t) {
+                const int kk = t / MT, i = t % MT;
+                if (MORE && t == R - 2) {
+                    arrived(s + 1);
+                    turn(here);
+                    stage(s + DEPTH);
+                }
+                if (MORE || t < R - 2) read_b((t + 2) % R);
+                if (i == MT - 2 && (MORE || kk == 0)) read_a((kk + 1) & 1);
+                if (MORE || t < R - 1) planes(rb[(t + 1) & 1][0], rb[(t + 1) & 1][1], b[(t + 1) & 1]);
+                if (i == MT - 1 && (MORE || kk == 0)) cut_a(kk + 1);
+#pragma unroll
+                for (int q = 0; q < 6; ++q)
+#pragma unroll
+                    for (int j = 0; j < NT; ++j) {
+                        acc[i][j] = mma_32(a[kk & 1][j][kPlaneN[q]], b[t & 1][kPlaneM[q]], acc[i][j]);
+                        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+                        if (i == MT - 1) __builtin_amdgcn_sched_group_barrier(0x2, 11, 0);
+                        else __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);
+                    }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        };
+        read_a(0);
+        read_b(0);
+        cut_a(0);
+        planes(rb[0][0], rb[0][1], b[0]);
+        read_b(1);
+        for (int s = first; s < end - 1; ++s) step(s, std::true_type{});
+        step(end - 1, std::false_type{});
     }
 
     // Results.  Lane 32 h + i: row 32 t + i, columns 16 h .. 16 h + 15 of a tile.
@@ -563,23 +612,22 @@ template <class E, int KIND> __global__ __launch_bounds__(256) void gdn_gated_jo
     gated_result<E, KIND>(p, m, n, v, u, e);
 }
 
-// Rows copied to a pitch that is a multiple of 64 elements, zeros behind them: operands whose rows do not start
+// x, Wg and Wu copied to rows of a multiple of 64 elements, zeros behind them: operands whose rows do not start
 // at 16 bytes.
 template <class E> struct PackParams {
-    const E *src;
+    const E *src[3];
     E *dst;
-    long long rows;
-    int C, ld;
+    int M, F, C, ld;
 };
 template <class E> __global__ __launch_bounds__(256) void gdn_gated_pack_kernel(PackParams<E> p) {
     const int G = p.ld / 8;
     const long long unit = (long long)blockIdx.x * 256 + threadIdx.x, r = unit / G;
     const int c = (int)(unit % G) * 8;
-    if (r >= p.rows) return;
-    const E *row = p.src + r * p.C;
-    Vec8<E> v;
+    if (r >= p.M + 2LL * p.F) return;
+    const E *row = r < p.M ? p.src[0] + r * p.C : r < p.M + (long long)p.F ? p.src[1] + (r - p.M) * p.C : p.src[2] + (r - p.M - p.F) * p.C;
+    Vec8<E> v{};
     if (c + 8 <= p.C) v.load(row + c);
-    else v.load_some(row + min(c, p.C - 1), max(p.C - c, 0));
+    else if (c < p.C) v.load_some(row + c, p.C - c);
     float f[8];
     v.values(f);
     Vec8<E>::store(p.dst + r * p.ld + c, f);
