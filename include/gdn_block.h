@@ -36,7 +36,10 @@ enum {
  *
  *   x [M][C], w_gate, w_up [F][C], h [M][F]   E
  *
- * with fp32 sums; h is rounded once.  M, C, F >= 1, C < 2^21, F < 2^20.  h overlaps nothing else.
+ * with fp32 sums; h is rounded once.  M, C, F >= 1, C < 2^21, F < 2^20, and M F, M C and F C so that a launch holds their
+ * tiles (below 2^35).  h overlaps nothing else.  In fp32, products are formed from three bf16 parts of each operand, as
+ * exact as fp32 sums are: an infinity may give NaN where fp32 arithmetic would keep it (in its own row of h, or hidden
+ * unit), and of values below 2^-110 the last bits may be lost.
  * `ws`: caller-owned device buffer, 256-byte aligned, of at least
  * gdn_gated_linear_workspace_bytes(..., 0) bytes.  That may be 0 (and ws NULL; it is for most sizes, and for arguments that
  * the call refuses); room is needed where rows of x are not whole multiples of 16 bytes, or few and long.
@@ -85,7 +88,7 @@ int gdn_short_conv_forward(const void *x, int64_t x_batch, int64_t x_token, cons
  *   dx [B][T][C] E, dx_batch and dx_token elements apart (no two of its elements the same)
  *   dw [C][W], dbias [C] fp32 (dbias may be NULL), dstate_in [B][W-1][C] E, or NULL
  *
- * The sums over tokens are fp32, in a fixed order.  Outputs overlap nothing.  ws: as above, at least
+ * The sums over tokens are fp32, in a fixed order.  Outputs overlap nothing.  B (C / 256 + 1) (T / 128 + 1) < 2^23.  ws: as above, at least
  * gdn_short_conv_workspace_bytes(...) bytes (0 for arguments that the call refuses).
  */
 size_t gdn_short_conv_workspace_bytes(int B, int T, int C, int W);

@@ -31,7 +31,9 @@ constexpr int kSkinnyRows = 64;      // rows up to which the weights may be stre
 
 bool gated_shape_ok(int M, int C, int F) {
     return M >= 1 && C >= 1 && F >= 1 && C < (1 << 21) && F < (1 << 20) &&
-           (M / 64 + 1LL) * (F / 64 + 1LL) < (1LL << 23) && (M / 64 + 1LL) * (C / 64 + 1LL) < (1LL << 23);
+           // a launch has fewer than 2^32 threads: the small tiles have 256, the large ones, which all larger sizes take, 512
+           (M / 64 + 1LL) * (F / 64 + 1LL) < (1LL << 23) && (M / 64 + 1LL) * (C / 64 + 1LL) < (1LL << 23) &&
+           (F / 128 + 1LL) * (C / 256 + 1LL) < (1LL << 22);
 }
 
 // How one of the products is cut: tiles of BM x BN and parts of the contraction.
@@ -245,6 +247,12 @@ ConvGrad conv_grad(int B, int T, int C, int W) {
     return g;
 }
 
+// Whether the gradient's launch has room for all workgroups: 2^23 of 256 threads.
+bool conv_grad_fits(int B, int T, int C, int W) {
+    const ConvGrad g = conv_grad(B, T, C, W);
+    return g.gx * B * g.blocks < (1LL << 23);
+}
+
 // ---------------------------------------------------------------------------
 // Gradient norm and clipping.
 
@@ -422,7 +430,7 @@ int gdn_short_conv_forward(const void *x, int64_t x_batch, int64_t x_token, cons
 }
 
 size_t gdn_short_conv_workspace_bytes(int B, int T, int C, int W) {
-    if (conv_shape(B, T, C, W, 0, 0) != GDN_OK) return 0;
+    if (conv_shape(B, T, C, W, 0, 0) != GDN_OK || !conv_grad_fits(B, T, C, W)) return 0;
     return align256(conv_grad(B, T, C, W).part);
 }
 
@@ -433,6 +441,7 @@ int gdn_short_conv_backward(const void *x, int64_t x_batch, int64_t x_token, con
     if (!x || !w || !dy || !dx || !dw) return GDN_ERR_NULL;
     const int st = conv_shape(B, T, C, W, x_batch, x_token);
     if (st != GDN_OK) return st;
+    if (!conv_grad_fits(B, T, C, W)) return GDN_ERR_SHAPE;
     if ((T > 1 && dx_token < C) || (B > 1 && dx_batch < (T - 1) * dx_token + C) || dx_token < 0 || dx_batch < 0) return GDN_ERR_SHAPE;
     if (!act_ok(act)) return GDN_ERR_UNSUPPORTED;
     const size_t esz = is_bf16 ? 2 : 4;

@@ -45,6 +45,15 @@ BACK = dict(x=addr(0), w_gate=addr(1), w_up=addr(2), dh=addr(3), dx=addr(4), dw_
             ws=addr(7), ws_bytes=MB)
 
 
+@pytest.mark.parametrize("kw", [dict(M=1 << 30, F=1 << 13), dict(M=1 << 30, C=1 << 13), dict(F=(1 << 20) - 1, C=(1 << 21) - 1)])
+def test_gated_larger_than_a_launch(kw):
+    a = dict(FWD, **kw)
+    assert block._lib().gdn_gated_linear_forward(*a.values(), None) == SHAPE
+    for backward in (0, 1):
+        assert block._lib().gdn_gated_linear_workspace_bytes(a["M"], a["C"], a["F"], 1, backward) == 0
+    assert block._lib().gdn_gated_linear_backward(*dict(BACK, **kw).values(), None) == SHAPE
+
+
 @pytest.mark.parametrize("kw,want", [
     (dict(x=None), NULL), (dict(w_gate=None), NULL), (dict(w_up=None), NULL), (dict(dh=None), NULL), (dict(dx=None), NULL),
     (dict(dw_gate=None), NULL), (dict(dw_up=None), NULL), (dict(M=0), SHAPE), (dict(F=0), SHAPE), (dict(act=9), UNSUPPORTED),
@@ -111,6 +120,13 @@ STEP = dict(x=addr(0), xb=1000, xt=100, w=addr(1), bias=addr(2), state_in=addr(3
     (dict(state_out=addr(5)), ALIAS), (dict(state_out=addr(6)), ALIAS)])
 def test_conv_step_refusals(kw, want):
     assert block._lib().gdn_short_conv_step(*dict(STEP, **kw).values(), None) == want
+
+
+@pytest.mark.parametrize("kw", [dict(B=1 << 23, T=1, C=8), dict(B=1 << 20, T=1, C=2048), dict(B=1, T=1 << 29, C=8192)])
+def test_conv_gradient_larger_than_a_launch(kw):
+    kw = dict(kw, dx=1 << 60, x=1 << 50, dxt=kw["C"], dxb=kw["T"] * kw["C"])
+    assert block._lib().gdn_short_conv_backward(*dict(CGRAD, **kw).values(), None) == SHAPE
+    assert block._lib().gdn_short_conv_workspace_bytes(kw["B"], kw["T"], kw["C"], 4) == 0
 
 
 def test_conv_workspace():
