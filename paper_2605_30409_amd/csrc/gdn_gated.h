@@ -158,15 +158,19 @@ template <class E, int MT> __global__ __launch_bounds__(64 * kSkinnyWaves) void 
 // not wait for it before every read of LDS; it has no output register, and M0 holds the LDS address.  What orders it is the
 // wait and barrier in front of the reads, and the barrier behind the last reads of what it overwrites: both are
 // volatile, too, and memory accesses do not cross them.  A scalar register that a vector instruction has written may be
-// read as an address five wait states later, and the compiler does not look for that inside assembly: the move and the
-// s_nop in front of the load are six.)
+// read as an address five wait states later only, and the compiler does not look for that inside assembly: the address goes
+// through a scalar move, which waits by itself and whose result may be used at once.  One wait state stands between M0 and
+// its use.)
 __device__ __forceinline__ void copy_tile(const void *base, uint32_t off, uint32_t lds) {
     const uint64_t at = (uint64_t)base;
     const uint64_t s = (uint64_t)__builtin_amdgcn_readfirstlane((uint32_t)(at >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)at);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(off), "s"(s));
+    uint64_t own;
+    asm volatile("s_mov_b32 m0, %1\n\ts_mov_b64 %0, %3\n\tglobal_load_lds_dwordx4 %2, %0"
+                 : "=&s"(own)
+                 : "s"(__builtin_amdgcn_readfirstlane(lds)), "v"(off), "s"(s));
 }
 __device__ __forceinline__ void copy_lane(const void *src, uint32_t lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(src));
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(lds)), "v"(src));
 }
 
 __device__ const u32x4 kZeroGranule = {0u, 0u, 0u, 0u};
