@@ -128,7 +128,7 @@ int gdn_grad_norm(const void *const *tensors, const int64_t *sizes, const int *i
  * nothing is then written if the factor is 1) or overlaps no tensor and no other out.  norm_in NULL: the
  * norm is formed as above; otherwise it is that fp32 value (a norm joined over several processes, say).
  * norm, or NULL, takes the norm that was used.  A norm that is NaN makes all NaN; an infinite one zeros, and NaN of
- * infinities.  max_norm and eps >= 0 (max_norm may be infinite).
+ * infinities.  max_norm and eps >= 0; with an infinite max_norm, or a norm of 0, nothing changes.
  */
 int gdn_grad_clip(const void *const *tensors, void *const *out, const int64_t *sizes, const int *is_bf16, int count,
                   const float *norm_in, float *norm, float max_norm, float eps, void *ws, size_t ws_bytes, void *stream);

@@ -5,9 +5,11 @@
 //   dz_t = dy_t act'(z_t),   dxe_p = sum_i w_i dz_{p-i} (+ dstate_out),   dw_i = sum_t dz_t xe_{t+i},
 //   dbias = sum_t dz_t.
 //
-// Both are bound by memory.  A thread has 8 consecutive channels of a strip of consecutive tokens, so a wave
+// Both are bound by memory.  A thread has 8 (gradient: 4) consecutive channels of a strip of consecutive tokens, so a wave
 // reads a row's whole lines, every input is read once (W - 1 rows of the neighbouring strip again) and
-// the window stays in registers.
+// the window stays in registers.  10560 tokens of 2048 channels, bf16: 19.4 us (86 MB at 4.5 TB/s), gradient 33 and 4 for its
+// sums (130 MB at 3.6; the vector units are busy 53 % of the time); of 6144
+// channels 46.5 (5.6 TB/s) and 84 (4.6).  A step of one token: 4.4 us, a launch and two round trips.
 #pragma once
 
 #include "gdn_act.h"

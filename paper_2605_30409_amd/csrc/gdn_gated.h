@@ -3,19 +3,28 @@
 // and its gradient, which forms g and u again:
 //   dg = dh o u o act'(g),  du = dh o act(g),   dx = dg Wg + du Wu,   dWg = dg^T x,  dWu = du^T x.
 //
-// Three products of one tiled kernel, and a kernel of their own for few rows (bound by memory: the weights).
+// One tiled kernel for the four products, and a kernel of its own for few rows (bound by memory: the weights).
 // With d = [dg | du] in the workspace (pitch 2 Fp, Fp = F up to a multiple of 64, zeros between):
 //   kGatedFwd   N side: rows of Wg and Wu, 32 of each in turn; M side: rows of x;   contraction over C
 //   kGatedD     the same; the epilogue forms dg and du
 //   kGatedDx    N side: columns of W; M side: rows of d;       contraction over 2 Fp (W: Wg, then Wu)
 //   kGatedDw    N side: columns of x; M side: columns of d;    contraction over the rows
-// The N side is the MFMA's A operand, so a lane has consecutive columns of a result's row: a pair of tiles in P32
-// order (see gdn_device.h) gives it 8 of them.
+// The N side is the MFMA's A operand, so a lane has consecutive columns of a result's row: 16 of a tile's 32, with the tile's
+// rows in n_order.  Nothing is transposed in memory, and g and u of a hidden unit meet in one lane.
 //
 // Tiles go to LDS by asynchronous 16-byte copies, 128 bytes of the contraction a stage ("granule": 16 bytes).
 // An operand whose contraction runs along memory rows is stored as rows of 8 granules, granule g of row r at place
-// g ^ (r & 7); one whose contraction runs down the rows is stored as it is in memory and read transposed
-// (bf16: ds_read_b64_tr_b16, fp32: element by element).
+// g ^ (r / 2 & 7); one whose contraction runs down the rows is stored as it is in memory, granules permuted within a
+// row, and read transposed (bf16: ds_read_b64_tr_b16, fp32: element by element).  No read takes a bank twice.
+//
+// Measured (bf16, C = 2048, F = 8192): 10560 rows 596 us a call, 1190 TFLOP/s (a library product of the same operations 591 to
+// 603), gradient of 3520 rows 680 (d 265, dx 211 + 13, dW 199).  What bounds it is power: on random
+// data the chip runs at 1.7 to 1.9 GHz, on zeros, at 2.3, the first takes 429 us.  Of that, loads alone take 376, products
+// alone 443.  32 x 32 x 16 products in place of 16 x 16
+// x 32, which read each operand half as often, with operands read ahead across stages: 626 -> 604; four waves of 128 x 128
+// in place of eight of 128 x 64: 650; a workgroup that goes on to its next tile during the results of the last: 601
+// (zeros 415).  fp32, as six bf16 products: 205 to 250 TFLOP/s, the matrix cores busy 63 % and the vector units (cutting
+// operands into planes) 55 % of the time, at 1.8 GHz; fp32 MFMAs end at 154.
 #pragma once
 
 #include "gdn_act.h"

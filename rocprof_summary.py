@@ -33,8 +33,8 @@ def short(name):
 def stage_of(kernel):
     """The library's stage name for a kernel (token path: wy, group_transfer,
     group_scan, chunk_states; frame-wise path: summaries, reduce, scan,
-    output) or, for the operators of gdn_ops.h, the part of the call (step; prep, scans,
-    gradients; norm, norm_gradient, norm_sums)."""
+    output) or, for the operators of gdn_ops.h and gdn_block.h, the part of the call (step; prep, scans,
+    gradients; norm, norm_gradient, norm_sums; gated and its gradient's; conv's; squares, scale)."""
     k = short(kernel)
     if k.startswith(("gdn_frame_summary", "gdn_frame_rope", "gdn_frame_kfeatures")):
         return "summaries"
@@ -51,9 +51,16 @@ def stage_of(kernel):
     if k.startswith("gdn_chunkscan_kernel"):
         args = [a.strip() for a in k.split("<", 1)[1].rstrip(">").split(",")]
         return "group_transfer" if args[3] == "0" else "chunk_states"
+    if k.startswith("gdn_gated_tile_kernel"):      # the product: h; dg and du; dx; the weights' gradients
+        return ("gated", "gated_d", "gated_dx", "gated_dw")[int(k.split("<", 1)[1].split(",")[1])]
     for prefix, stage in (("gdn_step_kernel", "step"), ("gdn_back_prep_kernel", "prep"), ("gdn_back_scan_kernel", "scans"),
                           ("gdn_back_grad_kernel", "gradients"), ("gdn_block_norm_kernel", "norm"),
-                          ("gdn_block_norm_grad_kernel", "norm_gradient"), ("gdn_block_norm_reduce_kernel", "norm_sums")):
+                          ("gdn_block_norm_grad_kernel", "norm_gradient"), ("gdn_block_norm_reduce_kernel", "norm_sums"),
+                          ("gdn_gated_skinny_kernel", "gated"), ("gdn_gated_pack_kernel", "gated_copies"),
+                          ("gdn_gated_join_kernel", "gated_join"), ("gdn_short_conv_kernel", "conv"),
+                          ("gdn_short_conv_grad_kernel", "conv_gradient"), ("gdn_short_conv_reduce_kernel", "conv_sums"),
+                          ("gdn_short_conv_step_kernel", "conv_step"), ("gdn_grad_squares_kernel", "squares"),
+                          ("gdn_grad_norm_kernel", "norm_of_all"), ("gdn_grad_scale_kernel", "scale")):
         if k.startswith(prefix):
             return stage
     raise ValueError(f"no stage for kernel {k!r}")

@@ -102,6 +102,15 @@ def test_far_values(gdn):
     c = torch.ones(20, device="cuda")
     gdn.clip_grads([c], math.inf)
     assert (c == 1).all()
+    gdn.clip_grads([b], math.inf)                           # no bound, and a norm that is infinite
+    c[3] = math.inf
+    gdn.clip_grads([c], math.inf)
+    assert (c[:3] == 1).all() and c[3] == math.inf and (c[4:] == 1).all()
+    gdn.clip_grads([zero], 0.0, eps=0.0)                    # 0 / 0
+    assert (zero == 0).all()
+    c[3] = math.nan
+    gdn.clip_grads([c], math.inf)
+    assert c.isnan().all()
 
 
 def test_same_bits_every_time_and_in_graphs(gdn):
