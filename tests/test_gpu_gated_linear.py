@@ -94,6 +94,15 @@ def test_large_tiles(gdn, dtype, M, C, F):
     check_gradient(t, gdn.gated_linear_backward(*t), "silu")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,C,F", [(100, 4096, 64), (40, 4096, 128), (64, 4104, 100), (20, 3000, 70), (9000, 72, 130), (70, 2056, 40), (20000, 16, 8)])
+def test_contractions_that_are_cut(gdn, dtype, M, C, F):
+    """Few tiles and long sums: each contraction in parts that are joined, whole ones and with a tail."""
+    t = make(M, C, F, dtype, M + C)
+    check_forward(t, gdn.gated_linear(*t[:3]), "silu")
+    check_gradient(t, gdn.gated_linear_backward(*t), "silu")
+
+
 def test_halves_of_one_weight_and_leading_dimensions(gdn):
     import torch
     t = make(6, 64, 96, "bf16", 3)
