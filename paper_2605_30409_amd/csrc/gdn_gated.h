@@ -17,14 +17,14 @@
 // g ^ (r / 2 & 7); one whose contraction runs down the rows is stored as it is in memory, granules permuted within a
 // row, and read transposed (bf16: ds_read_b64_tr_b16, fp32: element by element).  No read takes a bank twice.
 //
-// Measured (bf16, C = 2048, F = 8192): 10560 rows 596 us a call, 1190 TFLOP/s (a library product of the same operations 591 to
-// 603), gradient of 3520 rows 680 (d 265, dx 211 + 13, dW 199).  What bounds it is power: on random
-// data the chip runs at 1.7 to 1.9 GHz, on zeros, at 2.3, the first takes 429 us.  Of that, loads alone take 376, products
-// alone 443.  32 x 32 x 16 products in place of 16 x 16
-// x 32, which read each operand half as often, with operands read ahead across stages: 626 -> 604; four waves of 128 x 128
-// in place of eight of 128 x 64: 650; a workgroup that goes on to its next tile during the results of the last: 601
-// (zeros 415).  fp32, as six bf16 products: 205 to 250 TFLOP/s, the matrix cores busy 63 % and the vector units (cutting
-// operands into planes) 55 % of the time, at 1.8 GHz; fp32 MFMAs end at 154.
+// Measured (bf16, C = 2048, F = 8192): 10560 rows 575 to 620 us a call, by the card that it runs on (a library product of the
+// same operations 579 to 603), 1150 to 1230 TFLOP/s; gradient of 3520 rows 650 to 690.  What bounds it is power: on
+// random data the chip runs at 1.6 to 1.9 GHz, on zeros, above 2.2, the first takes 417 us.  Same card, us at 10560 rows:
+// 32 x 32 x 16 products with operands read ahead across stages in place of 16 x 16 x 32, 626 -> 604; a stage's copies in two
+// halves, a step apart, 644 -> 622; four waves of 128 x 128 in place of eight of 128 x 64: 617 (with copies as
+// spread; 650 without); a workgroup that goes on to its next tile during the results of the last: no gain.  fp32, as six bf16
+// products: 205 to 250 TFLOP/s, the matrix cores busy 63 % and the vector units (cutting operands into planes) 55 % of
+// the time, at 1.8 GHz; fp32 MFMAs end at 154.
 #pragma once
 
 #include "gdn_act.h"
@@ -434,13 +434,21 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gdn_gated_tile_kernel(GatedPa
 #pragma unroll
     for (int i = 0; i < DEPTH - 1; ++i) stage(first + i);
     arrived(first);
-    stage(first + DEPTH - 1);
     if constexpr (sizeof(E) == 2) {
         // Operands are read a step of 16 ahead of their products, also across stages: a stage's last ones are in
         // registers when all waves meet, so its buffer is free for the stage DEPTH on, and products to
         // do are left for the time until the next stage's first operands are there.  Products, reads and
-        // copies are dealt out evenly, a row of products at a time.
-        constexpr int ROW = (NT + MT + MT - 1) / MT, COPY = (COPIES + MT - 1) / MT;
+        // copies are dealt out evenly, a row of products at a time; half of the copies follow in the next stage's first
+        // step (all at once: 616 us in place of 595 at 10560 rows).
+        constexpr int ROW = (NT + MT + MT - 1) / MT, HALF = COPIES / 2;
+        const int plain = min(end, whole);
+        // copies c0 .. c1 - 1 of a whole stage
+        auto some = [&](int s, int c0, int c1) {
+#pragma unroll
+            for (int c = c0; c < c1; ++c) copy(c, s, ahead, std::false_type{});
+        };
+        if (first + DEPTH - 1 < plain) some(first + DEPTH - 1, 0, HALF);
+        else stage(first + DEPTH - 1);
         u32x4 a[2][NT], b[2][MT];
         // the r-th operand of step kk
         auto read = [&](uint32_t at, int kk, int r) {
@@ -452,7 +460,8 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gdn_gated_tile_kernel(GatedPa
             for (int j = 0; j < NT; ++j) acc[i][j] = mma_32(a[kk & 1][j], b[kk & 1][i], acc[i][j]);
             __builtin_amdgcn_sched_barrier(0);
         };
-        // Stage s, with the copies of stage s + DEPTH, if that is a whole one, between the last products.
+        // Stage s, with the second half of the copies of stage s + DEPTH - 1 and the first of those of stage s + DEPTH, if that is
+        // a whole one, between the first and the last products.
         auto step = [&](int s, auto copies) {
 #pragma unroll
             for (int kk = 0; kk < 4; ++kk) {
@@ -465,20 +474,20 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gdn_gated_tile_kernel(GatedPa
                 for (int i = 0; i < MT; ++i) {
 #pragma unroll
                     for (int r = ROW * i; r < ROW * i + ROW; ++r) read(here, (kk + 1) & 3, r);
-                    if (kk == 3 && decltype(copies)::value) {
-#pragma unroll
-                        for (int c = COPY * i; c < COPY * i + COPY; ++c)
-                            if (c < COPIES) copy(c, s + DEPTH, ahead, std::false_type{});
+                    if (decltype(copies)::value) {
+                        if (kk == 0) some(s + DEPTH - 1, HALF + (COPIES - HALF) * i / MT, HALF + (COPIES - HALF) * (i + 1) / MT);
+                        if (kk == 0 && i == MT - 1) turn(ahead);
+                        if (kk == 3) some(s + DEPTH, HALF * i / MT, HALF * (i + 1) / MT);
                     }
                     products(kk, i);
                 }
             }
-            if (decltype(copies)::value) turn(ahead);
         };
 #pragma unroll
         for (int r = 0; r < NT + MT; ++r) read(here, 0, r);
         int s = first;
-        for (const int to = min(end, whole) - DEPTH; s < to; ++s) step(s, std::true_type{});
+        for (; s + DEPTH < plain; ++s) step(s, std::true_type{});
+        if (s + DEPTH - 1 < plain) some(s + DEPTH - 1, HALF, COPIES), turn(ahead);
         for (; s < end - 1; ++s) step(s, std::false_type{});
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk)
@@ -491,6 +500,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gdn_gated_tile_kernel(GatedPa
                 products(kk, i);
             }
     } else if constexpr (MT == 1) {
+        stage(first + DEPTH - 1);
         for (int s = first; s < end; ++s) {
 #pragma unroll
             for (int kk = 0; kk < 2; ++kk) {
@@ -553,6 +563,7 @@ __global__ __launch_bounds__(64 * WM * WN, 2) void gdn_gated_tile_kernel(GatedPa
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
+        stage(first + DEPTH - 1);
         read_a(0);
         read_b(0);
         cut_a(0);
