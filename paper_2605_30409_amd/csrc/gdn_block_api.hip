@@ -287,6 +287,15 @@ template <class F> int clip_tables(const void *const *in, void *const *out, cons
     return flush();
 }
 
+// Room for all launches' sums; a norm stands behind it.
+size_t clip_sums_bytes(int count) {
+    return align256((size_t)std::max(1, clip_launches(count)) * gdn::kClipGroups * sizeof(double));
+}
+
+// Sums up to which every workgroup of the scaling adds them up for itself (64 KB from the caches); more are added once, by
+// a launch of their own.
+constexpr int kClipOwnSums = 4 * gdn::kClipGroups;
+
 int clip_check(const void *const *in, const int64_t *sizes, const int *is_bf16, int count) {
     if (count < 0) return GDN_ERR_SHAPE;
     if (count && (!in || !sizes || !is_bf16)) return GDN_ERR_NULL;
@@ -559,7 +568,7 @@ int gdn_short_conv_step(const void *x, int64_t x_row, int64_t x_token, const flo
 
 size_t gdn_grad_workspace_bytes(int count) {
     if (count < 0) return 0;
-    return align256((size_t)std::max(1, clip_launches(count)) * gdn::kClipGroups * sizeof(double));
+    return clip_sums_bytes(count) + 256;
 }
 
 int gdn_grad_norm(const void *const *tensors, const int64_t *sizes, const int *is_bf16, int count, float *norm, void *ws,
@@ -630,6 +639,15 @@ int gdn_grad_clip(const void *const *tensors, void *const *out, const int64_t *s
     if (!norm_in) {
         st = clip_squares(tensors, sizes, is_bf16, count, (double *)ws, parts, (hipStream_t)stream);
         if (st != GDN_OK) return st;
+    }
+    if (parts > kClipOwnSums) {
+        gdn::ClipTable t{};
+        t.parts = (const double *)ws;
+        t.all_parts = parts;
+        t.norm_out = (float *)((unsigned char *)ws + clip_sums_bytes(count));
+        st = launch(gdn::gdn_grad_norm_kernel, dim3(1), dim3(gdn::kClipThreads), 0, (hipStream_t)stream, t);
+        if (st != GDN_OK) return st;
+        norm_in = t.norm_out;
     }
     auto fill = [&](gdn::ClipTable &t) {
         t.parts = norm_in ? nullptr : (const double *)ws;

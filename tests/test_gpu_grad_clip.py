@@ -54,6 +54,20 @@ def test_lists(gdn, sizes, max_norm):
         assert all(torch.equal(a, b) for a, b in zip(here, ts))
 
 
+def test_many_launches(gdn):
+    """More sums than a workgroup adds up for itself: large tensors over six launches, small ones over forty."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(4)
+    for n, size in ((700, 262145), (5000, 3)):
+        ts = [torch.randn(size, generator=g, device="cuda", dtype=torch.bfloat16 if i % 2 else torch.float32) for i in range(n)]
+        want = math.sqrt(float(torch.stack([t.double().square().sum() for t in ts]).sum()))
+        norm, out = gdn.clip_grads(ts, 1.0, out=[torch.empty_like(t) for t in ts])
+        assert abs(float(norm) - want) <= 1.01 * U * want and float(gdn.grad_norm(ts)) == float(norm)
+        for t, o in list(zip(ts, out))[:: n // 50]:
+            ref = t.double() / (want + 1e-6)
+            assert ((o.double() - ref).abs() <= (5 * U + half(t.dtype)) * ref.abs()).all()
+
+
 def test_any_element_and_order(gdn):
     """Tensors that start at any element of a flat buffer, and permuted ones."""
     import torch
