@@ -76,7 +76,8 @@ int gdn_gated_linear_backward(const void *x, const void *w_gate, const void *w_u
  *   state_in, state_out [B][W-1][C] E, or NULL: zeros before the first token; not wanted
  *   y  [B][T][C] E
  *
- * Sums are fp32.  state_out may be state_in; outputs overlap nothing else.  B, T, C >= 1, B T C / 8 < 2^33.
+ * Sums are fp32.  state_out may be state_in; outputs overlap nothing else.  B, T, C >= 1, T < 2^30, B T C / 8 < 2^33, and
+ * for T = 1 B C / 8 < 2^32 - 2^8 (a launch's threads; C counts up to a multiple of 8 in both).
  */
 int gdn_short_conv_forward(const void *x, int64_t x_batch, int64_t x_token, const float *w, const float *bias,
                            const void *state_in, void *y, void *state_out, int B, int T, int C, int W, int act,

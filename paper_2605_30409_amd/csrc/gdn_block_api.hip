@@ -224,6 +224,13 @@ int conv_strip(int B, int T, int C) {
     return (int)std::max(4LL, std::min(16LL, turns / 4 * 4));
 }
 
+// Workgroups of the forward call's launch, and whether it has room for them: 2^24 of 256 threads.
+long long conv_groups(int B, int T, int C) {
+    const long long strips = (T - 1) / conv_strip(B, T, C) + 1;
+    return (B * strips * ((C + 7) / 8) + 255) / 256;
+}
+bool conv_fits(int B, int T, int C) { return conv_groups(B, T, C) < (1LL << 24); }
+
 struct ConvGrad {
     int TX, strip, strips, blocks;
     long long gx;
@@ -400,6 +407,7 @@ int gdn_short_conv_forward(const void *x, int64_t x_batch, int64_t x_token, cons
     if (!x || !w || !y) return GDN_ERR_NULL;
     const int st = conv_shape(B, T, C, W, x_batch, x_token);
     if (st != GDN_OK) return st;
+    if (!conv_fits(B, T, C)) return GDN_ERR_SHAPE;
     if (!act_ok(act)) return GDN_ERR_UNSUPPORTED;
     const size_t esz = is_bf16 ? 2 : 4;
     if (misaligned(x, esz)) return GDN_ERR_ALIGN;
@@ -429,9 +437,8 @@ int gdn_short_conv_forward(const void *x, int64_t x_batch, int64_t x_token, cons
         p.act = act;
         p.strip = conv_strip(B, T, C);
         p.strips = (T - 1) / p.strip + 1;
-        const long long units = (long long)B * p.strips * ((C + 7) / 8);
         return with_taps(W, p, [&](const auto &q, auto taps) {
-            return launch(gdn::gdn_short_conv_kernel<E, decltype(taps)::value>, dim3((unsigned)((units + 255) / 256)), dim3(256), 0,
+            return launch(gdn::gdn_short_conv_kernel<E, decltype(taps)::value>, dim3((unsigned)conv_groups(B, T, C)), dim3(256), 0,
                           (hipStream_t)stream, q);
         });
     };

@@ -129,6 +129,14 @@ def test_conv_gradient_larger_than_a_launch(kw):
     assert block._lib().gdn_short_conv_workspace_bytes(kw["B"], kw["T"], kw["C"], 4) == 0
 
 
+def test_conv_larger_than_a_launch():
+    """One token a sequence: a thread for 8 channels of each, so 512 threads a sequence here, and fewer than 2^32 in all.  (What is not
+    refused for that is for its address.)"""
+    args = dict(CONV, x=(1 << 50) + 1, xb=0, xt=0, y=1 << 60, state_in=None, state_out=None, T=1, C=4096)
+    for B, want in (((1 << 23) - 1, ALIGN), (1 << 23, SHAPE), ((1 << 24) - 1, SHAPE)):
+        assert block._lib().gdn_short_conv_forward(*dict(args, B=B).values(), None) == want
+
+
 def test_conv_workspace():
     f = block._lib().gdn_short_conv_workspace_bytes
     assert f(0, 1, 1, 4) == 0 and f(1, 1, 1, 5) == 0 and f(1, 1, 1, 1) == 0 and f(1 << 30, 1 << 20, 8, 4) == 0
