@@ -89,8 +89,8 @@ int gdn_short_conv_forward(const void *x, int64_t x_batch, int64_t x_token, cons
  *   dx [B][T][C] E, dx_batch and dx_token elements apart (no two of its elements the same)
  *   dw [C][W], dbias [C] fp32 (dbias may be NULL), dstate_in [B][W-1][C] E, or NULL
  *
- * The sums over tokens are fp32, in a fixed order.  Outputs overlap nothing.  B (C / 256 + 1) (T / 128 + 1) < 2^23.  ws: as above, at least
- * gdn_short_conv_workspace_bytes(...) bytes (0 for arguments that the call refuses).
+ * The sums over tokens are fp32, in a fixed order.  Outputs overlap nothing.  B (C / 256 + 1) (T / 128 + 1) < 2^23,
+ * (W + 1) C / 64 < 2^22.  ws: as above, at least gdn_short_conv_workspace_bytes(...) bytes (0 for arguments that the call refuses).
  */
 size_t gdn_short_conv_workspace_bytes(int B, int T, int C, int W);
 

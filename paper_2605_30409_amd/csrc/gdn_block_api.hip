@@ -254,10 +254,13 @@ ConvGrad conv_grad(int B, int T, int C, int W) {
     return g;
 }
 
-// Whether the gradient's launch has room for all workgroups: 2^23 of 256 threads.
+// Workgroups of the second launch, 64 sums each.
+long long conv_sums_groups(int C, int W) { return ((W + 1LL) * C + 63) / 64; }
+
+// Whether both of the gradient's launches have room for their workgroups: 2^23 of 256 threads, 2^22 of 1024.
 bool conv_grad_fits(int B, int T, int C, int W) {
     const ConvGrad g = conv_grad(B, T, C, W);
-    return g.gx * B * g.blocks < (1LL << 23);
+    return g.gx * B * g.blocks < (1LL << 23) && conv_sums_groups(C, W) < (1LL << 22);
 }
 
 // ---------------------------------------------------------------------------
@@ -518,7 +521,7 @@ int gdn_short_conv_backward(const void *x, int64_t x_batch, int64_t x_token, con
             };
             auto sums = [&](gdn::ConvParams<E> a, int taps_, int n) {
                 void *args[] = {&a, &taps_, &n};
-                return hipLaunchKernel((const void *)gdn::gdn_short_conv_reduce_kernel<E>, dim3((unsigned)(((N + 1LL) * C + 63) / 64)),
+                return hipLaunchKernel((const void *)gdn::gdn_short_conv_reduce_kernel<E>, dim3((unsigned)conv_sums_groups(C, N)),
                                        dim3(64 * gdn::kConvReduceWaves), args, 0, (hipStream_t)stream);
             };
             if (grad(q, g.TX) != hipSuccess || sums(q, N, rows) != hipSuccess) return (int)GDN_ERR_HIP;

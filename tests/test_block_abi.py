@@ -137,6 +137,17 @@ def test_conv_larger_than_a_launch():
         assert block._lib().gdn_short_conv_forward(*dict(args, B=B).values(), None) == want
 
 
+@pytest.mark.parametrize("W,C", [(4, 53687079), (3, 67108849), (2, 89478465)])
+def test_conv_gradient_with_more_sums_than_a_launch(W, C):
+    """(W + 1) C sums, 16 threads each in workgroups of 64 sums: from 2^32 threads on nothing is enqueued."""
+    assert -(-(W + 1) * C // 64) == 1 << 22
+    args = dict(CGRAD, x=(1 << 50) + 1, dx=1 << 51, dy=1 << 52, w=1 << 53, dw=1 << 54, bias=None, dbias=None, state_in=None, dstate_out=None,
+                dstate_in=None, ws=1 << 55, ws_bytes=1 << 40, B=1, T=1, W=W)
+    for c, want in ((C - 1, ALIGN), (C, SHAPE)):
+        assert block._lib().gdn_short_conv_backward(*dict(args, C=c, dxt=c, dxb=c).values(), None) == want
+        assert (block._lib().gdn_short_conv_workspace_bytes(1, 1, c, W) == 0) == (want == SHAPE)
+
+
 def test_conv_workspace():
     f = block._lib().gdn_short_conv_workspace_bytes
     assert f(0, 1, 1, 4) == 0 and f(1, 1, 1, 5) == 0 and f(1, 1, 1, 1) == 0 and f(1 << 30, 1 << 20, 8, 4) == 0
