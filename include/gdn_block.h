@@ -37,7 +37,8 @@ enum {
  *   x [M][C], w_gate, w_up [F][C], h [M][F]   E
  *
  * with fp32 sums; h is rounded once.  M, C, F >= 1, C < 2^21, F < 2^20, and M F, M C and F C so that a launch holds their
- * tiles (below 2^35).  h overlaps nothing else.  In fp32, products are formed from three bf16 parts of each operand, as
+ * tiles (M F and M C below 2^35, F C below 2^37) and, where rows of x are no whole multiples of 16 bytes, their copies
+ * ((M + 2 F) C below 2^35).  h overlaps nothing else.  In fp32, products are formed from three bf16 parts of each operand, as
  * exact as fp32 sums are: an infinity may give NaN where fp32 arithmetic would keep it (in its own row of h, or hidden
  * unit), and of values below 2^-110 the last bits may be lost.
  * `ws`: caller-owned device buffer, 256-byte aligned, of at least

@@ -132,6 +132,10 @@ GatedLayout gated_layout(int M, int C, int F, bool bf16, bool backward) {
     return L;
 }
 
+// Workgroups of the launch that copies rows, 8 elements a thread, and whether it has room for them: 2^24 of 256 threads.
+long long gated_copy_groups(const GatedLayout &L, int M, int F) { return ((M + 2LL * F) * (L.ld / 8) + 255) / 256; }
+bool gated_fits(const GatedLayout &L, int M, int F) { return !L.pack || gated_copy_groups(L, M, F) < (1LL << 24); }
+
 template <class E, int KIND, int BM, int BN, int WM, int WN, int DEPTH> int launch_tiles(const gdn::GatedParams<E> &p, hipStream_t s) {
     constexpr size_t lds = DEPTH * (BM + BN) * 128;
     const auto fn = gdn::gdn_gated_tile_kernel<E, KIND, BM, BN, WM, WN, DEPTH>;
@@ -178,8 +182,7 @@ template <class E> int run_gated(gdn::GatedParams<E> p, const GatedLayout &L, un
     int st = GDN_OK;
     if (L.pack) {
         const gdn::PackParams<E> q{{p.x, p.wg, p.wu}, (E *)(ws + L.x), p.M, p.F, p.C, L.ld};
-        const long long units = (p.M + 2LL * p.F) * (L.ld / 8);
-        st = launch(gdn::gdn_gated_pack_kernel<E>, dim3((unsigned)((units + 255) / 256)), dim3(256), 0, s, q);
+        st = launch(gdn::gdn_gated_pack_kernel<E>, dim3((unsigned)gated_copy_groups(L, p.M, p.F)), dim3(256), 0, s, q);
         p.x = (const E *)(ws + L.x);
         p.wg = p.x + (size_t)p.M * L.ld;
         p.wu = p.wg + (size_t)p.F * L.ld;
@@ -333,17 +336,19 @@ extern "C" {
 
 size_t gdn_gated_linear_workspace_bytes(int M, int C, int F, int is_bf16, int backward) {
     if (!gated_shape_ok(M, C, F)) return 0;
-    return gated_layout(M, C, F, is_bf16 != 0, backward != 0).total;
+    const GatedLayout L = gated_layout(M, C, F, is_bf16 != 0, backward != 0);
+    return gated_fits(L, M, F) ? L.total : 0;
 }
 
 int gdn_gated_linear_forward(const void *x, const void *w_gate, const void *w_up, void *h, int M, int C, int F,
                              int act, int is_bf16, void *ws, size_t ws_bytes, void *stream) {
     if (!x || !w_gate || !w_up || !h) return GDN_ERR_NULL;
     if (!gated_shape_ok(M, C, F)) return GDN_ERR_SHAPE;
+    const GatedLayout L = gated_layout(M, C, F, is_bf16 != 0, false);
+    if (!gated_fits(L, M, F)) return GDN_ERR_SHAPE;
     if (!act_ok(act)) return GDN_ERR_UNSUPPORTED;
     for (const void *p : {x, w_gate, w_up, (const void *)h})
         if (misaligned(p)) return GDN_ERR_ALIGN;
-    const GatedLayout L = gated_layout(M, C, F, is_bf16 != 0, false);
     if (!ws_ok(ws, ws_bytes, L.total)) return GDN_ERR_WORKSPACE;
     const size_t esz = is_bf16 ? 2 : 4, wb = (size_t)F * C * esz;
     const Range rh(h, (size_t)M * F * esz), rws(L.total ? ws : nullptr, L.total);
@@ -371,10 +376,11 @@ int gdn_gated_linear_backward(const void *x, const void *w_gate, const void *w_u
                               size_t ws_bytes, void *stream) {
     if (!x || !w_gate || !w_up || !dh || !dx || !dw_gate || !dw_up) return GDN_ERR_NULL;
     if (!gated_shape_ok(M, C, F)) return GDN_ERR_SHAPE;
+    const GatedLayout L = gated_layout(M, C, F, is_bf16 != 0, true);
+    if (!gated_fits(L, M, F)) return GDN_ERR_SHAPE;
     if (!act_ok(act)) return GDN_ERR_UNSUPPORTED;
     for (const void *p : {x, w_gate, w_up, dh, (const void *)dx, (const void *)dw_gate, (const void *)dw_up})
         if (misaligned(p)) return GDN_ERR_ALIGN;
-    const GatedLayout L = gated_layout(M, C, F, is_bf16 != 0, true);
     if (!ws_ok(ws, ws_bytes, L.total)) return GDN_ERR_WORKSPACE;
     const size_t esz = is_bf16 ? 2 : 4, xb = (size_t)M * C * esz, wb = (size_t)F * C * esz;
     const Range in[] = {Range(x, xb), Range(w_gate, wb), Range(w_up, wb), Range(dh, (size_t)M * F * esz)};

@@ -54,6 +54,22 @@ def test_gated_larger_than_a_launch(kw):
     assert block._lib().gdn_gated_linear_backward(*dict(BACK, **kw).values(), None) == SHAPE
 
 
+@pytest.mark.parametrize("bf16", [0, 1])
+def test_gated_copies_larger_than_a_launch(bf16):
+    """Rows of odd length are copied first, 131080 threads each here: from 2^32 threads on the call is refused, where rows are copied."""
+    fits, size = dict(C=(1 << 20) + 1, F=16350, bf16=bf16, ws_bytes=1 << 50), block._lib().gdn_gated_linear_workspace_bytes
+    far = dict(x=(1 << 50) + 1, w_gate=1 << 51, w_up=1 << 52, ws=1 << 59)
+    fwd, back = dict(FWD, h=1 << 53, **fits, **far), dict(BACK, dh=1 << 53, dx=1 << 54, dw_gate=1 << 55, dw_up=1 << 56, **fits, **far)
+    for M, want in ((65, ALIGN), (66, SHAPE), (70, SHAPE)):
+        assert block._lib().gdn_gated_linear_forward(*dict(fwd, M=M).values(), None) == want
+        assert block._lib().gdn_gated_linear_backward(*dict(back, M=M).values(), None) == want
+        for backward in (0, 1):
+            assert (size(M, fits["C"], fits["F"], bf16, backward) == 0) == (want == SHAPE)
+    more = dict(M=64, F=16352)                     # few rows are streamed as they are, but not for the gradient
+    assert block._lib().gdn_gated_linear_forward(*dict(fwd, **more).values(), None) == ALIGN
+    assert block._lib().gdn_gated_linear_backward(*dict(back, **more).values(), None) == SHAPE
+
+
 @pytest.mark.parametrize("kw,want", [
     (dict(x=None), NULL), (dict(w_gate=None), NULL), (dict(w_up=None), NULL), (dict(dh=None), NULL), (dict(dx=None), NULL),
     (dict(dw_gate=None), NULL), (dict(dw_up=None), NULL), (dict(M=0), SHAPE), (dict(F=0), SHAPE), (dict(act=9), UNSUPPORTED),
