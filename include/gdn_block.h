@@ -87,7 +87,8 @@ int gdn_short_conv_forward(const void *x, int64_t x_batch, int64_t x_token, cons
 /*
  * Its gradient, from dy = dL/dy [B][T][C] E and dstate_out = dL/d(state_out) [B][W-1][C] E (NULL: zero):
  *
- *   dx [B][T][C] E, dx_batch and dx_token elements apart (no two of its elements the same)
+ *   dx [B][T][C] E, dx_batch and dx_token elements apart (its sequences one behind the other, or all sequences of a
+ *      token before the next token, so that no two of its elements are the same)
  *   dw [C][W], dbias [C] fp32 (dbias may be NULL), dstate_in [B][W-1][C] E, or NULL
  *
  * The sums over tokens are fp32, in a fixed order.  Outputs overlap nothing.  B (C / 256 + 1) (T / 128 + 1) < 2^23,

@@ -236,8 +236,8 @@ def short_conv_backward(x, w, bias, state, dy, dstate_out=None, *, activation="s
                         dstate=None, want_dstate=True, ws=None, stream=None):
     """Gradient of ``short_conv`` from dy = dL/dy [B, T, C] and dstate_out = dL/d(state_out) [B, W - 1, C], both like x
     (dstate_out None: zero), with the forward call's inputs (bias and state may be None there and here).  dx, if given,
-    may be a part of a packed gradient.  Returns (dx, dw [C, W] fp32, dbias [C] fp32 or None without bias, dstate
-    [B, W - 1, C] like x or None without want_dstate)."""
+    may be a part of a packed gradient, [B, T, ..] or [T, B, ..] in memory.  Returns (dx, dw [C, W] fp32, dbias [C] fp32
+    or None without bias, dstate [B, W - 1, C] like x or None without want_dstate)."""
     if stream is not None:
         with _on(stream, x):
             return short_conv_backward(x, w, bias, state, dy, dstate_out, activation=activation, dx=dx, dw=dw, dbias=dbias,

@@ -221,6 +221,14 @@ int conv_shape(int B, int T, int C, int W, long long xb, long long xt) {
 // Elements from the first to behind the last of a [B][T][C] with these strides.
 size_t span(int B, int T, int C, long long xb, long long xt) { return (size_t)((B - 1) * xb + (T - 1) * xt + C); }
 
+// Whether no two elements of such a tensor are the same: its sequences lie one behind the other, or all sequences of a
+// token before the next token.
+bool conv_apart(int B, int T, int C, long long xb, long long xt) {
+    const bool by_sequence = (T == 1 || xt >= C) && (B == 1 || xb >= (T - 1) * xt + C);
+    const bool by_token = (B == 1 || xb >= C) && (T == 1 || xt >= (B - 1) * xb + C);
+    return by_sequence || by_token;
+}
+
 // Tokens of a thread's strip: many threads first, then fewer rows read twice (10560 x 2048 bf16 19.3 us, 10560 x 6144 46.5).
 int conv_strip(int B, int T, int C) {
     const long long turns = (long long)B * T * ((C + 7) / 8) / 65536;
@@ -467,7 +475,7 @@ int gdn_short_conv_backward(const void *x, int64_t x_batch, int64_t x_token, con
     const int st = conv_shape(B, T, C, W, x_batch, x_token);
     if (st != GDN_OK) return st;
     if (!conv_grad_fits(B, T, C, W)) return GDN_ERR_SHAPE;
-    if ((T > 1 && dx_token < C) || (B > 1 && dx_batch < (T - 1) * dx_token + C) || dx_token < 0 || dx_batch < 0) return GDN_ERR_SHAPE;
+    if (dx_token < 0 || dx_batch < 0 || !conv_apart(B, T, C, dx_batch, dx_token)) return GDN_ERR_SHAPE;
     if (!act_ok(act)) return GDN_ERR_UNSUPPORTED;
     const size_t esz = is_bf16 ? 2 : 4;
     if (misaligned(x, esz) || misaligned(dx, esz)) return GDN_ERR_ALIGN;

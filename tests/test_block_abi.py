@@ -124,6 +124,19 @@ def test_conv_gradient_refusals(kw, want):
     assert block._lib().gdn_short_conv_backward(*dict(CGRAD, **kw).values(), None) == want
 
 
+@pytest.mark.parametrize("dxb,dxt,want", [(400, 40, None), (40, 80, None), (41, 81, None), (1000, 3000, None), (3000, 300, None), (39, 80, SHAPE),
+                                          (40, 79, SHAPE), (400, 39, SHAPE), (399, 40, SHAPE), (0, 80, SHAPE), (40, 0, SHAPE), (-40, 80, SHAPE)])
+def test_conv_gradient_layouts(dxb, dxt, want):
+    """dx [2][10][40] with its sequences one behind the other, or all sequences of a token before the next token: any two strides that keep
+    its elements apart.  (What is taken is refused for the workspace.)"""
+    assert block._lib().gdn_short_conv_backward(*dict(CGRAD, dxb=dxb, dxt=dxt, ws=None).values(), None) == (want or WORKSPACE)
+
+
+@pytest.mark.parametrize("B,T,dxb,dxt", [(1, 10, 0, 40), (2, 1, 40, 0), (1, 1, 0, 0)])
+def test_conv_gradient_layouts_without_another_token_or_sequence(B, T, dxb, dxt):
+    assert block._lib().gdn_short_conv_backward(*dict(CGRAD, B=B, T=T, dxb=dxb, dxt=dxt, ws=None).values(), None) == WORKSPACE
+
+
 STEP = dict(x=addr(0), xb=1000, xt=100, w=addr(1), bias=addr(2), state_in=addr(3), slots=addr(4), lengths=addr(5), y=addr(6), state_out=addr(3), N=3,
             L=2, P=4, C=40, W=4, act=1, bf16=1)
 

@@ -120,6 +120,24 @@ def test_part_of_a_packed_projection(gdn, dtype, C, at):
     assert (grads[..., :at] == 9).all() and (grads[..., at + C:] == 9).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,T,C,at", [(3, 50, 64, 64), (2, 41, 33, 1), (5, 1, 9, 3), (4, 7, 2, 2), (1, 30, 24, 0)])
+def test_part_of_a_projection_token_by_token(gdn, dtype, B, T, C, at):
+    """x and dx as parts of [T, B, 3 C + 5] buffers, all sequences of a token before the next token."""
+    import torch
+    t = make(B, T, C, 4, dtype, 4)
+    packed = torch.full((T, B, 3 * C + 5), 9, dtype=t["x"].dtype, device="cuda")
+    grads = packed.clone()
+    view, dx = (a.transpose(0, 1)[..., at:at + C] for a in (packed, grads))
+    view.copy_(t["x"])
+    y, state = gdn.short_conv(view, t["w"], t["bias"], t["state"])
+    check_forward(t, y, state, "silu")
+    got = gdn.short_conv_backward(view, t["w"], t["bias"], t["state"], t["dy"], t["dstate"], dx=dx)
+    assert got[0].data_ptr() == dx.data_ptr()
+    check_gradient(t, got, "silu")
+    assert (grads[..., :at] == 9).all() and (grads[..., at + C:] == 9).all()
+
+
 def test_sequences_of_one_input(gdn):
     """The same tokens for every sequence (stride 0), and tokens in reverse order of memory refused."""
     import torch
