@@ -34,7 +34,8 @@ enum {
  *
  *   h = act(x Wg^T) o (x Wu^T)
  *
- *   x [M][C], w_gate, w_up [F][C], h [M][F]   E
+ *   x [M][C], w_gate, w_up [F][C], h [M][F]   E; those whose rows are no whole multiples of 16 bytes, here and in
+ *      the gradient, aligned to an element only
  *
  * with fp32 sums; h is rounded once.  M, C, F >= 1, C < 2^21, F < 2^20, and M F, M C and F C so that a launch holds their
  * tiles (M F and M C below 2^35, F C below 2^37) and, where rows of x are no whole multiples of 16 bytes, their copies

@@ -27,6 +27,13 @@ bool ws_ok(const void *ws, size_t have, size_t need) { return need == 0 || (ws &
 // ---------------------------------------------------------------------------
 // Gated linear map.
 
+// What a tensor with rows of n elements is aligned to: 16 bytes, or an element where its rows are not either (those are
+// copied, streamed and written at any element).
+uintptr_t row_alignment(int n, int is_bf16) {
+    const uintptr_t esz = is_bf16 ? 2 : 4;
+    return n * esz % 16 ? esz : 16;
+}
+
 constexpr int kSkinnyRows = 64;      // rows up to which the weights may be streamed
 
 bool gated_shape_ok(int M, int C, int F) {
@@ -355,8 +362,9 @@ int gdn_gated_linear_forward(const void *x, const void *w_gate, const void *w_up
     const GatedLayout L = gated_layout(M, C, F, is_bf16 != 0, false);
     if (!gated_fits(L, M, F)) return GDN_ERR_SHAPE;
     if (!act_ok(act)) return GDN_ERR_UNSUPPORTED;
-    for (const void *p : {x, w_gate, w_up, (const void *)h})
-        if (misaligned(p)) return GDN_ERR_ALIGN;
+    for (const void *p : {x, w_gate, w_up})
+        if (misaligned(p, row_alignment(C, is_bf16))) return GDN_ERR_ALIGN;
+    if (misaligned(h, row_alignment(F, is_bf16))) return GDN_ERR_ALIGN;
     if (!ws_ok(ws, ws_bytes, L.total)) return GDN_ERR_WORKSPACE;
     const size_t esz = is_bf16 ? 2 : 4, wb = (size_t)F * C * esz;
     const Range rh(h, (size_t)M * F * esz), rws(L.total ? ws : nullptr, L.total);
@@ -387,8 +395,9 @@ int gdn_gated_linear_backward(const void *x, const void *w_gate, const void *w_u
     const GatedLayout L = gated_layout(M, C, F, is_bf16 != 0, true);
     if (!gated_fits(L, M, F)) return GDN_ERR_SHAPE;
     if (!act_ok(act)) return GDN_ERR_UNSUPPORTED;
-    for (const void *p : {x, w_gate, w_up, dh, (const void *)dx, (const void *)dw_gate, (const void *)dw_up})
-        if (misaligned(p)) return GDN_ERR_ALIGN;
+    for (const void *p : {x, w_gate, w_up, (const void *)dx, (const void *)dw_gate, (const void *)dw_up})
+        if (misaligned(p, row_alignment(C, is_bf16))) return GDN_ERR_ALIGN;
+    if (misaligned(dh, row_alignment(F, is_bf16))) return GDN_ERR_ALIGN;
     if (!ws_ok(ws, ws_bytes, L.total)) return GDN_ERR_WORKSPACE;
     const size_t esz = is_bf16 ? 2 : 4, xb = (size_t)M * C * esz, wb = (size_t)F * C * esz;
     const Range in[] = {Range(x, xb), Range(w_gate, wb), Range(w_up, wb), Range(dh, (size_t)M * F * esz)};

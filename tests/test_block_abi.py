@@ -41,6 +41,24 @@ def test_gated_refusals(kw, want):
     assert block._lib().gdn_gated_linear_forward(*dict(FWD, **kw).values(), None) == want
 
 
+@pytest.mark.parametrize("bf16", [0, 1])
+@pytest.mark.parametrize("C,F", [(71, 40), (72, 41), (71, 41)])
+def test_gated_alignment_is_that_of_the_rows(C, F, bf16):
+    """Rows that are no whole multiples of 16 bytes start anywhere, and so may the tensor: the second half of one weight, say.  (What
+    is taken is refused for h or dw_up, which are the same as another tensor, behind the check of alignment.)"""
+    esz = 2 if bf16 else 4
+    back = dict(x=addr(0), w_gate=addr(1), w_up=addr(2), dh=addr(3), dx=addr(4), dw_gate=addr(5), dw_up=addr(5), M=100, C=C, F=F, act=1, bf16=bf16,
+                ws=addr(7), ws_bytes=16 * MB)
+    fwd = dict(FWD, C=C, F=F, bf16=bf16, h=addr(0), ws_bytes=16 * MB)
+    for args, call, names in ((fwd, block._lib().gdn_gated_linear_forward, ("x", "w_gate", "w_up", "h")),
+                              (back, block._lib().gdn_gated_linear_backward, ("x", "w_gate", "w_up", "dh", "dx", "dw_gate", "dw_up"))):
+        assert call(*args.values(), None) == ALIAS
+        for name in names:
+            loose = (F if name in ("h", "dh") else C) % 2 == 1
+            for off, want in ((1, ALIGN), (esz // 2, ALIGN), (esz, ALIAS if loose else ALIGN), (8, ALIAS if loose else ALIGN)):
+                assert call(*dict(args, **{name: args[name] + off}).values(), None) == want, (name, off)
+
+
 BACK = dict(x=addr(0), w_gate=addr(1), w_up=addr(2), dh=addr(3), dx=addr(4), dw_gate=addr(5), dw_up=addr(6), M=100, C=72, F=40, act=1, bf16=1,
             ws=addr(7), ws_bytes=MB)
 

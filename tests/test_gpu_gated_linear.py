@@ -118,6 +118,27 @@ def test_halves_of_one_weight_and_leading_dimensions(gdn):
     check_gradient(t, (dx.view(6, 64), dw[:96], dw[96:]), "silu")
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,C,F", [(6, 33, 31), (100, 33, 31), (70, 7, 5), (80, 1, 3), (300, 129, 131), (90, 64, 31), (90, 31, 64)])
+def test_halves_of_one_odd_weight(gdn, dtype, M, C, F):
+    """Tensors that start at any element, as halves of a weight and rows of a buffer with odd sizes do."""
+    import torch
+    t = make(M, C, F, dtype, M + C)
+    dt = t[0].dtype
+
+    def behind_a_row(a):
+        return torch.cat([torch.full_like(a[:1], 9), a])[1:]
+    x, w, dh = behind_a_row(t[0]), torch.cat(t[1:3]), behind_a_row(t[3])
+    h = torch.full((M + 2, F), 9, dtype=dt, device="cuda")
+    gdn.gated_linear(x, w[:F], w[F:], out=h[1:-1])
+    check_forward(t, h[1:-1], "silu")
+    dx, dw = torch.full((M + 2, C), 9, dtype=dt, device="cuda"), torch.full((2 * F + 2, C), 9, dtype=dt, device="cuda")
+    got = gdn.gated_linear_backward(x, w[:F], w[F:], dh, dx=dx[1:-1], dw_gate=dw[1:F + 1], dw_up=dw[F + 1:-1])
+    check_gradient(t, got, "silu")
+    for a in (h, dx, dw):
+        assert (a[0] == 9).all() and (a[-1] == 9).all()
+
+
 @pytest.mark.parametrize("name", ACTS[1:])
 def test_gradient_against_differences(gdn, name):
     import torch
