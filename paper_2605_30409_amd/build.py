@@ -10,7 +10,7 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libgdn.so")
 SOURCES = [os.path.join(CSRC, f) for f in ("gdn_api.hip", "gdn_ops_api.hip", "gdn_block_api.hip")]
 HEADERS = [os.path.join(CSRC, f) for f in ("gdn_act.h", "gdn_backward.h", "gdn_clip.h", "gdn_conv.h",
-                                           "gdn_device.h", "gdn_frame.h", "gdn_gated.h", "gdn_host.h",
+                                           "gdn_device.h", "gdn_frame.h", "gdn_gated.h", "gdn_gated_rule.h", "gdn_host.h",
                                            "gdn_kernels.h", "gdn_norm.h", "gdn_step.h")] + \
           [os.path.join(INCLUDE, f) for f in ("gdn.h", "gdn_block.h", "gdn_ops.h")]
 

@@ -16,6 +16,7 @@
 #include "gdn_clip.h"
 #include "gdn_conv.h"
 #include "gdn_gated.h"
+#include "gdn_gated_rule.h"
 #include "gdn_host.h"
 
 namespace {
@@ -34,76 +35,6 @@ uintptr_t row_alignment(int n, int is_bf16) {
     return n * esz % 16 ? esz : 16;
 }
 
-constexpr int kSkinnyRows = 64;      // rows up to which the weights may be streamed
-
-bool gated_shape_ok(int M, int C, int F) {
-    return M >= 1 && C >= 1 && F >= 1 && C < (1 << 21) && F < (1 << 20) &&
-           // a launch has fewer than 2^32 threads: the small tiles have 256, the large ones, which all larger sizes take, 512
-           (M / 64 + 1LL) * (F / 64 + 1LL) < (1LL << 23) && (M / 64 + 1LL) * (C / 64 + 1LL) < (1LL << 23) &&
-           (F / 128 + 1LL) * (C / 256 + 1LL) < (1LL << 22);
-}
-
-// How one of the products is cut: tiles of BM x BN and parts of the contraction.
-struct GatedCut {
-    int BM, BN, splits;
-    int rows, pitch;             // of a part's sums
-    long long tiles;
-    float us;
-};
-
-GatedCut gated_cut(int kind, int M, int C, int F, bool bf16) {
-    const bool fwd = kind == gdn::kGatedFwd || kind == gdn::kGatedD;
-    const int Fp = (F + 63) / 64 * 64, KB = bf16 ? 64 : 32;
-    const long long cols = fwd ? 2LL * F : C;
-    GatedCut g;
-    g.rows = kind == gdn::kGatedDw ? 2 * Fp : M;
-    g.pitch = fwd ? 2 * Fp : (C + 7) / 8 * 8;
-    const int stages = fwd ? (C - 1) / KB + 1 : kind == gdn::kGatedDx ? 2 * ((F - 1) / KB + 1) : (M - 1) / KB + 1;
-    // The cheapest by what stages were measured to take, us: of a tile that has its CU to itself, and of the one or two that a
-    // CU holds on a full chip.
-    const struct {
-        int BM, BN, slots;
-        float one, full;
-    } size[] = {{256, 256, 1, bf16 ? 1.35f : 4.2f, bf16 ? 1.6f : 4.6f},
-                {128, 128, 2, bf16 ? .62f : 1.65f, bf16 ? 1.2f : 3.f},
-                {64, 128, 2, bf16 ? .45f : 1.25f, bf16 ? .8f : 1.95f},
-                {64, 64, 2, .36f, .6f}};
-    g.us = INFINITY;
-    for (const auto &t : size) {
-        // (decoding batches in bf16: 64 rows of 2048 x 8192 19.0 us, with 64 x 128 tiles 21.1; nothing gained elsewhere)
-        if (t.BN == 64 && !(bf16 && kind == gdn::kGatedFwd && M <= kSkinnyRows)) continue;
-        const long long tiles = ((long long)g.rows + t.BM - 1) / t.BM * ((cols + t.BN - 1) / t.BN);
-        for (int splits = 1; splits <= 16 && splits * 4 <= stages + 3; ++splits) {
-            const long long n = tiles * splits, rounds = n / (256 * t.slots), left = n % (256 * t.slots);
-            if (splits > 1 && n > 256 * t.slots) break;
-            float us = (rounds * t.full + (left == 0 ? 0 : left <= 256 ? t.one : t.full)) * ((stages + splits - 1) / splits + 3);
-            if (splits > 1) us += 4 + 1.5e-6f * splits * g.rows * g.pitch;        // a launch, and the sums out and in at 5 TB/s
-            if (us < g.us) {
-                g.us = us;
-                g.BM = t.BM;
-                g.BN = t.BN;
-                g.tiles = tiles;
-                g.splits = splits;
-            }
-        }
-    }
-    return g;
-}
-
-// Whether a decoding batch streams the weights (every workgroup of 16 hidden units reads all rows of x) or goes through
-// tiles.  Streams reach 6 TB/s (fp32 5) of what they read, x from the caches, and 39 (24) GB/s a workgroup where there are few.
-// us, streams and tiles, bf16, 2048 x 8192: 1 row 16.3, 17.3; 16 rows 20.2, 18.3; 32 23.4, 19.0; 64 32.1, 19.0 (floor 14.2);
-// 4096 x 1024: 1 row 10.4, 15.8; 32 17.0, 17.8; 64 24.4, 14.8; fp32, 2048 x 8192: 1 row 32, 42; 16 38, 43; 64 82, 47.
-bool gated_streams(int M, int C, int F, bool bf16) {
-    if (M > kSkinnyRows) return false;
-    const size_t esz = bf16 ? 2 : 4;
-    if (C * esz % 16) return true;                 // tiles would have the weights copied first
-    const float row = (2 + M / 16.f) * (float)(C * esz), groups = (F + 15) / 16, turns = (F + 4095) / 4096;
-    const float weights = 2e-6f * C * F * esz / 4.7f;
-    const float stream = std::max({weights, row * 16 * groups / (bf16 ? 6e6f : 5e6f), row * 16 * turns / (bf16 ? 39e3f : 24e3f)});
-    return 3 + stream <= 5 + std::max(weights, gated_cut(gdn::kGatedFwd, M, C, F, bf16).us);
-}
-
 // Where the parts of the workspace begin.
 struct GatedLayout {
     size_t x, d, part, total;     // x: x, Wg and Wu at whole rows' pitch
@@ -115,7 +46,7 @@ GatedLayout gated_layout(int M, int C, int F, bool bf16, bool backward) {
     const size_t esz = bf16 ? 2 : 4;
     L.Fp = (F + 63) / 64 * 64;
     L.ld = C;
-    L.streams = !backward && gated_streams(M, C, F, bf16);
+    L.streams = !backward && gdn::gated_streams(M, C, F, bf16);
     if (L.streams) return L;
     L.pack = C * esz % 16 != 0;
     if (L.pack) L.ld = (C + 63) / 64 * 64;
@@ -131,7 +62,7 @@ GatedLayout gated_layout(int M, int C, int F, bool bf16, bool backward) {
     if (backward) L.d = take((size_t)M * 2 * L.Fp * esz);
     size_t part = 0;
     for (int kind = backward ? gdn::kGatedD : gdn::kGatedFwd; kind <= (backward ? gdn::kGatedDw : gdn::kGatedFwd); ++kind) {
-        const GatedCut g = gated_cut(kind, M, C, F, bf16);
+        const gdn::GatedCut g = gdn::gated_cut(kind, M, C, F, bf16);
         if (g.splits > 1) part = std::max(part, (size_t)g.splits * g.rows * g.pitch * 4);
     }
     L.part = take(part);
@@ -157,21 +88,20 @@ template <class E, int KIND, int BM, int BN, int WM, int WN, int DEPTH> int laun
 
 template <class E, int KIND> int run_tiles(gdn::GatedParams<E> p, hipStream_t s) {
     constexpr bool FWD = KIND == gdn::kGatedFwd || KIND == gdn::kGatedD;
-    const GatedCut g = gated_cut(KIND, p.M, p.C, p.F, sizeof(E) == 2);
+    const gdn::GatedCut g = gdn::gated_cut(KIND, p.M, p.C, p.F, sizeof(E) == 2);
     const int cols = FWD ? p.F : p.C, wide = FWD ? g.BN / 2 : g.BN;
     p.rows = g.rows;
     p.pitch = g.pitch;
     p.splits = g.splits;
     p.tiles_m = (g.rows + g.BM - 1) / g.BM;
     p.tiles_n = (cols + wide - 1) / wide;
-    const bool alone = g.tiles * g.splits <= 256;      // a CU each
     int st = GDN_ERR_UNSUPPORTED;
     if constexpr (KIND == gdn::kGatedFwd && sizeof(E) == 2)
-        if (g.BN == 64) st = alone ? launch_tiles<E, KIND, 64, 64, 2, 1, 8>(p, s) : launch_tiles<E, KIND, 64, 64, 2, 1, 4>(p, s);
+        if (g.BN == 64) st = g.depth == 8 ? launch_tiles<E, KIND, 64, 64, 2, 1, 8>(p, s) : launch_tiles<E, KIND, 64, 64, 2, 1, 4>(p, s);
     if (g.BN > 64)
         st = g.BM == 256   ? launch_tiles<E, KIND, 256, 256, 2, 4, 2>(p, s)
-             : g.BM == 128 ? (alone ? launch_tiles<E, KIND, 128, 128, 2, 2, 4>(p, s) : launch_tiles<E, KIND, 128, 128, 2, 2, 2>(p, s))
-                           : (alone ? launch_tiles<E, KIND, 64, 128, 2, 2, 6>(p, s) : launch_tiles<E, KIND, 64, 128, 2, 2, 3>(p, s));
+             : g.BM == 128 ? (g.depth == 4 ? launch_tiles<E, KIND, 128, 128, 2, 2, 4>(p, s) : launch_tiles<E, KIND, 128, 128, 2, 2, 2>(p, s))
+                           : (g.depth == 6 ? launch_tiles<E, KIND, 64, 128, 2, 2, 6>(p, s) : launch_tiles<E, KIND, 64, 128, 2, 2, 3>(p, s));
     if (st != GDN_OK || g.splits == 1) return st;
     const long long units = (long long)g.rows * ((FWD ? p.Fp : g.pitch) / 8);
     return launch(gdn::gdn_gated_join_kernel<E, KIND>, dim3((unsigned)((units + 255) / 256)), dim3(256), 0, s, p);
@@ -350,7 +280,7 @@ int clip_squares(const void *const *in, const int64_t *sizes, const int *is_bf16
 extern "C" {
 
 size_t gdn_gated_linear_workspace_bytes(int M, int C, int F, int is_bf16, int backward) {
-    if (!gated_shape_ok(M, C, F)) return 0;
+    if (!gdn::gated_shape_ok(M, C, F)) return 0;
     const GatedLayout L = gated_layout(M, C, F, is_bf16 != 0, backward != 0);
     return gated_fits(L, M, F) ? L.total : 0;
 }
@@ -358,7 +288,7 @@ size_t gdn_gated_linear_workspace_bytes(int M, int C, int F, int is_bf16, int ba
 int gdn_gated_linear_forward(const void *x, const void *w_gate, const void *w_up, void *h, int M, int C, int F,
                              int act, int is_bf16, void *ws, size_t ws_bytes, void *stream) {
     if (!x || !w_gate || !w_up || !h) return GDN_ERR_NULL;
-    if (!gated_shape_ok(M, C, F)) return GDN_ERR_SHAPE;
+    if (!gdn::gated_shape_ok(M, C, F)) return GDN_ERR_SHAPE;
     const GatedLayout L = gated_layout(M, C, F, is_bf16 != 0, false);
     if (!gated_fits(L, M, F)) return GDN_ERR_SHAPE;
     if (!act_ok(act)) return GDN_ERR_UNSUPPORTED;
@@ -391,7 +321,7 @@ int gdn_gated_linear_backward(const void *x, const void *w_gate, const void *w_u
                               void *dw_gate, void *dw_up, int M, int C, int F, int act, int is_bf16, void *ws,
                               size_t ws_bytes, void *stream) {
     if (!x || !w_gate || !w_up || !dh || !dx || !dw_gate || !dw_up) return GDN_ERR_NULL;
-    if (!gated_shape_ok(M, C, F)) return GDN_ERR_SHAPE;
+    if (!gdn::gated_shape_ok(M, C, F)) return GDN_ERR_SHAPE;
     const GatedLayout L = gated_layout(M, C, F, is_bf16 != 0, true);
     if (!gated_fits(L, M, F)) return GDN_ERR_SHAPE;
     if (!act_ok(act)) return GDN_ERR_UNSUPPORTED;

@@ -28,6 +28,7 @@
 #pragma once
 
 #include "gdn_act.h"
+#include "gdn_gated_rule.h"
 #include "gdn_norm.h"
 
 namespace gdn {
@@ -72,8 +73,6 @@ __device__ __forceinline__ void planes(u32x4 lo, u32x4 hi, u32x4 *p) {
 
 // The six products of planes that fp32 asks for, small ones first.
 constexpr int kPlaneN[6] = {2, 0, 1, 1, 0, 0}, kPlaneM[6] = {0, 2, 1, 0, 1, 0};
-
-enum GatedKind { kGatedFwd, kGatedD, kGatedDx, kGatedDw };
 
 // Products of a 16-byte granule of each operand: k = 8 (bf16) or 4 (fp32) a lane.
 __device__ __forceinline__ f32x4 mma_granule(uint16_t *, u32x4 a, u32x4 b, f32x4 c) {

@@ -103,6 +103,23 @@ def test_contractions_that_are_cut(gdn, dtype, M, C, F):
     check_gradient(t, gdn.gated_linear_backward(*t), "silu")
 
 
+# Sizes that take each variant of the tiles, whole contractions and parts, for more stages than it has buffers (which
+# sizes those are, a test on the host looks after).
+VARIANTS = [(452, 475, 10), (1, 4104, 8), (1426, 248, 121), (1, 8, 193), (1, 8, 1892), (1, 8, 3785), (4075, 8, 8), (65, 8590, 11), (7634, 8, 8),
+            (3223, 168, 383), (386, 800, 774), (5587, 336, 135), (2058, 272, 1067), (261, 641, 1807), (177, 152, 8215), (514, 285, 3278),
+            (2006, 1040, 579), (964, 136, 4207), (1801, 2490, 143), (1840, 668, 1148), (454, 201, 8504), (5377, 8, 556), (274, 3788, 1955),
+            (657, 5584, 66), (1033, 3745, 136), (4978, 2336, 398), (64, 768, 4159), (9, 8272, 547), (11020, 8, 1171), (2345, 8, 5813),
+            (8418, 137, 1409), (67, 3208, 8259), (64, 2048, 8192), (39, 1656, 6441), (57, 872, 5349)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,C,F", VARIANTS)
+def test_variants(gdn, dtype, M, C, F):
+    t = make(M, C, F, dtype, M + C)
+    check_forward(t, gdn.gated_linear(*t[:3]), "silu")
+    check_gradient(t, gdn.gated_linear_backward(*t), "silu")
+
+
 def test_halves_of_one_weight_and_leading_dimensions(gdn):
     import torch
     t = make(6, 64, 96, "bf16", 3)
