@@ -97,11 +97,12 @@ template <class E, int KIND> int run_tiles(gdn::GatedParams<E> p, hipStream_t s)
     p.tiles_n = (cols + wide - 1) / wide;
     int st = GDN_ERR_UNSUPPORTED;
     if constexpr (KIND == gdn::kGatedFwd && sizeof(E) == 2)
-        if (g.BN == 64) st = g.depth == 8 ? launch_tiles<E, KIND, 64, 64, 2, 1, 8>(p, s) : launch_tiles<E, KIND, 64, 64, 2, 1, 4>(p, s);
-    if (g.BN > 64)
-        st = g.BM == 256   ? launch_tiles<E, KIND, 256, 256, 2, 4, 2>(p, s)
-             : g.BM == 128 ? (g.depth == 4 ? launch_tiles<E, KIND, 128, 128, 2, 2, 4>(p, s) : launch_tiles<E, KIND, 128, 128, 2, 2, 2>(p, s))
-                           : (g.depth == 6 ? launch_tiles<E, KIND, 64, 128, 2, 2, 6>(p, s) : launch_tiles<E, KIND, 64, 128, 2, 2, 3>(p, s));
+        if (g.BN == 64) st = launch_tiles<E, KIND, 64, 64, 2, 1, 8>(p, s);
+    if constexpr (KIND != gdn::kGatedDw)
+        if (g.BM == 64 && g.depth == 3) st = launch_tiles<E, KIND, 64, 128, 2, 2, 3>(p, s);
+    if (g.BM == 64 && g.depth == 6) st = launch_tiles<E, KIND, 64, 128, 2, 2, 6>(p, s);
+    if (g.BM == 128) st = g.depth == 4 ? launch_tiles<E, KIND, 128, 128, 2, 2, 4>(p, s) : launch_tiles<E, KIND, 128, 128, 2, 2, 2>(p, s);
+    if (g.BM == 256) st = launch_tiles<E, KIND, 256, 256, 2, 4, 2>(p, s);
     if (st != GDN_OK || g.splits == 1) return st;
     const long long units = (long long)g.rows * ((FWD ? p.Fp : g.pitch) / 8);
     return launch(gdn::gdn_gated_join_kernel<E, KIND>, dim3((unsigned)((units + 255) / 256)), dim3(256), 0, s, p);

@@ -64,8 +64,10 @@ inline GatedCut gated_cut(int kind, int M, int C, int F, bool bf16) {
             }
         }
     }
+    // (more than 256 tiles of 64 x 64 are never the cheapest, nor of 64 x 128 for the weights' gradients, whose 2 Fp rows
+    // half as many of 128 x 128 cover)
     const bool alone = g.tiles * g.splits <= 256;      // a CU each, and its LDS
-    g.depth = g.BM == 256 ? 2 : g.BM == 128 ? (alone ? 4 : 2) : g.BN == 128 ? (alone ? 6 : 3) : alone ? 8 : 4;
+    g.depth = g.BM == 256 ? 2 : g.BM == 128 ? (alone ? 4 : 2) : g.BN == 64 ? 8 : alone || kind == kGatedDw ? 6 : 3;
     return g;
 }
 

@@ -56,3 +56,14 @@ def test_decoding_batches_through_tiles(variants):
     for s in ((64, 2048, 8192), (39, 1656, 6441), (57, 872, 5349), (64, 768, 4159)):
         assert variants(*s, 1)[(FWD, 1, 64, 64, 8, False)] > 9
     assert variants(9, 8272, 547, 1)[(FWD, 1, 64, 64, 8, True)] > 9
+
+
+def test_nothing_is_built_that_no_size_takes(variants):
+    """The tiled kernels by their names in the built library: those that the sizes above take."""
+    import re
+
+    import paper_2605_30409_amd as gdn
+    with open(gdn.LIB_PATH, "rb") as f:
+        names = set(re.findall(rb"gdn_gated_tile_kernelI([tf])Li(\d)ELi(\d+)ELi(\d+)ELi\dELi\dELi(\d)EEE", f.read()))
+    built = {(int(kind), int(e == b"t"), int(bm), int(bn), int(depth)) for e, kind, bm, bn, depth in names}
+    assert built == {v[:5] for v in taken(variants)}
