@@ -14,8 +14,7 @@ import ctypes
 import torch
 
 from . import gdn as _gdn
-from . import ops as _ops
-from .ops import _BF16, _F32, _I32, _Tensor, _call, _dims, _element, _fit, _given, _int, _needs, _on, _ptr
+from .ops import _BF16, _F32, _I32, _Tensor, _call, _dims, _element, _fit, _given, _needs, _on, _ptr
 
 ACTIVATIONS = {None: 0, "silu": 1, "gelu": 2, "gelu_tanh": 3}
 
