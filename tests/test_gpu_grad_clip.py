@@ -68,6 +68,46 @@ def test_many_launches(gdn):
             assert ((o.double() - ref).abs() <= (5 * U + half(t.dtype)) * ref.abs()).all()
 
 
+@pytest.mark.parametrize("n", [8192, 8193, 9000])
+def test_sums_of_many_small_tensors(gdn, n):
+    """Tensors of three elements, a sum each: 8192 sums are the most that every workgroup of the scaling adds up for itself, more are read from
+    the workspace as one norm; over 64 launches and more, in place too and from replays of a graph."""
+    import torch
+    g = torch.Generator(device="cuda").manual_seed(n)
+    flat = [torch.randn(3 * n, generator=g, device="cuda").to(dt) for dt in (torch.bfloat16, torch.float32)]
+
+    def parts(pair):
+        return [pair[i % 2][3 * i:3 * i + 3] for i in range(n)]
+    used = [torch.arange(3 * n, device="cuda") // 3 % 2 == k for k in (0, 1)]
+
+    def check(norm, out):
+        want = math.sqrt(sum(float(f[u].double().square().sum()) for f, u in zip(flat, used)))
+        assert abs(float(norm) - want) <= 1.01 * U * want
+        for f, u, o in zip(flat, used, out):
+            ref = f[u].double() * min(1.0, 1.0 / (want + 1e-6))
+            assert ((o[u].double() - ref).abs() <= (5 * U + half(f.dtype)) * ref.abs()).all()
+            assert (o[~u] == 9).all()
+    outs = [[torch.full_like(f, 9) for f in flat] for _ in range(2)]
+    norm, _ = gdn.clip_grads(parts(flat), 1.0, out=parts(outs[0]))
+    check(norm, outs[0])
+    assert torch.equal(gdn.grad_norm(parts(flat)), norm)
+    here = [torch.where(u, f, 9) for f, u in zip(flat, used)]
+    n2, _ = gdn.clip_grads(parts(here), 1.0)
+    assert torch.equal(n2, norm) and all(torch.equal(a, b) for a, b in zip(here, outs[0]))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        n3, _ = gdn.clip_grads(parts(flat), 1.0, out=parts(outs[1]))
+    for i in range(3):
+        n3.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        check(n3, outs[1])
+        for f in flat:
+            f.mul_(-0.75)
+        gdn.clip_grads(parts(here), 1.0)
+        torch.cuda.synchronize()
+
+
 def test_any_element_and_order(gdn):
     """Tensors that start at any element of a flat buffer, and permuted ones."""
     import torch
