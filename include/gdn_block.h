@@ -39,9 +39,10 @@ enum {
  *
  * with fp32 sums; h is rounded once.  M, C, F >= 1, C < 2^21, F < 2^20, and M F, M C and F C so that a launch holds their
  * tiles (M F and M C below 2^35, F C below 2^37) and, where rows of x are no whole multiples of 16 bytes, their copies
- * ((M + 2 F) C below 2^35).  h overlaps nothing else.  In fp32, products are formed from three bf16 parts of each operand, as
- * exact as fp32 sums are: an infinity may give NaN where fp32 arithmetic would keep it (in its own row of h, or hidden
- * unit), and of values below 2^-110 the last bits may be lost.
+ * ((M + 2 F) C below 2^35).  h overlaps nothing else.  In fp32, products are formed from three bf16 parts of each
+ * operand, each to within 2^-21 of itself (mostly 2^-24), so that all but the shortest sums are as exact as in fp32
+ * arithmetic: an infinity may give NaN where that would keep it (in its own row of h, or hidden unit), and of values
+ * below 2^-110 the last bits may be lost.
  * `ws`: caller-owned device buffer, 256-byte aligned, of at least
  * gdn_gated_linear_workspace_bytes(..., 0) bytes.  That may be 0 (and ws NULL; it is for most sizes, and for arguments that
  * the call refuses); room is needed where rows of x are not whole multiples of 16 bytes, or few and long.
@@ -60,7 +61,7 @@ int gdn_gated_linear_forward(const void *x, const void *w_gate, const void *w_up
  * The gradients of the two projections are operands of the products behind them and are rounded to E
  * for those, as the results are.  An infinity or NaN makes NaN of what depends on it, and an infinity may also where
  * fp32 arithmetic would keep it.  Outputs overlap nothing else.
- * ws as above, of gdn_gated_linear_workspace_bytes(..., 1) bytes (2 M F of E and a little; never 0).
+ * ws as above, of gdn_gated_linear_workspace_bytes(..., 1) bytes (2 M F of E and a little; 0 for arguments that the call refuses).
  */
 int gdn_gated_linear_backward(const void *x, const void *w_gate, const void *w_up, const void *dh, void *dx,
                               void *dw_gate, void *dw_up, int M, int C, int F, int act, int is_bf16, void *ws,

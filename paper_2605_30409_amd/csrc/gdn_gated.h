@@ -24,7 +24,8 @@
 // halves, a step apart, 644 -> 622; four waves of 128 x 128 in place of eight of 128 x 64: 617 (with copies as
 // spread; 650 without); a workgroup that goes on to its next tile during the results of the last: no gain.  fp32, as six bf16
 // products: 205 to 250 TFLOP/s, the matrix cores busy 63 % and the vector units (cutting operands into planes) 55 % of
-// the time, at 1.8 GHz; fp32 MFMAs end at 154.
+// the time, at 1.8 GHz; fp32 MFMAs end at 154.  The 256 x 256 tiles of the fp32 weights' gradients take all 256 registers and spill 8
+// (36 bytes a lane; one is read back once a stage, the others outside the loop); no other variant spills.
 #pragma once
 
 #include "gdn_act.h"
@@ -71,7 +72,8 @@ __device__ __forceinline__ void planes(u32x4 lo, u32x4 hi, u32x4 *p) {
         }
 }
 
-// The six products of planes that fp32 asks for, small ones first.
+// Six products of planes, small ones first.  The three left out are below (2 2^-22 + 2^-30) of a product together, mostly
+// under 2^-24: sums of some dozens of products and more are off by as much in fp32.
 constexpr int kPlaneN[6] = {2, 0, 1, 1, 0, 0}, kPlaneM[6] = {0, 2, 1, 0, 1, 0};
 
 // Products of a 16-byte granule of each operand: k = 8 (bf16) or 4 (fp32) a lane.
@@ -280,6 +282,9 @@ __device__ __forceinline__ void gated_result(const GatedParams<E> &p, int m, int
         for (int q = 0; q < 8; ++q) v[q] *= u[q];
         store_row(p.h + (size_t)m * p.F, n, p.F, v);
     } else if constexpr (KIND == kGatedD) {
+        // (dg and du are operands of the next products and rounded to E for those: half a step each, so in bf16 the gradients are 2.4e-3
+        // off in place of 1.7e-3 with their own rounding alone.  A second plane for what is cut off would double those products, 400 of
+        // 660 us at 3520 rows.)
         if (n >= p.Fp) return;
         float dh[8];
         e.values(dh);
