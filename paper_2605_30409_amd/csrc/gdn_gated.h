@@ -17,8 +17,9 @@
 // g ^ (r / 2 & 7); one whose contraction runs down the rows is stored as it is in memory, granules permuted within a
 // row, and read transposed (bf16: ds_read_b64_tr_b16, fp32: element by element).  No read takes a bank twice.
 //
-// Measured (bf16, C = 2048, F = 8192): 10560 rows 589 to 622 us a call, by the card that it runs on (a library product of the
-// same operations 579 to 603), 1140 to 1200 TFLOP/s; gradient of 3520 rows 663 to 689.  What bounds it is power: on
+// Measured (bf16, C = 2048, F = 8192): 10560 rows 573 to 622 us a call, by the card that it runs on (a library product of the
+// same operations 579 to 603), 1140 to 1240 TFLOP/s; gradient of 3520 rows 657 to 689; the first 20 to 40 calls after a
+// pause take up to 13 % more.  What bounds it is power: on
 // random data the chip runs at 1.6 to 1.9 GHz, on zeros, above 2.2, the first takes 417 us.  Same card, us at 10560 rows:
 // 32 x 32 x 16 products with operands read ahead across stages in place of 16 x 16 x 32, 626 -> 604; a stage's copies in two
 // halves, a step apart, 644 -> 622; four waves of 128 x 128 in place of eight of 128 x 64: 617 (with copies as
